@@ -361,6 +361,67 @@ mb_status mb_conv_xproj(const void *x, void *state, const float *w, const float 
                         void *out, int64_t batch, int64_t width, int32_t n_out, int32_t dtype, void *ws,
                         size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * What a training step runs around the scan (Section 4 training setup), and
+ * the convolution of a prompt before its decode steps. Each call works on
+ * `stream` like the others; workspaces are 256-byte aligned, hold the status
+ * block first (left as it is by these calls) and may be shared with the other
+ * calls of one stream.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * Causal depthwise convolution (kernel size 4) with SiLU over a span: what
+ * mb_conv1d_step does, for every step of [batch, seqlen, width] at once
+ * (Table 6 "Pre-SSM 1D convolution"). With u[b, -3 .. -1] = state[b, 0 .. 2]
+ * (zeros if NULL) and u[b, t] = x[b, t]:
+ *   p[b,t,d]   = bias[d] + sum_{k < 4} w[d,k] u[b,t-3+k,d]
+ *   out[b,t,d] = p * sigmoid(p)
+ *   state_out[b, j] = u[b, seqlen-3+j], j < 3   (the window mb_conv1d_step continues from)
+ *   batch, seqlen, width : >= 0, width % 8 == 0, batch*seqlen*width <= 2^31
+ *   dtype  : of x, state, out (MB_F32 or MB_BF16); sums in fp32, out rounded once
+ *   x      : [batch, seqlen, width]; row (b, t) starts x_stride elements after
+ *            row (b, t-1). 0 means width; otherwise >= width with x_stride *
+ *            element size a multiple of 16 bytes (x may be the column block of
+ *            an in-projection's [x | z] rows)
+ *   state  : [batch, 3, width], oldest first, or NULL (zeros)
+ *   w, bias: [width, 4] fp32; [width] fp32 or NULL
+ *   out    : [batch, seqlen, width], contiguous
+ *   state_out : [batch, 3, width] or NULL; may be state itself. seqlen 0 copies the window.
+ * The outputs must not overlap anything else.
+ */
+typedef struct {
+    int64_t batch, seqlen, width;
+    int32_t dtype;
+    int32_t x_stride;
+    const void *x, *state;
+    const float *w, *bias;
+} mb_conv1d_args;
+
+mb_status mb_conv1d(const mb_conv1d_args *args, void *out, void *state_out, void *stream);
+
+/* Gradients written by mb_conv1d_backward (device pointers, overwritten). */
+typedef struct {
+    void *dx;         /* [batch, seqlen, width], dtype, rows dx_stride elements apart */
+    int64_t dx_stride; /* as x_stride: dx may be a column block of wider rows */
+    void *dstate;     /* [batch, 3, width], dtype, or NULL to skip */
+    float *dw;        /* [width, 4] */
+    float *dbias;     /* [width], or NULL to skip */
+} mb_conv1d_grads;
+
+/*
+ * Gradients of mb_conv1d given dout = dJ/dout [batch, seqlen, width] and
+ * dstate_out = dJ/dstate_out [batch, 3, width] (dtype; NULL = zeros). args: the
+ * forward's. With s = sigmoid(p) and g = dout s (1 + p (1 - s)):
+ *   du[i] = sum_{k < 4, 0 <= i+3-k < seqlen} w[k] g[i+3-k]  (+ dstate_out[i-seqlen+3] for i >= seqlen-3)
+ *   dx[i] = du[i], dstate[j] = du[j-3], dw[k] = sum_{b,t} g[t] u[t-3+k], dbias = sum_{b,t} g[t]
+ * Sums over batch rows and steps are fp32, added in an order that depends on
+ * the sizes only. ws_bytes >= mb_conv1d_backward_workspace_size (0: sizes not
+ * accepted). The outputs and the workspace must not overlap anything else.
+ */
+size_t mb_conv1d_backward_workspace_size(int64_t batch, int64_t seqlen, int64_t width);
+mb_status mb_conv1d_backward(const mb_conv1d_args *args, const void *dout, const void *dstate_out,
+                             const mb_conv1d_grads *grads, void *ws, size_t ws_bytes, void *stream);
+
 /*
  * Read and clear the status block of a workspace (blocking: waits for
  * `stream`). Returns MB_OK, or the first device-side error recorded by

@@ -33,6 +33,8 @@ struct Api {
     decltype(&mb_rmsnorm) rmsnorm;
     decltype(&mb_conv1d_step) conv1d_step;
     decltype(&mb_conv_xproj) conv_xproj;
+    decltype(&mb_conv1d) conv1d;
+    decltype(&mb_conv1d_backward) conv1d_backward;
 } api;
 
 // One call's tensors and whether all of them are as they should be.
@@ -361,6 +363,62 @@ PyObject *conv_xproj(ARGS) {
     });
 }
 
+// The arguments of a convolution over a span.
+bool fill_conv(Call &c, mb_conv1d_args &a, int x_at, int w_at, int bias_at, int state_at) {
+    a = mb_conv1d_args{};
+    const at::Tensor *x = c.get(x_at);
+    if (!x || x->dim() != 3 || !dtype_of(x, a.dtype)) return false;
+    c.on(*x);
+    const at::ScalarType ty = x->scalar_type();
+    a.batch = x->size(0); a.seqlen = x->size(1); a.width = x->size(2);
+    const int64_t S = c.row_stride(x, a.batch, a.seqlen, a.width, ty);
+    if (S > INT32_MAX) c.ok = false;
+    a.x_stride = S == a.width ? 0 : (int32_t)S;
+    a.x = c.ptr(x);
+    a.w = static_cast<const float *>(c.must(w_at, kF32, {a.width, 4}));
+    a.bias = static_cast<const float *>(c.need(bias_at, kF32, {a.width}));
+    a.state = c.need(state_at, ty, {a.batch, 3, a.width});
+    return c.ok;
+}
+
+// x, w, out, bias, state, state_out
+PyObject *conv1d(ARGS) {
+    return guarded(n, 6, [&]() -> long {
+        Call c{v};
+        mb_conv1d_args a;
+        if (!fill_conv(c, a, 0, 1, 3, 4)) return -1;
+        const at::ScalarType ty = c.get(0)->scalar_type();
+        void *out = c.must(2, ty, {a.batch, a.seqlen, a.width});
+        void *so = c.need(5, ty, {a.batch, 3, a.width});
+        if (!c.ok) return -1;
+        return call([&](void *s) { return api.conv1d(&a, out, so, s); });
+    });
+}
+
+// x, w, dout, bias, state, dstate_out, dx, dw, dbias, dstate, ws
+PyObject *conv1d_backward(ARGS) {
+    return guarded(n, 11, [&]() -> long {
+        Call c{v};
+        mb_conv1d_args a;
+        if (!fill_conv(c, a, 0, 1, 3, 4)) return -1;
+        const at::ScalarType ty = c.get(0)->scalar_type();
+        const void *dout = c.must(2, ty, {a.batch, a.seqlen, a.width});
+        const void *dso = c.need(5, ty, {a.batch, 3, a.width});
+        const at::Tensor *dx = c.get(6);
+        const int64_t S = c.row_stride(dx, a.batch, a.seqlen, a.width, ty);
+        mb_conv1d_grads g{};
+        g.dx = c.ptr(dx);
+        g.dx_stride = S == a.width ? 0 : S;
+        g.dw = static_cast<float *>(c.must(7, kF32, {a.width, 4}));
+        g.dbias = static_cast<float *>(c.need(8, kF32, {a.width}));
+        g.dstate = c.need(9, ty, {a.batch, 3, a.width});
+        size_t wb;
+        void *ws = workspace(c, 10, wb, false);
+        if (!c.ok) return -1;
+        return call([&](void *s) { return api.conv1d_backward(&a, dout, dso, &g, ws, wb, s); });
+    });
+}
+
 // init(addresses of the entry points, in Api's order)
 PyObject *init(ARGS) {
     constexpr Py_ssize_t kN = sizeof(Api) / sizeof(void *);
@@ -381,7 +439,8 @@ PyObject *init(ARGS) {
 #define DEF(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {DEF(init),     DEF(step),          DEF(step_resume), DEF(prefill), DEF(prefill_ckpt),
                          DEF(verify),   DEF(verify_resume), DEF(rollback),    DEF(accept_topk), DEF(rmsnorm),
-                         DEF(conv1d_step), DEF(conv_xproj), {nullptr, nullptr, 0, nullptr}};
+                         DEF(conv1d_step), DEF(conv_xproj), DEF(conv1d), DEF(conv1d_backward),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mbcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

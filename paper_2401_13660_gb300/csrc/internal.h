@@ -141,6 +141,20 @@ cudaError_t launch_rmsnorm(const void *add, float *residual, const float *w, flo
                            int64_t batch, int64_t width, bool bf16, cudaStream_t s);
 cudaError_t launch_conv_step(const void *x, void *state, const float *w, const float *bias, void *out,
                              int64_t batch, int64_t width, bool bf16, cudaStream_t s);
+// Causal convolution with SiLU over a span and its gradients (conv.cu). batch, width > 0.
+struct ConvParams {
+    int64_t batch, seqlen, width;
+    int64_t x_stride, dx_stride;       // elements between consecutive (b, t) rows of x and of dx
+    const void *x, *state;             // state: the window in, or null (zeros)
+    const float *w, *bias;             // bias may be null
+    void *out, *state_out;             // forward; state_out may be null or state itself
+    const void *dout, *dstate_out;     // backward; dstate_out may be null
+    void *dx, *dstate;                 // dstate may be null
+    float *dw, *dbias;                 // dbias may be null
+};
+cudaError_t launch_conv(const ConvParams &p, bool bf16, cudaStream_t s);
+size_t conv_backward_scratch(int64_t batch, int64_t seqlen, int64_t width);   // bytes of `part`
+cudaError_t launch_conv_backward(const ConvParams &p, bool bf16, float *part, cudaStream_t s);
 // Decode-step convolution fused with the x-projection (xproj.cu): supported
 // widths and output widths, the fp32 partial-sum scratch it needs, the launch.
 bool conv_xproj_supported(int64_t width, int n_out);

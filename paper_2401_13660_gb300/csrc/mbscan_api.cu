@@ -10,27 +10,19 @@
 #include <mutex>
 
 #include "../../include/mbscan.h"
+#include "checks.h"
 #include "internal.h"
 
+using mbscan::aligned16;
+using mbscan::from_cuda;
+using mbscan::kMaxTokens;
+using mbscan::overlap;
+using mbscan::Range;
+using mbscan::range_of;
 using mbscan::ScanParams;
 using mbscan::StatusBlock;
 
 namespace {
-
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-struct Range {
-    uintptr_t lo, hi;
-};
-Range range_of(const void *p, int64_t bytes) {   // a null pointer is an empty range
-    uintptr_t a = reinterpret_cast<uintptr_t>(p);
-    return Range{a, p ? a + (uintptr_t)(bytes > 0 ? bytes : 0) : a};
-}
-bool overlap(Range a, Range b) { return a.lo < b.hi && b.lo < a.hi && a.lo != a.hi && b.lo != b.hi; }
-
-// Products of sizes must stay far from int64 overflow and inside the
-// 32-bit element counts the kernels assume for token tensors.
-constexpr int64_t kMaxTokens = (int64_t)1 << 31;
 
 // Bytes spanned by B (or C): rows bc_stride elements apart.
 int64_t bc_bytes(const mb_scan_args *a) {
@@ -175,8 +167,6 @@ void plan_prefill(const mb_scan_args *args, ScanParams &p, const float *h_last, 
                           range_of(args->D, args->d_inner * 4), range_of(args->dt_bias, args->d_inner * 4)};
     use_scratch(p, nseg, shares, ws, ws_bytes, used, sizeof(used) / sizeof(used[0]));
 }
-
-mb_status from_cuda(cudaError_t e) { return e == cudaSuccess ? MB_OK : MB_ERR_CUDA; }
 
 // The prefill's rules for h_last (shared by mb_scan_prefill and
 // mb_scan_prefill_noalloc): 16-byte aligned; it may be exactly h0 (in-place

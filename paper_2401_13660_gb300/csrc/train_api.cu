@@ -1,0 +1,134 @@
+// C ABI of the operators that a training step runs around the scan: host-side
+// validation, then the launches on the caller's stream. Declarations and the
+// contract of every entry point are in include/mbscan.h.
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/mbscan.h"
+#include "checks.h"
+#include "internal.h"
+
+using mbscan::aligned16;
+using mbscan::from_cuda;
+using mbscan::kMaxTokens;
+using mbscan::overlap;
+using mbscan::Range;
+using mbscan::range_of;
+
+namespace {
+
+int64_t elem_size(int32_t dtype) { return dtype == MB_BF16 ? 2 : 4; }
+
+// Bytes spanned by `rows` rows of `width` elements, `stride` elements apart.
+int64_t strided_bytes(int64_t rows, int64_t width, int64_t stride, int64_t es) {
+    return rows > 0 && width > 0 ? ((rows - 1) * stride + width) * es : 0;
+}
+
+// A row stride in elements: 0 (contiguous), or at least the width and whole 16-byte groups.
+bool stride_ok(int64_t stride, int64_t width, int64_t es) {
+    return stride == 0 || (stride >= width && stride <= INT32_MAX && (stride * es) % 16 == 0);
+}
+
+// Scratch of a workspace: what follows its status block.
+bool ws_ok(const void *ws, size_t ws_bytes, size_t need) {
+    return ws != nullptr && ws_bytes >= need && (reinterpret_cast<uintptr_t>(ws) & 255u) == 0;
+}
+template <typename P> P *scratch_of(void *ws) {
+    return reinterpret_cast<P *>(static_cast<char *>(ws) + mbscan::kStatusBytes);
+}
+
+// Sizes and strides of a convolution: sets *any when there is something to do.
+mb_status check_conv(const mb_conv1d_args *a, bool *any) {
+    *any = false;
+    if (!a || a->batch < 0 || a->seqlen < 0 || a->width < 0) return MB_ERR_INVALID_ARG;
+    if (a->batch > kMaxTokens || a->seqlen > kMaxTokens || a->width > kMaxTokens) return MB_ERR_INVALID_ARG;
+    if (a->dtype != MB_F32 && a->dtype != MB_BF16) return MB_ERR_INVALID_ARG;
+    if (a->width % 8 != 0) return MB_ERR_UNSUPPORTED;
+    if (!stride_ok(a->x_stride, a->width, elem_size(a->dtype))) return MB_ERR_INVALID_ARG;
+    if (a->batch * a->width == 0) return MB_OK;
+    if (a->batch > kMaxTokens / a->width) return MB_ERR_INVALID_ARG;
+    if (a->seqlen > 0 && a->batch * a->width > kMaxTokens / a->seqlen) return MB_ERR_INVALID_ARG;
+    if ((a->seqlen > 0 && !a->x) || !a->w) return MB_ERR_INVALID_ARG;
+    for (const void *p : {a->x, a->state, static_cast<const void *>(a->w), static_cast<const void *>(a->bias)})
+        if (!aligned16(p)) return MB_ERR_INVALID_ARG;
+    *any = true;
+    return MB_OK;
+}
+
+mbscan::ConvParams to_conv(const mb_conv1d_args *a) {
+    mbscan::ConvParams p{};
+    p.batch = a->batch; p.seqlen = a->seqlen; p.width = a->width;
+    p.x_stride = a->x_stride ? a->x_stride : a->width;
+    p.x = a->x; p.state = a->state; p.w = a->w; p.bias = a->bias;
+    return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+mb_status mb_conv1d(const mb_conv1d_args *args, void *out, void *state_out, void *stream) {
+    bool any;
+    if (const mb_status st = check_conv(args, &any); st != MB_OK || !any) return st;
+    if ((args->seqlen > 0 && !out) || !aligned16(out) || !aligned16(state_out)) return MB_ERR_INVALID_ARG;
+    const int64_t es = elem_size(args->dtype), rows = args->batch * args->seqlen;
+    mbscan::ConvParams p = to_conv(args);
+    const int64_t window = 3 * args->batch * args->width * es;
+    const Range ro = range_of(out, rows * args->width * es), rw = range_of(state_out, window);
+    const Range ins[] = {range_of(args->x, strided_bytes(rows, args->width, p.x_stride, es)),
+                         range_of(args->w, args->width * 16), range_of(args->bias, args->width * 4)};
+    const Range rs = range_of(args->state, window);
+    for (const Range &r : ins)
+        if (overlap(ro, r) || overlap(rw, r)) return MB_ERR_INVALID_ARG;
+    if (overlap(ro, rw) || overlap(ro, rs) || (state_out != args->state && overlap(rw, rs))) return MB_ERR_INVALID_ARG;
+    if (args->seqlen == 0 && !state_out) return MB_OK;
+    p.out = out;
+    p.state_out = state_out;
+    return from_cuda(mbscan::launch_conv(p, args->dtype == MB_BF16, (cudaStream_t)stream));
+}
+
+size_t mb_conv1d_backward_workspace_size(int64_t batch, int64_t seqlen, int64_t width) {
+    mb_conv1d_args a{};
+    a.batch = batch; a.seqlen = seqlen; a.width = width;
+    a.x = a.w = reinterpret_cast<const float *>(mbscan::kStatusBytes);   // only the sizes are looked at
+    bool any;
+    if (check_conv(&a, &any) != MB_OK) return 0;
+    return mbscan::kStatusBytes + (any ? mbscan::conv_backward_scratch(batch, seqlen, width) : 0);
+}
+
+mb_status mb_conv1d_backward(const mb_conv1d_args *args, const void *dout, const void *dstate_out,
+                             const mb_conv1d_grads *grads, void *ws, size_t ws_bytes, void *stream) {
+    bool any;
+    if (const mb_status st = check_conv(args, &any); st != MB_OK) return st;
+    if (!grads) return MB_ERR_INVALID_ARG;
+    const int64_t es = elem_size(args->dtype), rows = args->batch * args->seqlen, width = args->width;
+    const mb_conv1d_grads &g = *grads;
+    if (!stride_ok(g.dx_stride, width, es)) return MB_ERR_INVALID_ARG;
+    if (width == 0) return MB_OK;
+    if (!g.dw || (rows > 0 && (!dout || !g.dx))) return MB_ERR_INVALID_ARG;
+    for (const void *q : {dout, dstate_out, static_cast<const void *>(g.dx), static_cast<const void *>(g.dstate),
+                          static_cast<const void *>(g.dw), static_cast<const void *>(g.dbias)})
+        if (!aligned16(q)) return MB_ERR_INVALID_ARG;
+    mbscan::ConvParams p = to_conv(args);
+    p.dx_stride = g.dx_stride ? g.dx_stride : width;
+    p.dout = dout; p.dstate_out = dstate_out;
+    p.dx = g.dx; p.dstate = g.dstate; p.dw = g.dw; p.dbias = g.dbias;
+    const size_t need = mb_conv1d_backward_workspace_size(args->batch, args->seqlen, width);
+    if (!ws_ok(ws, ws_bytes, need)) return MB_ERR_INVALID_ARG;
+    const int64_t window = 3 * args->batch * width * es;
+    const Range outs[] = {range_of(g.dx, strided_bytes(rows, width, p.dx_stride, es)), range_of(g.dstate, window),
+                          range_of(g.dw, width * 16), range_of(g.dbias, width * 4), range_of(ws, (int64_t)need)};
+    const Range ins[] = {range_of(args->x, strided_bytes(rows, width, p.x_stride, es)), range_of(args->state, window),
+                         range_of(args->w, width * 16), range_of(args->bias, width * 4),
+                         range_of(dout, rows * width * es), range_of(dstate_out, window)};
+    constexpr int kOuts = sizeof(outs) / sizeof(outs[0]);
+    for (int i = 0; i < kOuts; ++i) {
+        for (const Range &r : ins)
+            if (overlap(outs[i], r)) return MB_ERR_INVALID_ARG;
+        for (int j = i + 1; j < kOuts; ++j)
+            if (overlap(outs[i], outs[j])) return MB_ERR_INVALID_ARG;
+    }
+    return from_cuda(mbscan::launch_conv_backward(p, args->dtype == MB_BF16, scratch_of<float>(ws), (cudaStream_t)stream));
+}
+
+}  // extern "C"

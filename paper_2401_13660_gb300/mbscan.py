@@ -30,7 +30,8 @@ _lib = None
 _fast = None   # csrc/binding.cpp, loaded with the library
 # the entry points that binding.cpp calls, in the order of its Api struct
 _FAST = ("mb_scan_prefill", "mb_scan_verify", "mb_scan_verify_resume", "mb_scan_prefill_ckpt", "mb_step",
-         "mb_step_resume", "mb_rollback", "mb_accept_topk", "mb_rmsnorm", "mb_conv1d_step", "mb_conv_xproj")
+         "mb_step_resume", "mb_rollback", "mb_accept_topk", "mb_rmsnorm", "mb_conv1d_step", "mb_conv_xproj",
+         "mb_conv1d", "mb_conv1d_backward")
 
 MB_OK, MB_ERR_INVALID_ARG, MB_ERR_UNSUPPORTED, MB_ERR_CUDA, MB_ERR_TIMEOUT = range(5)
 MB_F32, MB_BF16 = 0, 1
@@ -61,6 +62,18 @@ class mb_scan_grads(ctypes.Structure):
     _fields_ = [("dx", ctypes.c_void_p), ("dz", ctypes.c_void_p), ("ddt", ctypes.c_void_p),
                 ("dB", ctypes.c_void_p), ("dC", ctypes.c_void_p), ("dA", ctypes.c_void_p),
                 ("dD", ctypes.c_void_p), ("ddt_bias", ctypes.c_void_p), ("dh0", ctypes.c_void_p)]
+
+
+class mb_conv1d_args(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("seqlen", ctypes.c_int64), ("width", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("x_stride", ctypes.c_int32),
+                ("x", ctypes.c_void_p), ("state", ctypes.c_void_p),
+                ("w", ctypes.c_void_p), ("bias", ctypes.c_void_p)]
+
+
+class mb_conv1d_grads(ctypes.Structure):
+    _fields_ = [("dx", ctypes.c_void_p), ("dx_stride", ctypes.c_int64), ("dstate", ctypes.c_void_p),
+                ("dw", ctypes.c_void_p), ("dbias", ctypes.c_void_p)]
 
 
 MB_CKPT_STEPS = 16
@@ -120,10 +133,15 @@ def load_library(build_if_needed: bool = True) -> ctypes.CDLL:
             lib.mb_conv_xproj_workspace_size.restype = sz
             lib.mb_conv_xproj.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, ctypes.c_int32, ctypes.c_int32,
                                           vp, sz, vp]
+            cp = ctypes.POINTER(mb_conv1d_args)
+            lib.mb_conv1d.argtypes = [cp, vp, vp, vp]
+            lib.mb_conv1d_backward_workspace_size.argtypes = [i64, i64, i64]
+            lib.mb_conv1d_backward_workspace_size.restype = sz
+            lib.mb_conv1d_backward.argtypes = [cp, vp, vp, ctypes.POINTER(mb_conv1d_grads), vp, sz, vp]
             for f in ("mb_scan_prefill", "mb_scan_verify", "mb_rollback", "mb_step", "mb_check",
                       "mb_accept_topk", "mb_step_resume", "mb_scan_prefill_ckpt", "mb_scan_backward",
                       "mb_rmsnorm", "mb_conv1d_step", "mb_selftest_timeout", "mb_scan_verify_resume",
-                      "mb_conv_xproj"):
+                      "mb_conv_xproj", "mb_conv1d", "mb_conv1d_backward"):
                 getattr(lib, f).restype = ctypes.c_int
             lib.mb_status_string.argtypes = [ctypes.c_int]
             lib.mb_status_string.restype = ctypes.c_char_p
@@ -547,6 +565,86 @@ def mb_accept_topk(logits, drafted, beta, accept=None, stream=None):
                                        int(beta), _ptr(accept), _stream(stream))
     _check(rc, "mb_accept_topk")
     return accept
+
+
+def _conv1d_args(x, w, bias, state) -> mb_conv1d_args:
+    if x.dtype not in _DTYPES:
+        raise TypeError(f"unsupported dtype {x.dtype}")
+    batch, L, width = x.shape
+    dev = x.device
+    S = _row_stride("x", x, batch, L, width, x.dtype, dev)
+    _need(w, "w", torch.float32, (width, 4), dev)
+    _need(bias, "bias", torch.float32, (width,), dev)
+    _need(state, "state", x.dtype, (batch, 3, width), dev)
+    a = mb_conv1d_args()
+    a.batch, a.seqlen, a.width, a.dtype = batch, L, width, _DTYPES[x.dtype]
+    a.x_stride = 0 if S == width else S
+    a.x, a.state, a.w, a.bias = (t.data_ptr() if t is not None else None for t in (x, state, w, bias))
+    return a
+
+
+def mb_conv1d(x, w, out, *, bias=None, state=None, state_out=None, stream=None):
+    """Causal depthwise convolution (kernel 4) with SiLU over a span: x
+    [batch, L, width] (contiguous or a column block of wider rows, strides
+    (L*S, S, 1)), out [batch, L, width]; w [width, 4], bias [width] fp32; state
+    [batch, 3, width]: the inputs before the span, oldest first (None: zeros);
+    state_out (if given): those before the next one, as mb_conv1d_step's state
+    (it may be `state` itself)."""
+    if stream is None:
+        rc = (_fast or _native()).conv1d(x, w, out, bias, state, state_out)
+        if rc >= 0:
+            _check(rc, "mb_conv1d")
+            return out
+    a = _conv1d_args(x, w, bias, state)
+    _need(out, "out", x.dtype, tuple(x.shape), x.device)
+    _need(state_out, "state_out", x.dtype, (a.batch, 3, a.width), x.device)
+    rc = load_library().mb_conv1d(ctypes.byref(a), _ptr(out), _ptr(state_out), _stream(stream))
+    _check(rc, "mb_conv1d")
+    return out
+
+
+def mb_conv1d_backward_workspace_size(batch: int, seqlen: int, width: int) -> int:
+    """Workspace bytes mb_conv1d_backward needs (0: sizes not accepted)."""
+    return int(load_library().mb_conv1d_backward_workspace_size(batch, seqlen, width))
+
+
+def mb_conv1d_backward(x, w, dout, *, bias=None, state=None, dstate_out=None, grads=None, ws=None, stream=None):
+    """Gradients of mb_conv1d given dout [batch, L, width] and dstate_out
+    [batch, 3, width] (None: zeros). Returns a dict: dx [batch, L, width]
+    (`grads["dx"]` may be a column block of wider rows), dw [width, 4] fp32,
+    dbias [width] fp32 (None without a bias, unless given), dstate [batch, 3,
+    width] (None without a state, unless given). What is missing from `grads`
+    is allocated, and ws too."""
+    if ws is not None and stream is None and grads is not None and "dx" in grads and "dw" in grads and             (bias is None or "dbias" in grads) and (state is None or "dstate" in grads):
+        rc = (_fast or _native()).conv1d_backward(x, w, dout, bias, state, dstate_out, grads["dx"], grads["dw"],
+                                                  grads.get("dbias"), grads.get("dstate"), ws)
+        if rc >= 0:
+            _check(rc, "mb_conv1d_backward")
+            return {k: grads.get(k) for k in ("dx", "dw", "dbias", "dstate")}
+    a = _conv1d_args(x, w, bias, state)
+    batch, L, width = x.shape
+    dev = x.device
+    _need(dout, "dout", x.dtype, (batch, L, width), dev)
+    _need(dstate_out, "dstate_out", x.dtype, (batch, 3, width), dev)
+    g = {k: (grads or {}).get(k) for k in ("dx", "dw", "dbias", "dstate")}
+    wanted = {"dx": True, "dw": True, "dbias": bias is not None, "dstate": state is not None}
+    shapes = {"dx": ((batch, L, width), x.dtype), "dw": ((width, 4), torch.float32),
+              "dbias": ((width,), torch.float32), "dstate": ((batch, 3, width), x.dtype)}
+    for k, (shape, dtype) in shapes.items():
+        if g[k] is None and wanted[k]:
+            g[k] = torch.empty(shape, dtype=dtype, device=dev)
+        if k != "dx":
+            _need(g[k], k, dtype, shape, dev)
+    S = _row_stride("dx", g["dx"], batch, L, width, x.dtype, dev)
+    st = mb_conv1d_grads(g["dx"].data_ptr(), 0 if S == width else S,
+                         *(None if g[k] is None else g[k].data_ptr() for k in ("dstate", "dw", "dbias")))
+    if ws is None:
+        ws = torch.zeros(max(mb_conv1d_backward_workspace_size(batch, L, width), 256), dtype=torch.uint8, device=dev)
+    _need(ws, "ws", torch.uint8, None, dev)
+    rc = load_library().mb_conv1d_backward(ctypes.byref(a), _ptr(dout), _ptr(dstate_out), ctypes.byref(st), _ptr(ws),
+                                           ws.numel(), _stream(stream))
+    _check(rc, "mb_conv1d_backward")
+    return g
 
 
 def mb_selftest_timeout(ws, wait_cycles, stream=None):
