@@ -422,6 +422,89 @@ size_t mb_conv1d_backward_workspace_size(int64_t batch, int64_t seqlen, int64_t 
 mb_status mb_conv1d_backward(const mb_conv1d_args *args, const void *dout, const void *dstate_out,
                              const mb_conv1d_grads *grads, void *ws, size_t ws_bytes, void *stream);
 
+/* Integer type of token ids. */
+typedef enum { MB_TOKEN_U8 = 0, MB_TOKEN_I32 = 1, MB_TOKEN_I64 = 2 } mb_token_type;
+
+/*
+ * Embedding with scaling: out[i] = scale * table[tokens[i]], i < n; a row of
+ * zeros where tokens[i] is outside [0, vocab) (padding).
+ *   tokens : [n], token_type (mb_token_type), aligned to its size
+ *   table  : [vocab, width], table_dtype; vocab < 2^31
+ *   out    : [n, width], out_dtype (MB_F32: the residual stream), rounded once
+ *   width % 8 == 0 and <= 2^20; n * width and vocab * width <= 2^31
+ * out must not overlap the inputs.
+ */
+mb_status mb_embed(const void *tokens, int32_t token_type, const void *table, int32_t table_dtype, float scale,
+                   void *out, int32_t out_dtype, int64_t n, int64_t vocab, int64_t width, void *stream);
+
+/*
+ * Gradient of the table, given dout = dJ/dout [n, width] (dtype):
+ *   dtable[v] = (accumulate ? dtable[v] : 0) + scale * sum of dout[i] over tokens[i] == v
+ * dtable [vocab, width] fp32; with accumulate != 0 it is added to, so that the
+ * gradient of a tied output head can be there already. The positions are
+ * sorted by token and each row's terms added in fp32 in an order that depends
+ * on the tokens only (no atomics): the result is reproducible to the last bit.
+ *   ws_bytes >= mb_embed_backward_workspace_size(n, vocab, width) (0: sizes not accepted)
+ * dtable and the workspace must not overlap the inputs or each other.
+ */
+size_t mb_embed_backward_workspace_size(int64_t n, int64_t vocab, int64_t width);
+mb_status mb_embed_backward(const void *tokens, int32_t token_type, const void *dout, int32_t dtype, float scale,
+                            int32_t accumulate, float *dtable, int64_t n, int64_t vocab, int64_t width, void *ws,
+                            size_t ws_bytes, void *stream);
+
+/*
+ * Cross entropy of next tokens and its gradient, in one call. For row i with
+ * target y = targets[i] and weight w = weight ? weight[i] : 1:
+ *   loss[i]       = -w log softmax(logits[i])[y]                  (fp32, nats)
+ *   dlogits[i, v] = scale * w * (softmax(logits[i])[v] - [v == y])
+ * Rows with w == 0, or whose target is outside [0, vocab), are zeros whatever
+ * their logits hold. A logit of -inf is a masked token (probability 0; as the
+ * target its loss is +inf); a row of nothing but -inf has no distribution: NaN.
+ *   logits  : [n, vocab], dtype, contiguous (any vocab from 1 to 2^30; n * vocab <= 2^31)
+ *   targets : [n], token_type, aligned to its size
+ *   weight  : [n] fp32 or NULL
+ *   loss    : [n] fp32
+ *   dlogits : [n, vocab], dtype, or NULL to skip; may be logits itself
+ * Statistics and sums are fp32; dlogits is rounded once.
+ */
+mb_status mb_cross_entropy(const void *logits, int32_t dtype, const void *targets, int32_t token_type,
+                           const float *weight, float scale, float *loss, void *dlogits, int64_t n, int64_t vocab,
+                           void *stream);
+
+/* One tensor of a list: numel contiguous elements of dtype at data, aligned to
+ * the element's size (16-byte aligned tensors are read faster). */
+typedef struct mb_tensor {
+    void *data;
+    int64_t numel;
+    int32_t dtype;
+    int32_t reserved;   /* 0 */
+} mb_tensor;
+
+/*
+ * Global norm of a model's gradients: norm[0] = sqrt(sum of squares over every
+ * element of every tensor), fp32. Squares are summed so that none overflows or
+ * vanishes over the fp32 range, in an order that depends on the sizes only;
+ * an infinity or NaN among the gradients gives infinity or NaN.
+ *   list  : host array of `count` tensors (read before the call returns)
+ *   norm  : [1] fp32 on the device
+ *   ws_bytes >= mb_grad_norm_workspace_size()
+ */
+size_t mb_grad_norm_workspace_size(void);
+mb_status mb_grad_norm(const mb_tensor *list, int64_t count, float *norm, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Clipping by the global norm (norm [1] on the device, as mb_grad_norm leaves
+ * it): out = g * max_norm / norm when max_norm < norm < inf, else out = g (a
+ * norm that is not finite tells the caller to skip the step; the gradients are
+ * left as they are). Each product is rounded once.
+ *   list : the gradients; out: as many tensors of the same numel, each of
+ *          either dtype (e.g. fp32 for an optimizer), not overlapping the list
+ *          unless out[i] is list[i]; or NULL: in place
+ *   max_norm > 0
+ */
+mb_status mb_grad_clip(const mb_tensor *list, const mb_tensor *out, int64_t count, const float *norm,
+                       float max_norm, void *stream);
+
 /*
  * Read and clear the status block of a workspace (blocking: waits for
  * `stream`). Returns MB_OK, or the first device-side error recorded by

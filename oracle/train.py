@@ -89,7 +89,7 @@ def cross_entropy(logits, targets, weight=None, scale=1.0):
     for i in np.nonzero(ok)[0]:
         m = np.max(l[i])
         e = np.exp(l[i] - m)
-        loss[i] = w[i] * (m + np.log(np.sum(e)) - l[i, t[i]])
+        loss[i] = w[i] * ((m - l[i, t[i]]) + np.log(np.sum(e)))   # m may be of the type's largest magnitude
         d[i] = e / np.sum(e)
         d[i, t[i]] -= 1.0
         d[i] *= w[i] * scale

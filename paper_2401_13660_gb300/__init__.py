@@ -8,7 +8,8 @@ library.
 _BINDING = ("mb_scan_prefill", "mb_scan_verify", "mb_rollback", "mb_step", "mb_step_resume", "mb_check",
             "mb_accept_topk", "mb_scan_prefill_ckpt", "mb_scan_backward", "mb_rmsnorm", "mb_conv1d_step",
             "mb_selftest_timeout", "mb_scan_verify_resume", "mb_conv1d", "mb_conv1d_backward",
-            "mb_conv1d_backward_workspace_size",
+            "mb_conv1d_backward_workspace_size", "mb_embed", "mb_embed_backward", "mb_embed_backward_workspace_size",
+            "mb_cross_entropy", "mb_tensor_list", "mb_grad_norm", "mb_grad_norm_workspace_size", "mb_grad_clip",
             "mb_workspace_size", "mb_status_string", "mb_version", "load_library", "MbError",
             "make_args", "new_workspace")
 

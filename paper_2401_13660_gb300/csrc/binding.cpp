@@ -35,6 +35,9 @@ struct Api {
     decltype(&mb_conv_xproj) conv_xproj;
     decltype(&mb_conv1d) conv1d;
     decltype(&mb_conv1d_backward) conv1d_backward;
+    decltype(&mb_embed) embed;
+    decltype(&mb_embed_backward) embed_backward;
+    decltype(&mb_cross_entropy) cross_entropy;
 } api;
 
 // One call's tensors and whether all of them are as they should be.
@@ -419,6 +422,82 @@ PyObject *conv1d_backward(ARGS) {
     });
 }
 
+bool token_type(const at::Tensor *t, int32_t &ty) {
+    if (!t) return false;
+    if (t->scalar_type() == at::kByte) ty = MB_TOKEN_U8;
+    else if (t->scalar_type() == at::kInt) ty = MB_TOKEN_I32;
+    else if (t->scalar_type() == at::kLong) ty = MB_TOKEN_I64;
+    else return false;
+    return true;
+}
+
+// Whether t's shape is that of `rows` with one more dimension of this size.
+bool rows_of(const at::Tensor *t, const at::Tensor *rows, int64_t last) {
+    return t && t->dim() == rows->dim() + 1 && t->size(-1) == last && t->sizes().slice(0, rows->dim()) == rows->sizes();
+}
+
+// tokens, table, out, scale
+PyObject *embed(ARGS) {
+    return guarded(n, 4, [&]() -> long {
+        Call c{v};
+        const at::Tensor *tok = c.get(0), *table = c.get(1), *o = c.get(2);
+        int32_t tt, dt, od;
+        if (!token_type(tok, tt) || !dtype_of(table, dt) || !dtype_of(o, od) || table->dim() != 2 ||
+            !PyFloat_CheckExact(v[3]) || !rows_of(o, tok, table->size(1)))
+            return -1;
+        const void *tp = c.must(0, tok->scalar_type(), {}, true), *wp = c.must(1, table->scalar_type(), {}, true);
+        void *op = c.must(2, o->scalar_type(), {}, true);
+        if (!c.ok) return -1;
+        const float scale = (float)PyFloat_AS_DOUBLE(v[3]);
+        const int64_t count = tok->numel(), vocab = table->size(0), width = table->size(1);
+        return call([&](void *s) { return api.embed(tp, tt, wp, dt, scale, op, od, count, vocab, width, s); });
+    });
+}
+
+// tokens, dout, dtable, scale, accumulate, ws
+PyObject *embed_backward(ARGS) {
+    return guarded(n, 6, [&]() -> long {
+        Call c{v};
+        const at::Tensor *tok = c.get(0), *d = c.get(1), *table = c.get(2);
+        int32_t tt, dt;
+        if (!token_type(tok, tt) || !dtype_of(d, dt) || !table || table->dim() != 2 || !PyFloat_CheckExact(v[3]) ||
+            !PyBool_Check(v[4]) || !rows_of(d, tok, table->size(1)))
+            return -1;
+        const void *tp = c.must(0, tok->scalar_type(), {}, true), *dp = c.must(1, d->scalar_type(), {}, true);
+        float *op = static_cast<float *>(c.must(2, kF32, {}, true));
+        size_t wb;
+        void *ws = workspace(c, 5, wb, false);
+        if (!c.ok) return -1;
+        const float scale = (float)PyFloat_AS_DOUBLE(v[3]);
+        const int32_t acc = v[4] == Py_True;
+        const int64_t count = tok->numel(), vocab = table->size(0), width = table->size(1);
+        return call([&](void *s) {
+            return api.embed_backward(tp, tt, dp, dt, scale, acc, op, count, vocab, width, ws, wb, s);
+        });
+    });
+}
+
+// logits, targets, loss, dlogits, weight, scale
+PyObject *cross_entropy(ARGS) {
+    return guarded(n, 6, [&]() -> long {
+        Call c{v};
+        const at::Tensor *l = c.get(0), *tgt = c.get(1);
+        int32_t tt, dt;
+        if (!token_type(tgt, tt) || !dtype_of(l, dt) || l->dim() < 1 || !PyFloat_CheckExact(v[5]) ||
+            !rows_of(l, tgt, l->size(-1)))
+            return -1;
+        const at::ScalarType ty = l->scalar_type();
+        const void *lp = c.must(0, ty, {}, true), *tp = c.must(1, tgt->scalar_type(), {}, true);
+        float *loss = static_cast<float *>(c.must(2, kF32, tgt->sizes()));
+        void *dl = c.need(3, ty, l->sizes());
+        const float *w = static_cast<const float *>(c.need(4, kF32, tgt->sizes()));
+        if (!c.ok) return -1;
+        const float scale = (float)PyFloat_AS_DOUBLE(v[5]);
+        const int64_t count = tgt->numel(), vocab = l->size(-1);
+        return call([&](void *s) { return api.cross_entropy(lp, dt, tp, tt, w, scale, loss, dl, count, vocab, s); });
+    });
+}
+
 // init(addresses of the entry points, in Api's order)
 PyObject *init(ARGS) {
     constexpr Py_ssize_t kN = sizeof(Api) / sizeof(void *);
@@ -440,7 +519,7 @@ PyObject *init(ARGS) {
 PyMethodDef methods[] = {DEF(init),     DEF(step),          DEF(step_resume), DEF(prefill), DEF(prefill_ckpt),
                          DEF(verify),   DEF(verify_resume), DEF(rollback),    DEF(accept_topk), DEF(rmsnorm),
                          DEF(conv1d_step), DEF(conv_xproj), DEF(conv1d), DEF(conv1d_backward),
-                         {nullptr, nullptr, 0, nullptr}};
+                         DEF(embed), DEF(embed_backward), DEF(cross_entropy), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mbcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

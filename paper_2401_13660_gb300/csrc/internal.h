@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+struct mb_tensor;   // include/mbscan.h
+
 namespace mbscan {
 
 // Layout of the workspace status block (first bytes of `ws`).
@@ -155,6 +157,20 @@ struct ConvParams {
 cudaError_t launch_conv(const ConvParams &p, bool bf16, cudaStream_t s);
 size_t conv_backward_scratch(int64_t batch, int64_t seqlen, int64_t width);   // bytes of `part`
 cudaError_t launch_conv_backward(const ConvParams &p, bool bf16, float *part, cudaStream_t s);
+// Embedding and its gradient (embed.cu). All sizes > 0 but n in the backward.
+cudaError_t launch_embed(const void *tokens, int type, const void *table, bool table_bf16, float scale, void *out,
+                         bool out_bf16, int64_t n, int vocab, int64_t width, cudaStream_t s);
+size_t embed_backward_scratch(int64_t n, int64_t width);
+cudaError_t launch_embed_backward(const void *tokens, int type, const void *dout, bool bf16, float scale, bool accumulate,
+                                  float *dtable, int64_t n, int vocab, int64_t width, void *scratch, cudaStream_t s);
+// Cross entropy with its gradient (loss.cu); weight and dlogits may be null, dlogits may be logits.
+cudaError_t launch_cross_entropy(const void *logits, bool bf16, const void *targets, int type, const float *weight,
+                                 float scale, float *out, void *dlogits, int64_t n, int vocab, cudaStream_t s);
+// Norm over a list of tensors and clipping by it (gradnorm.cu); out may be null (in place).
+size_t grad_norm_scratch();
+cudaError_t launch_grad_norm(const ::mb_tensor *in, int64_t count, float *norm, void *scratch, cudaStream_t s);
+cudaError_t launch_grad_clip(const ::mb_tensor *in, const ::mb_tensor *out, int64_t count, const float *norm,
+                             float max_norm, cudaStream_t s);
 // Decode-step convolution fused with the x-projection (xproj.cu): supported
 // widths and output widths, the fp32 partial-sum scratch it needs, the launch.
 bool conv_xproj_supported(int64_t width, int n_out);

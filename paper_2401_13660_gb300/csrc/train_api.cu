@@ -63,6 +63,36 @@ mbscan::ConvParams to_conv(const mb_conv1d_args *a) {
     return p;
 }
 
+bool dtype_ok(int32_t dtype) { return dtype == MB_F32 || dtype == MB_BF16; }
+
+// Bytes of a token id; 0 for a type that is none.
+int64_t token_size(int32_t type) {
+    return type == MB_TOKEN_U8 ? 1 : type == MB_TOKEN_I32 ? 4 : type == MB_TOKEN_I64 ? 8 : 0;
+}
+bool aligned_to(const void *p, int64_t size) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)size == 0; }
+
+constexpr int64_t kMaxEmbedWidth = (int64_t)1 << 20;
+
+mb_status check_embed(int64_t n, int64_t vocab, int64_t width) {
+    if (n < 0 || vocab < 0 || width < 0 || n > kMaxTokens || vocab >= kMaxTokens) return MB_ERR_INVALID_ARG;
+    if (width % 8 != 0 || width > kMaxEmbedWidth) return MB_ERR_UNSUPPORTED;
+    if (width > 0 && (n > kMaxTokens / width || vocab > kMaxTokens / width)) return MB_ERR_INVALID_ARG;
+    return MB_OK;
+}
+
+constexpr int64_t kMaxNumel = (int64_t)1 << 40;
+
+mb_status check_list(const mb_tensor *list, int64_t count) {
+    if (count < 0 || (count > 0 && !list)) return MB_ERR_INVALID_ARG;
+    for (int64_t i = 0; i < count; ++i) {
+        const mb_tensor &t = list[i];
+        if (t.numel < 0 || t.numel > kMaxNumel || !dtype_ok(t.dtype) || t.reserved != 0) return MB_ERR_INVALID_ARG;
+        if (t.numel > 0 && (!t.data || !aligned_to(t.data, elem_size(t.dtype)))) return MB_ERR_INVALID_ARG;
+    }
+    return MB_OK;
+}
+Range tensor_range(const mb_tensor &t) { return range_of(t.data, t.numel * elem_size(t.dtype)); }
+
 }  // namespace
 
 extern "C" {
@@ -129,6 +159,100 @@ mb_status mb_conv1d_backward(const mb_conv1d_args *args, const void *dout, const
             if (overlap(outs[i], outs[j])) return MB_ERR_INVALID_ARG;
     }
     return from_cuda(mbscan::launch_conv_backward(p, args->dtype == MB_BF16, scratch_of<float>(ws), (cudaStream_t)stream));
+}
+
+mb_status mb_embed(const void *tokens, int32_t token_type, const void *table, int32_t table_dtype, float scale,
+                   void *out, int32_t out_dtype, int64_t n, int64_t vocab, int64_t width, void *stream) {
+    const int64_t ts = token_size(token_type);
+    if (ts == 0 || !dtype_ok(table_dtype) || !dtype_ok(out_dtype)) return MB_ERR_INVALID_ARG;
+    if (const mb_status st = check_embed(n, vocab, width); st != MB_OK) return st;
+    if (n * width == 0) return MB_OK;
+    if (!tokens || !out || (vocab > 0 && !table)) return MB_ERR_INVALID_ARG;
+    if (!aligned_to(tokens, ts) || !aligned16(table) || !aligned16(out)) return MB_ERR_INVALID_ARG;
+    const Range ro = range_of(out, n * width * elem_size(out_dtype));
+    if (overlap(ro, range_of(tokens, n * ts)) || overlap(ro, range_of(table, vocab * width * elem_size(table_dtype))))
+        return MB_ERR_INVALID_ARG;
+    return from_cuda(mbscan::launch_embed(tokens, token_type, table, table_dtype == MB_BF16, scale, out,
+                                          out_dtype == MB_BF16, n, (int)vocab, width, (cudaStream_t)stream));
+}
+
+size_t mb_embed_backward_workspace_size(int64_t n, int64_t vocab, int64_t width) {
+    if (check_embed(n, vocab, width) != MB_OK) return 0;
+    return mbscan::kStatusBytes + mbscan::embed_backward_scratch(n, width);
+}
+
+mb_status mb_embed_backward(const void *tokens, int32_t token_type, const void *dout, int32_t dtype, float scale,
+                            int32_t accumulate, float *dtable, int64_t n, int64_t vocab, int64_t width, void *ws,
+                            size_t ws_bytes, void *stream) {
+    const int64_t ts = token_size(token_type);
+    if (ts == 0 || !dtype_ok(dtype)) return MB_ERR_INVALID_ARG;
+    if (const mb_status st = check_embed(n, vocab, width); st != MB_OK) return st;
+    if (vocab * width == 0) return MB_OK;
+    if (!dtable || (n > 0 && (!tokens || !dout))) return MB_ERR_INVALID_ARG;
+    if (!aligned_to(tokens, ts) || !aligned16(dout) || !aligned16(dtable)) return MB_ERR_INVALID_ARG;
+    const size_t need = mb_embed_backward_workspace_size(n, vocab, width);
+    if (!ws_ok(ws, ws_bytes, need)) return MB_ERR_INVALID_ARG;
+    const Range rd = range_of(dtable, vocab * width * 4), rw = range_of(ws, (int64_t)need);
+    const Range ins[] = {range_of(tokens, n * ts), range_of(dout, n * width * elem_size(dtype))};
+    for (const Range &r : ins)
+        if (overlap(rd, r) || overlap(rw, r)) return MB_ERR_INVALID_ARG;
+    if (overlap(rd, rw)) return MB_ERR_INVALID_ARG;
+    return from_cuda(mbscan::launch_embed_backward(tokens, token_type, dout, dtype == MB_BF16, scale, accumulate != 0,
+                                                   dtable, n, (int)vocab, width, scratch_of<char>(ws),
+                                                   (cudaStream_t)stream));
+}
+
+mb_status mb_cross_entropy(const void *logits, int32_t dtype, const void *targets, int32_t token_type,
+                           const float *weight, float scale, float *loss, void *dlogits, int64_t n, int64_t vocab,
+                           void *stream) {
+    const int64_t ts = token_size(token_type);
+    if (ts == 0 || !dtype_ok(dtype)) return MB_ERR_INVALID_ARG;
+    if (n < 0 || n > kMaxTokens || vocab < 1 || vocab > kMaxTokens / 2 || n > kMaxTokens / vocab) return MB_ERR_INVALID_ARG;
+    if (n == 0) return MB_OK;
+    if (!logits || !targets || !loss) return MB_ERR_INVALID_ARG;
+    if (!aligned16(logits) || !aligned16(dlogits) || !aligned_to(targets, ts) || !aligned_to(weight, 4) ||
+        !aligned_to(loss, 4))
+        return MB_ERR_INVALID_ARG;
+    const int64_t bytes = n * vocab * elem_size(dtype);
+    const Range rl = range_of(logits, bytes), rd = range_of(dlogits, bytes), ro = range_of(loss, n * 4);
+    const Range ins[] = {range_of(targets, n * ts), range_of(weight, n * 4)};
+    for (const Range &r : ins)
+        if (overlap(rd, r) || overlap(ro, r)) return MB_ERR_INVALID_ARG;
+    if (overlap(ro, rl) || overlap(ro, rd) || (dlogits != logits && overlap(rd, rl))) return MB_ERR_INVALID_ARG;
+    return from_cuda(mbscan::launch_cross_entropy(logits, dtype == MB_BF16, targets, token_type, weight, scale, loss,
+                                                  dlogits, n, (int)vocab, (cudaStream_t)stream));
+}
+
+size_t mb_grad_norm_workspace_size(void) { return mbscan::kStatusBytes + mbscan::grad_norm_scratch(); }
+
+mb_status mb_grad_norm(const mb_tensor *list, int64_t count, float *norm, void *ws, size_t ws_bytes, void *stream) {
+    if (const mb_status st = check_list(list, count); st != MB_OK) return st;
+    if (!norm || !aligned_to(norm, 4)) return MB_ERR_INVALID_ARG;
+    const size_t need = mb_grad_norm_workspace_size();
+    if (!ws_ok(ws, ws_bytes, need)) return MB_ERR_INVALID_ARG;
+    const Range rn = range_of(norm, 4), rw = range_of(ws, (int64_t)need);
+    if (overlap(rn, rw)) return MB_ERR_INVALID_ARG;
+    for (int64_t i = 0; i < count; ++i)
+        if (overlap(tensor_range(list[i]), rn) || overlap(tensor_range(list[i]), rw)) return MB_ERR_INVALID_ARG;
+    return from_cuda(mbscan::launch_grad_norm(list, count, norm, scratch_of<char>(ws), (cudaStream_t)stream));
+}
+
+mb_status mb_grad_clip(const mb_tensor *list, const mb_tensor *out, int64_t count, const float *norm,
+                       float max_norm, void *stream) {
+    if (const mb_status st = check_list(list, count); st != MB_OK) return st;
+    if (!norm || !aligned_to(norm, 4) || !(max_norm > 0.f)) return MB_ERR_INVALID_ARG;
+    const Range rn = range_of(norm, 4);
+    if (out) {
+        if (const mb_status st = check_list(out, count); st != MB_OK) return st;
+        for (int64_t i = 0; i < count; ++i) {
+            if (out[i].numel != list[i].numel) return MB_ERR_INVALID_ARG;
+            const bool same = out[i].data == list[i].data && out[i].dtype == list[i].dtype;
+            if (!same && overlap(tensor_range(out[i]), tensor_range(list[i]))) return MB_ERR_INVALID_ARG;
+        }
+    }
+    for (int64_t i = 0; i < count; ++i)
+        if (overlap(tensor_range((out ? out : list)[i]), rn)) return MB_ERR_INVALID_ARG;
+    return from_cuda(mbscan::launch_grad_clip(list, out, count, norm, max_norm, (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -31,11 +31,12 @@ _fast = None   # csrc/binding.cpp, loaded with the library
 # the entry points that binding.cpp calls, in the order of its Api struct
 _FAST = ("mb_scan_prefill", "mb_scan_verify", "mb_scan_verify_resume", "mb_scan_prefill_ckpt", "mb_step",
          "mb_step_resume", "mb_rollback", "mb_accept_topk", "mb_rmsnorm", "mb_conv1d_step", "mb_conv_xproj",
-         "mb_conv1d", "mb_conv1d_backward")
+         "mb_conv1d", "mb_conv1d_backward", "mb_embed", "mb_embed_backward", "mb_cross_entropy")
 
 MB_OK, MB_ERR_INVALID_ARG, MB_ERR_UNSUPPORTED, MB_ERR_CUDA, MB_ERR_TIMEOUT = range(5)
 MB_F32, MB_BF16 = 0, 1
 _DTYPES = {torch.float32: MB_F32, torch.bfloat16: MB_BF16}
+_TOKENS = {torch.uint8: 0, torch.int32: 1, torch.int64: 2}
 
 
 class MbError(RuntimeError):
@@ -74,6 +75,11 @@ class mb_conv1d_args(ctypes.Structure):
 class mb_conv1d_grads(ctypes.Structure):
     _fields_ = [("dx", ctypes.c_void_p), ("dx_stride", ctypes.c_int64), ("dstate", ctypes.c_void_p),
                 ("dw", ctypes.c_void_p), ("dbias", ctypes.c_void_p)]
+
+
+class mb_tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("numel", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 MB_CKPT_STEPS = 16
@@ -138,10 +144,22 @@ def load_library(build_if_needed: bool = True) -> ctypes.CDLL:
             lib.mb_conv1d_backward_workspace_size.argtypes = [i64, i64, i64]
             lib.mb_conv1d_backward_workspace_size.restype = sz
             lib.mb_conv1d_backward.argtypes = [cp, vp, vp, ctypes.POINTER(mb_conv1d_grads), vp, sz, vp]
+            i32, f32 = ctypes.c_int32, ctypes.c_float
+            lib.mb_embed.argtypes = [vp, i32, vp, i32, f32, vp, i32, i64, i64, i64, vp]
+            lib.mb_embed_backward_workspace_size.argtypes = [i64, i64, i64]
+            lib.mb_embed_backward_workspace_size.restype = sz
+            lib.mb_embed_backward.argtypes = [vp, i32, vp, i32, f32, i32, vp, i64, i64, i64, vp, sz, vp]
+            lib.mb_cross_entropy.argtypes = [vp, i32, vp, i32, vp, f32, vp, vp, i64, i64, vp]
+            lib.mb_grad_norm_workspace_size.argtypes = []
+            lib.mb_grad_norm_workspace_size.restype = sz
+            tp = ctypes.POINTER(mb_tensor)
+            lib.mb_grad_norm.argtypes = [tp, i64, vp, vp, sz, vp]
+            lib.mb_grad_clip.argtypes = [tp, tp, i64, vp, f32, vp]
             for f in ("mb_scan_prefill", "mb_scan_verify", "mb_rollback", "mb_step", "mb_check",
                       "mb_accept_topk", "mb_step_resume", "mb_scan_prefill_ckpt", "mb_scan_backward",
                       "mb_rmsnorm", "mb_conv1d_step", "mb_selftest_timeout", "mb_scan_verify_resume",
-                      "mb_conv_xproj", "mb_conv1d", "mb_conv1d_backward"):
+                      "mb_conv_xproj", "mb_conv1d", "mb_conv1d_backward", "mb_embed", "mb_embed_backward",
+                      "mb_cross_entropy", "mb_grad_norm", "mb_grad_clip"):
                 getattr(lib, f).restype = ctypes.c_int
             lib.mb_status_string.argtypes = [ctypes.c_int]
             lib.mb_status_string.restype = ctypes.c_char_p
@@ -645,6 +663,163 @@ def mb_conv1d_backward(x, w, dout, *, bias=None, state=None, dstate_out=None, gr
                                            ws.numel(), _stream(stream))
     _check(rc, "mb_conv1d_backward")
     return g
+
+
+def _token_type(t, name):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype not in _TOKENS:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected one of {list(_TOKENS)}")
+    return _TOKENS[t.dtype]
+
+
+def mb_embed(tokens, table, out, *, scale=1.0, stream=None):
+    """out[..., :] = scale * table[tokens] (zeros where a token is outside the
+    table): tokens uint8, int32 or int64, any shape; table [vocab, width]; out
+    [*tokens.shape, width]; table and out fp32 or bf16 each."""
+    if stream is None:
+        rc = (_fast or _native()).embed(tokens, table, out, scale)
+        if rc >= 0:
+            _check(rc, "mb_embed")
+            return out
+    tt = _token_type(tokens, "tokens")
+    for name, t in (("table", table), ("out", out)):
+        if t.dtype not in _DTYPES:
+            raise TypeError(f"{name}: unsupported dtype {t.dtype}")
+    vocab, width = table.shape
+    dev = table.device
+    _need(tokens, "tokens", None, None, dev)
+    _need(table, "table")
+    _need(out, "out", None, (*tokens.shape, width), dev)
+    rc = load_library().mb_embed(_ptr(tokens), tt, _ptr(table), _DTYPES[table.dtype], float(scale), _ptr(out),
+                                 _DTYPES[out.dtype], tokens.numel(), vocab, width, _stream(stream))
+    _check(rc, "mb_embed")
+    return out
+
+
+def mb_embed_backward_workspace_size(n: int, vocab: int, width: int) -> int:
+    """Workspace bytes mb_embed_backward needs for n tokens (0: sizes not accepted)."""
+    return int(load_library().mb_embed_backward_workspace_size(n, vocab, width))
+
+
+def mb_embed_backward(tokens, dout, dtable, *, scale=1.0, accumulate=False, ws=None, stream=None):
+    """dtable [vocab, width] fp32 = (accumulate: itself +) scale * the sum of
+    dout's rows for each token: tokens as in mb_embed, dout [*tokens.shape,
+    width] fp32 or bf16."""
+    if ws is not None and stream is None:
+        rc = (_fast or _native()).embed_backward(tokens, dout, dtable, scale, accumulate, ws)
+        if rc >= 0:
+            _check(rc, "mb_embed_backward")
+            return dtable
+    tt = _token_type(tokens, "tokens")
+    if dout.dtype not in _DTYPES:
+        raise TypeError(f"dout: unsupported dtype {dout.dtype}")
+    vocab, width = dtable.shape
+    dev = dtable.device
+    _need(tokens, "tokens", None, None, dev)
+    _need(dtable, "dtable", torch.float32)
+    _need(dout, "dout", None, (*tokens.shape, width), dev)
+    n = tokens.numel()
+    if ws is None:
+        ws = torch.zeros(max(mb_embed_backward_workspace_size(n, vocab, width), 256), dtype=torch.uint8, device=dev)
+    _need(ws, "ws", torch.uint8, None, dev)
+    rc = load_library().mb_embed_backward(_ptr(tokens), tt, _ptr(dout), _DTYPES[dout.dtype], float(scale),
+                                          int(bool(accumulate)), _ptr(dtable), n, vocab, width, _ptr(ws), ws.numel(),
+                                          _stream(stream))
+    _check(rc, "mb_embed_backward")
+    return dtable
+
+
+def mb_cross_entropy(logits, targets, loss, dlogits=None, *, weight=None, scale=1.0, stream=None):
+    """Next-token losses and the logits' gradient: logits [..., vocab] fp32 or
+    bf16; targets [...] uint8, int32 or int64 (outside the vocabulary: ignored);
+    weight [...] fp32 (0: ignored). loss [...] fp32 = -weight log softmax at the
+    target; dlogits (None: not wanted; it may be logits) = scale * the gradient
+    of the losses' sum. Returns (loss, dlogits)."""
+    if stream is None:
+        rc = (_fast or _native()).cross_entropy(logits, targets, loss, dlogits, weight, scale)
+        if rc >= 0:
+            _check(rc, "mb_cross_entropy")
+            return loss, dlogits
+    tt = _token_type(targets, "targets")
+    if logits.dtype not in _DTYPES:
+        raise TypeError(f"logits: unsupported dtype {logits.dtype}")
+    rows, vocab = tuple(logits.shape[:-1]), logits.shape[-1]
+    dev = logits.device
+    _need(logits, "logits")
+    _need(targets, "targets", None, rows, dev)
+    _need(weight, "weight", torch.float32, rows, dev)
+    _need(loss, "loss", torch.float32, rows, dev)
+    _need(dlogits, "dlogits", logits.dtype, tuple(logits.shape), dev)
+    rc = load_library().mb_cross_entropy(_ptr(logits), _DTYPES[logits.dtype], _ptr(targets), tt, _ptr(weight),
+                                         float(scale), _ptr(loss), _ptr(dlogits), targets.numel(), vocab,
+                                         _stream(stream))
+    _check(rc, "mb_cross_entropy")
+    return loss, dlogits
+
+
+class TensorList:
+    """A list of tensors as the C ABI takes it, checked once; keeps them alive."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.array = (mb_tensor * len(self.tensors))()
+        dev = getattr(self.tensors[0], "device", None) if self.tensors else None
+        for a, t in zip(self.array, self.tensors):
+            _need(t, "tensor", None, None, dev)
+            if t.dtype not in _DTYPES:
+                raise TypeError(f"unsupported dtype {t.dtype}")
+            a.data, a.numel, a.dtype = t.data_ptr(), t.numel(), _DTYPES[t.dtype]
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def mb_tensor_list(tensors) -> TensorList:
+    """The handle that mb_grad_norm and mb_grad_clip take, for tensors that stay where they are."""
+    return TensorList(tensors)
+
+
+def _tensor_list(tensors) -> TensorList:
+    return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
+
+
+def mb_grad_norm_workspace_size() -> int:
+    return int(load_library().mb_grad_norm_workspace_size())
+
+
+def mb_grad_norm(tensors, norm=None, *, ws=None, stream=None):
+    """norm [1] fp32 = the 2-norm over every element of `tensors` (an
+    mb_tensor_list, or tensors: contiguous, fp32 or bf16, on one device)."""
+    lst = _tensor_list(tensors)
+    dev = lst.tensors[0].device if len(lst) else norm.device if norm is not None else torch.device("cuda")
+    if norm is None:
+        norm = torch.empty(1, device=dev)
+    _need(norm, "norm", torch.float32, (1,), dev)
+    if ws is None:
+        ws = torch.zeros(mb_grad_norm_workspace_size(), dtype=torch.uint8, device=dev)
+    _need(ws, "ws", torch.uint8, None, dev)
+    rc = load_library().mb_grad_norm(lst.array, len(lst), _ptr(norm), _ptr(ws), ws.numel(), _stream(stream))
+    _check(rc, "mb_grad_norm")
+    return norm
+
+
+def mb_grad_clip(tensors, norm, max_norm, *, out=None, stream=None):
+    """Scale `tensors` by max_norm / norm where max_norm < norm < inf (norm [1]
+    on the device, from mb_grad_norm), in place or into `out` (as many tensors
+    of the same sizes, fp32 or bf16 each; copied where nothing is clipped)."""
+    lst = _tensor_list(tensors)
+    o = None if out is None else _tensor_list(out)
+    if o is not None and len(o) != len(lst):
+        raise ValueError(f"out has {len(o)} tensors, expected {len(lst)}")
+    for t in () if not len(lst) else (norm, *(o.tensors[:1] if o is not None else ())):
+        if t.device != lst.tensors[0].device:
+            raise ValueError(f"tensor on {t.device}, expected {lst.tensors[0].device}")
+    _need(norm, "norm", torch.float32, (1,))
+    rc = load_library().mb_grad_clip(lst.array, None if o is None else o.array, len(lst), _ptr(norm), float(max_norm),
+                                     _stream(stream))
+    _check(rc, "mb_grad_clip")
+    return tensors if out is None else out
 
 
 def mb_selftest_timeout(ws, wait_cycles, stream=None):
