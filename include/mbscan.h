@@ -443,7 +443,7 @@ mb_status mb_embed(const void *tokens, int32_t token_type, const void *table, in
  * dtable [vocab, width] fp32; with accumulate != 0 it is added to, so that the
  * gradient of a tied output head can be there already. The positions are
  * sorted by token and each row's terms added in fp32 in an order that depends
- * on the tokens only (no atomics): the result is reproducible to the last bit.
+ * on the tokens only: the result is reproducible to the last bit.
  *   ws_bytes >= mb_embed_backward_workspace_size(n, vocab, width) (0: sizes not accepted)
  * dtable and the workspace must not overlap the inputs or each other.
  */

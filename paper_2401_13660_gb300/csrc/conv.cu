@@ -72,14 +72,6 @@ struct ConvShape {
     int rows, tx, gx;
 };
 
-__device__ __forceinline__ void copy(uint4 *dst, const void *src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copy_wait() {   // all but the last N groups of this thread
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
 // sigmoid(p) of a pair; e^-p of the accuracy that T wants.
 template <typename T> __device__ __forceinline__ float2 sigmoid2(float2 p);
 template <> __device__ __forceinline__ float2 sigmoid2<__nv_bfloat16>(float2 p) {
@@ -158,11 +150,11 @@ __global__ void __launch_bounds__(kFwdThreads, kFwdCtas)
     const auto issue = [&](int r) {   // stage of the rows from r on
         if (r + kStage <= n) {
 #pragma unroll
-            for (int j = 0; j < kStage; ++j) copy(mine + (slot + j) * kFwdThreads, src + j * s.x_stride);
+            for (int j = 0; j < kStage; ++j) copy16(mine + (slot + j) * kFwdThreads, src + j * s.x_stride);
         } else {
 #pragma unroll
             for (int j = 0; j < kStage - 1; ++j)
-                if (r + j < n) copy(mine + (slot + j) * kFwdThreads, src + j * s.x_stride);
+                if (r + j < n) copy16(mine + (slot + j) * kFwdThreads, src + j * s.x_stride);
         }
         src += kStage * s.x_stride;
         copy_commit();
@@ -237,8 +229,8 @@ __global__ void __launch_bounds__(kBwdThreads, kBwdCtas<T>)
         int slot = 0;
         const auto issue = [&](int r) {
             const auto one = [&](int j) {
-                copy(mine + 2 * (slot + j) * kBwdThreads, xs + j * s.x_stride);
-                copy(mine + (2 * (slot + j) + 1) * kBwdThreads, gs + j * s.width);
+                copy16(mine + 2 * (slot + j) * kBwdThreads, xs + j * s.x_stride);
+                copy16(mine + (2 * (slot + j) + 1) * kBwdThreads, gs + j * s.width);
             };
             if (r + kStage <= m) {
 #pragma unroll

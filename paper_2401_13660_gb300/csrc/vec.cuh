@@ -41,6 +41,16 @@ template <typename T> __device__ __forceinline__ void st16(T *p, const float (&v
     *reinterpret_cast<uint4 *>(p) = narrow(v);
 }
 
+// Asynchronous 16-byte copies of a thread to shared memory, in groups that the thread waits for.
+__device__ __forceinline__ void copy16(uint4 *dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src)
+                 : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() {   // for all but the last N groups
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
 // N consecutive floats, 16-byte aligned.
 template <int N> __device__ __forceinline__ void ldf(const float *p, float (&v)[N]) {
     static_assert(N % 4 == 0, "whole 16-byte groups");
