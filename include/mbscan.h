@@ -487,7 +487,8 @@ typedef struct mb_tensor {
  * an infinity or NaN among the gradients gives infinity or NaN.
  *   list  : host array of `count` tensors (read before the call returns)
  *   norm  : [1] fp32 on the device
- *   ws_bytes >= mb_grad_norm_workspace_size()
+ *   ws_bytes >= mb_grad_norm_workspace_size(); the first 256 bytes start zeroed
+ *   (once after allocation, as for mb_scan_prefill) and are left zeroed
  */
 size_t mb_grad_norm_workspace_size(void);
 mb_status mb_grad_norm(const mb_tensor *list, int64_t count, float *norm, void *ws, size_t ws_bytes, void *stream);

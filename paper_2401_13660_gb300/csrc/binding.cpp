@@ -38,6 +38,8 @@ struct Api {
     decltype(&mb_embed) embed;
     decltype(&mb_embed_backward) embed_backward;
     decltype(&mb_cross_entropy) cross_entropy;
+    decltype(&mb_grad_norm) grad_norm;
+    decltype(&mb_grad_clip) grad_clip;
 } api;
 
 // One call's tensors and whether all of them are as they should be.
@@ -498,6 +500,51 @@ PyObject *cross_entropy(ARGS) {
     });
 }
 
+// The array of a tensor list (mbscan.py's TensorList, which has checked its tensors) and its length.
+bool tensor_list(Call &c, int at, int count_at, const mb_tensor *&list, int64_t &count) {
+    if (!PyLong_CheckExact(c.v[at]) || !PyLong_CheckExact(c.v[count_at])) return false;
+    list = static_cast<const mb_tensor *>(PyLong_AsVoidPtr(c.v[at]));
+    count = PyLong_AsLongLong(c.v[count_at]);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        return false;
+    }
+    return true;
+}
+
+// address, count, the list's first tensor, norm, ws
+PyObject *grad_norm(ARGS) {
+    return guarded(n, 5, [&]() -> long {
+        Call c{v};
+        const mb_tensor *list;
+        int64_t count;
+        const at::Tensor *first = c.get(2);
+        if (!tensor_list(c, 0, 1, list, count) || !first || !c.on(*first)) return -1;
+        float *norm = static_cast<float *>(c.must(3, kF32, {1}));
+        size_t wb;
+        void *ws = workspace(c, 4, wb, false);
+        if (!c.ok) return -1;
+        return call([&](void *s) { return api.grad_norm(list, count, norm, ws, wb, s); });
+    });
+}
+
+// address, count, the list's first tensor, norm, max_norm, the outputs' address (0: in place), their first tensor or None
+PyObject *grad_clip(ARGS) {
+    return guarded(n, 7, [&]() -> long {
+        Call c{v};
+        const mb_tensor *list, *out;
+        int64_t count;
+        const at::Tensor *first = c.get(2), *first_out = c.get(6);
+        if (!tensor_list(c, 0, 1, list, count) || !tensor_list(c, 5, 1, out, count) || !first || !c.on(*first) ||
+            (first_out && !c.on(*first_out)) || !PyFloat_CheckExact(v[4]))
+            return -1;
+        const float *norm = static_cast<const float *>(c.must(3, kF32, {1}));
+        if (!c.ok) return -1;
+        const float most = (float)PyFloat_AS_DOUBLE(v[4]);
+        return call([&](void *s) { return api.grad_clip(list, out, count, norm, most, s); });
+    });
+}
+
 // init(addresses of the entry points, in Api's order)
 PyObject *init(ARGS) {
     constexpr Py_ssize_t kN = sizeof(Api) / sizeof(void *);
@@ -519,7 +566,8 @@ PyObject *init(ARGS) {
 PyMethodDef methods[] = {DEF(init),     DEF(step),          DEF(step_resume), DEF(prefill), DEF(prefill_ckpt),
                          DEF(verify),   DEF(verify_resume), DEF(rollback),    DEF(accept_topk), DEF(rmsnorm),
                          DEF(conv1d_step), DEF(conv_xproj), DEF(conv1d), DEF(conv1d_backward),
-                         DEF(embed), DEF(embed_backward), DEF(cross_entropy), {nullptr, nullptr, 0, nullptr}};
+                         DEF(embed), DEF(embed_backward), DEF(cross_entropy), DEF(grad_norm), DEF(grad_clip),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mbcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -168,7 +168,8 @@ cudaError_t launch_cross_entropy(const void *logits, bool bf16, const void *targ
                                  float scale, float *out, void *dlogits, int64_t n, int vocab, cudaStream_t s);
 // Norm over a list of tensors and clipping by it (gradnorm.cu); out may be null (in place).
 size_t grad_norm_scratch();
-cudaError_t launch_grad_norm(const ::mb_tensor *in, int64_t count, float *norm, void *scratch, cudaStream_t s);
+cudaError_t launch_grad_norm(const ::mb_tensor *in, int64_t count, float *norm, StatusBlock *status, void *scratch,
+                             cudaStream_t s);
 cudaError_t launch_grad_clip(const ::mb_tensor *in, const ::mb_tensor *out, int64_t count, const float *norm,
                              float max_norm, cudaStream_t s);
 // Decode-step convolution fused with the x-projection (xproj.cu): supported

@@ -11,13 +11,20 @@
 #include <algorithm>
 
 #include "cluster.cuh"
+#include "pairs.cuh"
 #include "tokens.cuh"
 #include "vec.cuh"
 
 namespace mbscan {
 namespace {
 
-constexpr int kWarpVocab = 1024, kWarpRows = 8, kRowThreads = 512, kSms = 152;
+constexpr int kWarpVocab = 1024, kSms = 152;
+// Warps of a CTA, rows of a warp. 65536 x 256 bf16: 2 and 2 14.3 us, 4 and 2 14.7, 8 and 2 15.7, 2 and 4 14.7, 4 and 4 15.1;
+// warps that stay and fetch rows ahead 19.
+constexpr int kWarpRows = 2, kRows = 2;
+// Threads of a long row, 16-byte groups loaded at once by each. 1003 x 32001 fp32: 512 and 8 43.3 us, 4 51.1, 16 51.2;
+// 1024 and 4 47.3, 256 and 8 51.5.
+constexpr int kRowThreads = 512, kAhead = 8;
 
 struct LossArgs {
     const void *targets;
@@ -35,86 +42,115 @@ __device__ __forceinline__ int target_of(const LossArgs &a, int64_t row, float &
     return w == 0.f ? -1 : y;
 }
 
-// The same for rows that are read anyway: no target when it counts for nothing.
-struct Row {
-    int y;
-    float w;
-};
+// e^x for x = l - m <= 0, both types: on the SFU, within (1.5 |x| + 4) 2^-24 relative. What is far below the maximum
+// weighs as little in the sums as its error does in the gradient (expf takes four times the instructions).
+__device__ __forceinline__ float2 exp2_of(float2 l, float2 minus_m) {
+    const float2 t = mul2(add2(l, minus_m), splat(kLog2e));
+    return make_float2(ex2(t.x), ex2(t.y));
+}
+__device__ __forceinline__ float exp_of(float x) { return ex2(x * kLog2e); }
 
-// A row of whole 16-byte groups, G per lane (lane l has groups l, l + 32, ...); a warp takes R rows at a time.
+// A 16-byte group as pairs.
+template <typename T> constexpr int kPairs = kVec<T> / 2;
+template <typename T> __device__ __forceinline__ void to_pairs(const uint4 &q, float2 (&v)[kPairs<T>]) {
+    float f[kVec<T>];
+    widen(q, f);
+#pragma unroll
+    for (int j = 0; j < kPairs<T>; ++j) v[j] = make_float2(f[2 * j], f[2 * j + 1]);
+}
+template <typename T> __device__ __forceinline__ uint4 from_pairs(const float2 (&v)[kPairs<T>]) {
+    float f[kVec<T>];
+#pragma unroll
+    for (int j = 0; j < kPairs<T>; ++j) {
+        f[2 * j] = v[j].x;
+        f[2 * j + 1] = v[j].y;
+    }
+    return narrow(f);
+}
+// A group of masked logits (-inf): neither the maximum nor a sum changes by it.
+template <typename T> __device__ __forceinline__ uint4 masked() {
+    const unsigned w = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+    return make_uint4(w, w, w, w);
+}
+
+// Maximum over a warp; a NaN is passed over.
+__device__ __forceinline__ float warp_max(float v) {
+    float m;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+    return m;
+}
+
+// Rows of whole 16-byte groups, G per lane (lane l has groups l, l + 32, ...); a warp takes R rows at a time, side by
+// side, for the loads and the chains of shuffles.
 template <typename T, int G, int R>
 __global__ void __launch_bounds__(32 * kWarpRows) loss_groups_kernel(const T *logits, T *dlogits, const LossArgs a) {
-    constexpr int V = kVec<T>;
+    constexpr int V = kVec<T>, P = kPairs<T>;
     pdl_wait();
     const int lane = threadIdx.x & 31, groups = a.vocab / V;
     const int64_t row0 = ((int64_t)blockIdx.x * kWarpRows + threadIdx.x / 32) * R;
+    if (row0 >= a.n) return;
     uint4 raw[R][G];
-    Row of[R];
+    int y[R];   // -1: the row counts for nothing, whatever its logits hold
+    float w[R], at[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const bool in = row0 + r < a.n;
-        of[r].y = -1;
-        if (in) of[r].y = target_of(a, row0 + r, of[r].w);
+        const int64_t row = min(row0 + r, a.n - 1);   // beyond the last: that one again, not stored
+        const T *l = logits + row * a.vocab;
+#pragma unroll
+        for (int g = 0; g < G; ++g) raw[r][g] = g * 32 + lane < groups ? ld16(l + (g * 32 + lane) * V) : masked<T>();
+        y[r] = target_of(a, row, w[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) at[r] = to_f32(logits[min(row0 + r, a.n - 1) * a.vocab + max(y[r], 0)]);
+    float2 x[R][G][P];
+    float m[R], s[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        m[r] = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            to_pairs<T>(raw[r][g], x[r][g]);
+#pragma unroll
+            for (int j = 0; j < P; ++j) m[r] = fmaxf(m[r], fmaxf(x[r][g][j].x, x[r][g][j].y));
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) m[r] = warp_max(m[r]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        float2 sum = splat(0.f);
 #pragma unroll
         for (int g = 0; g < G; ++g)
-            if (in && g * 32 + lane < groups) raw[r][g] = ld16(logits + (row0 + r) * a.vocab + (g * 32 + lane) * V);
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                x[r][g][j] = exp2_of(x[r][g][j], splat(-m[r]));
+                sum = add2(sum, x[r][g][j]);
+            }
+        s[r] = sum.x + sum.y;
     }
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2)
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r] += __shfl_xor_sync(kFull, s[r], o);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         if (row0 + r >= a.n) break;
-        const int y = of[r].y;
-        T *d = dlogits ? dlogits + (row0 + r) * a.vocab : nullptr;
-        if (y < 0) {   // whatever the logits hold
-            if (lane == 0) a.loss[row0 + r] = 0.f;
-#pragma unroll
-            for (int g = 0; g < G; ++g)
-                if (d && g * 32 + lane < groups)
-                    *reinterpret_cast<uint4 *>(d + (g * 32 + lane) * V) = make_uint4(0, 0, 0, 0);
-            continue;
-        }
-        float x[G][V];
-        float m = -INFINITY, at = 0.f, s = 0.f;
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            if (g * 32 + lane < groups) {
-                widen(raw[r][g], x[g]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) x[g][j] = -INFINITY;
-            }
-            const int hit = y - (g * 32 + lane) * V;   // 0 .. V-1: the target is in this group
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                m = fmaxf(m, x[g][j]);
-                if (hit == j) at = x[g][j];
-            }
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o /= 2) m = fmaxf(m, __shfl_xor_sync(kFull, m, o));
-        at = __shfl_sync(kFull, at, y / V & 31);
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            const bool in = g * 32 + lane < groups;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                x[g][j] = in ? exp_for<T>(x[g][j] - m) : 0.f;
-                s += x[g][j];
-            }
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o /= 2) s += __shfl_xor_sync(kFull, s, o);
-        const float w = of[r].w, c = w * a.scale, k = c / s;
-        if (lane == 0) a.loss[row0 + r] = w * ((m - at) + logf(s));
-        if (!d) continue;
+        const bool counts = y[r] >= 0;
+        const float c = w[r] * a.scale, k = __fdividef(c, s[r]);
+        if (lane == 0) a.loss[row0 + r] = counts ? w[r] * ((m[r] - at[r]) + logf(s[r])) : 0.f;
+        if (!dlogits) continue;
+        T *d = dlogits + (row0 + r) * a.vocab;
+        const T hot = from_f32<T>(fmaf(exp_of(at[r] - m[r]), k, -c));
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             if (g * 32 + lane >= groups) break;
-            const int hit = y - (g * 32 + lane) * V;
-            float o[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) o[j] = hit == j ? fmaf(x[g][j], k, -c) : x[g][j] * k;
-            st16(d + (g * 32 + lane) * V, o);
+            for (int j = 0; j < P; ++j) x[r][g][j] = mul2(x[r][g][j], splat(k));
+            uint4 q = from_pairs<T>(x[r][g]);
+            if (!counts) q = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4 *>(d + (g * 32 + lane) * V) = q;
         }
+        if (counts && y[r] / V % 32 == lane) d[y[r]] = hot;   // over what this lane has just stored
     }
 }
 
@@ -149,12 +185,12 @@ __global__ void __launch_bounds__(32 * kWarpRows) loss_warp_kernel(const T *logi
     at = __shfl_sync(kFull, at, y & 31);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-        x[j] = j * 32 + lane < a.vocab ? exp_for<T>(x[j] - m) : 0.f;
+        x[j] = exp_of(x[j] - m);
         s += x[j];
     }
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) s += __shfl_xor_sync(kFull, s, o);
-    const float c = w * a.scale, k = c / s;
+    const float c = w * a.scale, k = __fdividef(c, s);
     if (lane == 0) a.loss[row] = w * ((m - at) + logf(s));
     if (!d) return;
 #pragma unroll
@@ -167,30 +203,32 @@ __global__ void __launch_bounds__(32 * kWarpRows) loss_warp_kernel(const T *logi
 // Running maximum m and sum s of exp(x - m); nothing yet: m = -inf, s = 0. A NaN stays in s.
 struct Running {
     float m = -INFINITY, s = 0.f;
-    template <typename T, int N> __device__ __forceinline__ void add(const float (&x)[N]) {
+    // masked logits only, so far: their exp(-inf - 0) = 0
+    static __device__ __forceinline__ float reference(float top) { return top == -INFINITY ? 0.f : top; }
+    template <int N> __device__ __forceinline__ void add(const float2 (&x)[N]) {
         float top = m;
 #pragma unroll
-        for (int j = 0; j < N; ++j) top = fmaxf(top, x[j]);
-        const float ref = top == -INFINITY ? 0.f : top;   // masked logits only, so far: exp(-inf) = 0
-        s *= exp_for<T>(m - ref);
+        for (int j = 0; j < N; ++j) top = fmaxf(top, fmaxf(x[j].x, x[j].y));
+        const float ref = reference(top);
+        float2 sum = make_float2(s * exp_of(m - ref), 0.f);
 #pragma unroll
-        for (int j = 0; j < N; ++j) s += exp_for<T>(x[j] - ref);
+        for (int j = 0; j < N; ++j) sum = add2(sum, exp2_of(x[j], splat(-ref)));
+        s = sum.x + sum.y;
         m = top;
     }
-    template <typename T> __device__ __forceinline__ void join(float m2, float s2) {
-        const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
-        s = s * exp_for<T>(m - ref) + s2 * exp_for<T>(m2 - ref);
+    __device__ __forceinline__ void join(float m2, float s2) {
+        const float top = fmaxf(m, m2), ref = reference(top);
+        s = s * exp_of(m - ref) + s2 * exp_of(m2 - ref);
         m = top;
     }
 };
 
 // A row per cluster of C CTAs: each takes a contiguous part of the row's whole 16-byte groups, the first and the last
 // also the elements before and behind them (rows of odd length begin at any element).
-constexpr int kAhead = 4;   // groups loaded at once by a thread
 template <typename T, int C>
 __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kRowThreads) loss_row_kernel(const T *logits, T *dlogits,
                                                                                        const LossArgs a) {
-    constexpr int V = kVec<T>;
+    constexpr int V = kVec<T>, P = kPairs<T>;
     __shared__ float sm[kRowThreads / 32], ss[kRowThreads / 32], mine[2];
     pdl_wait();
     const int tid = threadIdx.x, part = blockIdx.x % C;
@@ -217,29 +255,29 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kRowThreads) loss_ro
     const float at = to_f32(l[y]);
     const float own = odd >= 0 ? to_f32(l[odd]) : -INFINITY;
     Running run;
-    if (odd >= 0) {
-        const float x[1] = {own};
-        run.add<T>(x);
+    {
+        const float2 x[1] = {make_float2(own, -INFINITY)};
+        run.add(x);
     }
     for (int g = g0 + tid; g < g1; g += kAhead * kRowThreads) {
         uint4 raw[kAhead];
-        float x[kAhead * V];
+        float2 x[kAhead * P];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-            if (g + k * kRowThreads < g1) raw[k] = ld16(l + head + (int64_t)(g + k * kRowThreads) * V);
+            raw[k] = g + k * kRowThreads < g1 ? ld16(l + head + (int64_t)(g + k * kRowThreads) * V) : masked<T>();
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            float v[V];
-            widen(raw[k], v);
+            float2 v[P];
+            to_pairs<T>(raw[k], v);
 #pragma unroll
-            for (int j = 0; j < V; ++j) x[k * V + j] = g + k * kRowThreads < g1 ? v[j] : -INFINITY;
+            for (int j = 0; j < P; ++j) x[k * P + j] = v[j];
         }
-        run.add<T>(x);
+        run.add(x);
     }
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) {
         const float m2 = __shfl_xor_sync(kFull, run.m, o), s2 = __shfl_xor_sync(kFull, run.s, o);
-        run.join<T>(m2, s2);
+        run.join(m2, s2);
     }
     if ((tid & 31) == 0) {
         sm[tid / 32] = run.m;
@@ -249,7 +287,7 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kRowThreads) loss_ro
     run.m = sm[0];
     run.s = ss[0];
 #pragma unroll
-    for (int i = 1; i < kRowThreads / 32; ++i) run.join<T>(sm[i], ss[i]);
+    for (int i = 1; i < kRowThreads / 32; ++i) run.join(sm[i], ss[i]);
     if constexpr (C > 1) {
         if (tid == 0) {
             mine[0] = run.m;
@@ -259,18 +297,15 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kRowThreads) loss_ro
         cluster_wait();
         Running all;
 #pragma unroll
-        for (int i = 0; i < C; ++i) all.join<T>(cluster_load(&mine[0], i), cluster_load(&mine[1], i));
+        for (int i = 0; i < C; ++i) all.join(cluster_load(&mine[0], i), cluster_load(&mine[1], i));
         run = all;
         cluster_arrive();   // has read the others'; waited for at the end
     }
-    const float c = w * a.scale, k = c / run.s, m = run.m;
+    const float c = w * a.scale, k = __fdividef(c, run.s), m = run.m;
     if (tid == 0 && part == 0) a.loss[row] = w * ((m - at) + logf(run.s));
     if (d) {
-        const auto grad = [&](float x, int v) {
-            const float e = exp_for<T>(x - m);
-            return v == y ? fmaf(e, k, -c) : e * k;
-        };
-        if (odd >= 0) d[odd] = from_f32<T>(grad(own, odd));
+        const T hot = from_f32<T>(fmaf(exp_of(at - m), k, -c));
+        if (odd >= 0) d[odd] = odd == y ? hot : from_f32<T>(exp_of(own - m) * k);
         for (int g = g0 + tid; g < g1; g += kAhead * kRowThreads) {
             uint4 raw[kAhead];
 #pragma unroll
@@ -280,11 +315,12 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kRowThreads) loss_ro
             for (int q = 0; q < kAhead; ++q) {
                 if (g + q * kRowThreads >= g1) break;
                 const int v0 = head + (g + q * kRowThreads) * V;
-                float v[V];
-                widen(raw[q], v);
+                float2 v[P];
+                to_pairs<T>(raw[q], v);
 #pragma unroll
-                for (int j = 0; j < V; ++j) v[j] = grad(v[j], v0 + j);
-                st16(d + v0, v);
+                for (int j = 0; j < P; ++j) v[j] = mul2(exp2_of(v[j], splat(-m)), splat(k));
+                *reinterpret_cast<uint4 *>(d + v0) = from_pairs<T>(v);
+                if (y >= v0 && y < v0 + V) d[y] = hot;   // over what this thread has just stored
             }
         }
     }
@@ -311,14 +347,12 @@ cudaError_t loss(const LossArgs &a, const void *logits, void *dlogits, cudaStrea
     const auto warps = [&](auto kernel, int rows) {
         return run(kernel, (a.n + kWarpRows * rows - 1) / (kWarpRows * rows), 32 * kWarpRows);
     };
-    if (a.vocab % kVec<T> != 0) {
-        if (a.vocab <= 256) return warps(loss_warp_kernel<T, 8>, 1);
-        return warps(loss_warp_kernel<T, kWarpVocab / 32>, 1);
-    }
+    if (a.vocab % kVec<T> != 0)
+        return warps(a.vocab <= 256 ? loss_warp_kernel<T, 8> : loss_warp_kernel<T, kWarpVocab / 32>, 1);
     constexpr int kMost = kWarpVocab / 32 / kVec<T>;   // groups of a lane: 4 (bf16), 8 (fp32)
     const int groups = (a.vocab / kVec<T> + 31) / 32;
-    if (groups <= kMost / 4) return warps(loss_groups_kernel<T, kMost / 4, 2>, 2);
-    if (groups <= kMost / 2) return warps(loss_groups_kernel<T, kMost / 2, 1>, 1);
+    if (groups <= kMost / 4) return warps(loss_groups_kernel<T, kMost / 4, kRows>, kRows);
+    if (groups <= kMost / 2) return warps(loss_groups_kernel<T, kMost / 2, kRows>, kRows);
     return warps(loss_groups_kernel<T, kMost, 1>, 1);
 }
 

@@ -234,7 +234,8 @@ mb_status mb_grad_norm(const mb_tensor *list, int64_t count, float *norm, void *
     if (overlap(rn, rw)) return MB_ERR_INVALID_ARG;
     for (int64_t i = 0; i < count; ++i)
         if (overlap(tensor_range(list[i]), rn) || overlap(tensor_range(list[i]), rw)) return MB_ERR_INVALID_ARG;
-    return from_cuda(mbscan::launch_grad_norm(list, count, norm, scratch_of<char>(ws), (cudaStream_t)stream));
+    return from_cuda(mbscan::launch_grad_norm(list, count, norm, static_cast<mbscan::StatusBlock *>(ws), scratch_of<char>(ws),
+                                              (cudaStream_t)stream));
 }
 
 mb_status mb_grad_clip(const mb_tensor *list, const mb_tensor *out, int64_t count, const float *norm,

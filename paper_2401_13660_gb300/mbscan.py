@@ -31,7 +31,8 @@ _fast = None   # csrc/binding.cpp, loaded with the library
 # the entry points that binding.cpp calls, in the order of its Api struct
 _FAST = ("mb_scan_prefill", "mb_scan_verify", "mb_scan_verify_resume", "mb_scan_prefill_ckpt", "mb_step",
          "mb_step_resume", "mb_rollback", "mb_accept_topk", "mb_rmsnorm", "mb_conv1d_step", "mb_conv_xproj",
-         "mb_conv1d", "mb_conv1d_backward", "mb_embed", "mb_embed_backward", "mb_cross_entropy")
+         "mb_conv1d", "mb_conv1d_backward", "mb_embed", "mb_embed_backward", "mb_cross_entropy",
+         "mb_grad_norm", "mb_grad_clip")
 
 MB_OK, MB_ERR_INVALID_ARG, MB_ERR_UNSUPPORTED, MB_ERR_CUDA, MB_ERR_TIMEOUT = range(5)
 MB_F32, MB_BF16 = 0, 1
@@ -770,6 +771,7 @@ class TensorList:
             if t.dtype not in _DTYPES:
                 raise TypeError(f"unsupported dtype {t.dtype}")
             a.data, a.numel, a.dtype = t.data_ptr(), t.numel(), _DTYPES[t.dtype]
+        self.address = ctypes.addressof(self.array)
 
     def __len__(self):
         return len(self.tensors)
@@ -791,6 +793,11 @@ def mb_grad_norm_workspace_size() -> int:
 def mb_grad_norm(tensors, norm=None, *, ws=None, stream=None):
     """norm [1] fp32 = the 2-norm over every element of `tensors` (an
     mb_tensor_list, or tensors: contiguous, fp32 or bf16, on one device)."""
+    if type(tensors) is TensorList and len(tensors) and norm is not None and ws is not None and stream is None:
+        rc = (_fast or _native()).grad_norm(tensors.address, len(tensors), tensors.tensors[0], norm, ws)
+        if rc >= 0:
+            _check(rc, "mb_grad_norm")
+            return norm
     lst = _tensor_list(tensors)
     dev = lst.tensors[0].device if len(lst) else norm.device if norm is not None else torch.device("cuda")
     if norm is None:
@@ -808,6 +815,13 @@ def mb_grad_clip(tensors, norm, max_norm, *, out=None, stream=None):
     """Scale `tensors` by max_norm / norm where max_norm < norm < inf (norm [1]
     on the device, from mb_grad_norm), in place or into `out` (as many tensors
     of the same sizes, fp32 or bf16 each; copied where nothing is clipped)."""
+    if type(tensors) is TensorList and len(tensors) and stream is None and (
+            out is None or type(out) is TensorList and len(out) == len(tensors)):
+        rc = (_fast or _native()).grad_clip(tensors.address, len(tensors), tensors.tensors[0], norm, max_norm,
+                                            0 if out is None else out.address, None if out is None else out.tensors[0])
+        if rc >= 0:
+            _check(rc, "mb_grad_clip")
+            return tensors if out is None else out
     lst = _tensor_list(tensors)
     o = None if out is None else _tensor_list(out)
     if o is not None and len(o) != len(lst):
