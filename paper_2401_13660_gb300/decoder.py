@@ -1,7 +1,7 @@
 """Recurrent decoding of a whole MambaByte model on the library's kernels.
 
 One call of `Decoder.step` generates the next byte of every stream: byte
-embedding, then per layer the Mamba block of MambaByte (Figure 6; Table 6 rows
+embedding (mb_embed), then per layer the Mamba block of MambaByte (Figure 6; Table 6 rows
 "Linear projections", "Pre-SSM 1D convolution", "Delta, B, C from input x",
 the scan rows, "Element-wise gating"):
 
@@ -124,7 +124,7 @@ class Decoder:
 
     def _forward(self, trace=None):
         cfg = self.cfg
-        self.residual.copy_(self.emb.index_select(0, self.tokens).float())
+        mb.mb_embed(self.tokens, self.emb, self.residual)
         add = None
         R, N = cfg.dt_rank, cfg.d_state
         hb = self.h.unsqueeze(0).expand(2, -1, -1)
