@@ -360,7 +360,6 @@ __global__ void __launch_bounds__(kSumThreads, kSumCtas) embed_sum_kernel(const 
     extern __shared__ uint4 smem[];   // [kSumStages * kSumStage][kSumThreads]
     __shared__ int keys_of[kMostRows + 2 * kMostTy], perm_of[kMostRows];
     __shared__ int64_t begin_of[kMostTy], end_of[kMostTy];   // pieces where the run that enters begins, that leaves ends
-    __shared__ int valid_of[kMostTy];                        // positions of tokens of the table (the others sort last)
     __shared__ int joins[kMostTy];                           // bit 0, 1: this CTA joins the one that enters, leaves
     pdl_wait();
     if (blockIdx.x >= a.sum_blocks) {
@@ -376,31 +375,20 @@ __global__ void __launch_bounds__(kSumThreads, kSumCtas) embed_sum_kernel(const 
     const auto key_at = [&](int64_t i) { return i >= 0 && i < a.n ? a.keys[i] : -1; };
     for (int i = x; i < count + 2; i += a.tx) keys[i] = key_at(p0 + i - 1);   // and the neighbours' keys
     for (int i = x; i < count; i += a.tx) perm[i] = a.perm[p0 + i];
-    const int lane = threadIdx.x & 31;
-    for (int g = threadIdx.x / 32; g < ty; g += kSumThreads / 32) {   // a warp: where the runs at a piece's ends lie
-        const int64_t p = piece0 + g, q0 = p * a.piece, q1 = q0 + a.piece;
-        const int enters = key_at(q0), leaves = key_at(q1 - 1);
-        const int back = key_at(q0 - 1 - (int64_t)lane * a.piece), ahead = key_at(q1 + (int64_t)lane * a.piece);
-        const unsigned b = __ballot_sync(kFull, back != enters), f = __ballot_sync(kFull, ahead != leaves);
-        int64_t begin = p - (b ? __ffs(b) - 1 : 32), end = p + (f ? __ffs(f) - 1 : 32);
-        if (!b) begin = first_at(0, begin, enters, [&](int64_t q) { return a.keys[(q + 1) * a.piece - 1]; });
-        if (leaves < 0) end = p;   // the last piece, cut short
-        else if (!f) end = first_at(end + 1, a.pieces, leaves + 1, [&](int64_t q) { return a.keys[q * a.piece]; }) - 1;
-        const int64_t stop = max(q0, min(q1, a.n));
-        int64_t valid = stop;
-        if (key_at(stop - 1) >= a.vocab) valid = first_at(q0, stop, a.vocab, [&](int64_t i) { return a.keys[i]; });
-        if (lane == 0) {
-            begin_of[g] = begin;
-            end_of[g] = end;
-            valid_of[g] = (int)(valid - q0);
-        }
-    }
     __syncthreads();
     float acc[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) acc[j] = 0.f;
     const bool active = c < a.width;
-    const int m = active ? valid_of[y] : 0;
+    int m = active ? count : 0;   // tokens outside the table sort last: without them
+    if (m > 0 && keys[m] >= a.vocab) {
+        int lo = 0;   // the first of them lies in [lo, m]
+        while (lo < m) {
+            const int mid = (lo + m) / 2;
+            if (keys[mid + 1] < a.vocab) lo = mid + 1;
+            else m = mid;
+        }
+    }
     uint4 *mine = smem + threadIdx.x;
     const T *column = dout + c;
     int slot = 0;
@@ -413,6 +401,22 @@ __global__ void __launch_bounds__(kSumThreads, kSumCtas) embed_sum_kernel(const 
     };
 #pragma unroll
     for (int k = 0; k < kSumStages - 1; ++k) issue(k * kSumStage);
+    const int lane = threadIdx.x & 31;
+    // while the first rows are on their way, a warp per piece finds where the runs at its ends lie
+    for (int g = threadIdx.x / 32; g < ty; g += kSumThreads / 32) {
+        const int64_t p = piece0 + g, q0 = p * a.piece, q1 = q0 + a.piece;
+        const int enters = key_at(q0), leaves = key_at(q1 - 1);
+        const int back = key_at(q0 - 1 - (int64_t)lane * a.piece), ahead = key_at(q1 + (int64_t)lane * a.piece);
+        const unsigned b = __ballot_sync(kFull, back != enters), f = __ballot_sync(kFull, ahead != leaves);
+        int64_t begin = p - (b ? __ffs(b) - 1 : 32), end = p + (f ? __ffs(f) - 1 : 32);
+        if (!b) begin = first_at(0, begin, enters, [&](int64_t q) { return a.keys[(q + 1) * a.piece - 1]; });
+        if (leaves < 0) end = p;   // the last piece, cut short
+        else if (!f) end = first_at(end + 1, a.pieces, leaves + 1, [&](int64_t q) { return a.keys[q * a.piece]; }) - 1;
+        if (lane == 0) {
+            begin_of[g] = begin;
+            end_of[g] = end;
+        }
+    }
     bool whole = keys[1] != keys[0];   // the run began here
     for (int r = 0; r < m; r += kSumStage) {
         issue(r + (kSumStages - 1) * kSumStage);   // into the slots read in the round before

@@ -19,9 +19,9 @@ namespace mbscan {
 namespace {
 
 constexpr int kWarpVocab = 1024, kSms = 152;
-// Warps of a CTA, rows of a warp. 65536 x 256 bf16: 2 and 2 14.3 us, 4 and 2 14.7, 8 and 2 15.7, 2 and 4 14.7, 4 and 4 15.1;
-// warps that stay and fetch rows ahead 19.
-constexpr int kWarpRows = 2, kRows = 2;
+// Warps of a CTA. 65536 x 256 bf16, eight lanes to a row: 1, 2, 4, 8 11.5, 11.4, 11.5, 12.1 us; a whole warp to a row, two
+// rows side by side 14.3; warps that stay and fetch rows ahead 19.
+constexpr int kWarpRows = 2;
 // Threads of a long row, 16-byte groups loaded at once by each. 1003 x 32001 fp32: 512 and 8 43.3 us, 4 51.1, 16 51.2;
 // 1024 and 4 47.3, 256 and 8 51.5.
 constexpr int kRowThreads = 512, kAhead = 8;
@@ -73,85 +73,60 @@ template <typename T> __device__ __forceinline__ uint4 masked() {
     return make_uint4(w, w, w, w);
 }
 
-// Maximum over a warp; a NaN is passed over.
-__device__ __forceinline__ float warp_max(float v) {
-    float m;
-    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
-    return m;
-}
-
-// Rows of whole 16-byte groups, G per lane (lane l has groups l, l + 32, ...); a warp takes R rows at a time, side by
-// side, for the loads and the chains of shuffles.
-template <typename T, int G, int R>
+// Rows of whole 16-byte groups: L lanes to a row, 32 / L rows to a warp, so that what a row needs once (its target, the
+// steps of its sums, the logarithm) is done for several at a time; G groups per lane (lane l of them: l, l + L, ...).
+template <typename T, int L, int G>
 __global__ void __launch_bounds__(32 * kWarpRows) loss_groups_kernel(const T *logits, T *dlogits, const LossArgs a) {
     constexpr int V = kVec<T>, P = kPairs<T>;
     pdl_wait();
-    const int lane = threadIdx.x & 31, groups = a.vocab / V;
-    const int64_t row0 = ((int64_t)blockIdx.x * kWarpRows + threadIdx.x / 32) * R;
-    if (row0 >= a.n) return;
-    uint4 raw[R][G];
-    int y[R];   // -1: the row counts for nothing, whatever its logits hold
-    float w[R], at[R];
+    const int lane = threadIdx.x % L, groups = a.vocab / V;
+    const int64_t row = ((int64_t)blockIdx.x * (32 * kWarpRows) + threadIdx.x) / L;
+    const bool in = row < a.n;
+    const int64_t base = row * a.vocab;
+    uint4 raw[G];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int64_t row = min(row0 + r, a.n - 1);   // beyond the last: that one again, not stored
-        const T *l = logits + row * a.vocab;
+    for (int g = 0; g < G; ++g)
+        raw[g] = in && g * L + lane < groups ? ld16(logits + base + (g * L + lane) * V) : masked<T>();
+    float w = 0.f, at = 0.f;
+    const int y = in ? target_of(a, row, w) : -1;   // -1: the row counts for nothing, whatever its logits hold
+    if (y >= 0) at = to_f32(logits[base + y]);
+    float2 x[G][P];
+    float m = -INFINITY;
 #pragma unroll
-        for (int g = 0; g < G; ++g) raw[r][g] = g * 32 + lane < groups ? ld16(l + (g * 32 + lane) * V) : masked<T>();
-        y[r] = target_of(a, row, w[r]);
+    for (int g = 0; g < G; ++g) {
+        to_pairs<T>(raw[g], x[g]);
+#pragma unroll
+        for (int j = 0; j < P; ++j) m = fmaxf(m, fmaxf(x[g][j].x, x[g][j].y));
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r) at[r] = to_f32(logits[min(row0 + r, a.n - 1) * a.vocab + max(y[r], 0)]);
-    float2 x[R][G][P];
-    float m[R], s[R];
+    for (int o = L / 2; o > 0; o /= 2) m = fmaxf(m, __shfl_xor_sync(kFull, m, o));
+    float2 sum = splat(0.f);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        m[r] = -INFINITY;
+    for (int g = 0; g < G; ++g)
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            to_pairs<T>(raw[r][g], x[r][g]);
-#pragma unroll
-            for (int j = 0; j < P; ++j) m[r] = fmaxf(m[r], fmaxf(x[r][g][j].x, x[r][g][j].y));
+        for (int j = 0; j < P; ++j) {
+            x[g][j] = exp2_of(x[g][j], splat(-m));
+            sum = add2(sum, x[g][j]);
         }
+    float s = sum.x + sum.y;
+#pragma unroll
+    for (int o = L / 2; o > 0; o /= 2) s += __shfl_xor_sync(kFull, s, o);
+    if (!in) return;
+    const float c = w * a.scale, k = __fdividef(c, s);
+    if (lane == 0) a.loss[row] = y >= 0 ? w * ((m - at) + logf(s)) : 0.f;
+    if (!dlogits) return;
+    T *d = dlogits + base;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        if (g * L + lane >= groups) break;
+#pragma unroll
+        for (int j = 0; j < P; ++j) x[g][j] = mul2(x[g][j], splat(k));
+        uint4 q = from_pairs<T>(x[g]);
+        if (y < 0) q = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4 *>(d + (g * L + lane) * V) = q;
     }
-#pragma unroll
-    for (int r = 0; r < R; ++r) m[r] = warp_max(m[r]);
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        float2 sum = splat(0.f);
-#pragma unroll
-        for (int g = 0; g < G; ++g)
-#pragma unroll
-            for (int j = 0; j < P; ++j) {
-                x[r][g][j] = exp2_of(x[r][g][j], splat(-m[r]));
-                sum = add2(sum, x[r][g][j]);
-            }
-        s[r] = sum.x + sum.y;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o /= 2)
-#pragma unroll
-        for (int r = 0; r < R; ++r) s[r] += __shfl_xor_sync(kFull, s[r], o);
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        if (row0 + r >= a.n) break;
-        const bool counts = y[r] >= 0;
-        const float c = w[r] * a.scale, k = __fdividef(c, s[r]);
-        if (lane == 0) a.loss[row0 + r] = counts ? w[r] * ((m[r] - at[r]) + logf(s[r])) : 0.f;
-        if (!dlogits) continue;
-        T *d = dlogits + (row0 + r) * a.vocab;
-        const T hot = from_f32<T>(fmaf(exp_of(at[r] - m[r]), k, -c));
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            if (g * 32 + lane >= groups) break;
-#pragma unroll
-            for (int j = 0; j < P; ++j) x[r][g][j] = mul2(x[r][g][j], splat(k));
-            uint4 q = from_pairs<T>(x[r][g]);
-            if (!counts) q = make_uint4(0, 0, 0, 0);
-            *reinterpret_cast<uint4 *>(d + (g * 32 + lane) * V) = q;
-        }
-        if (counts && y[r] / V % 32 == lane) d[y[r]] = hot;   // over what this lane has just stored
-    }
+    // over what this lane has just stored
+    if (y >= 0 && y / V % L == lane) d[y] = from_f32<T>(fmaf(exp_of(at - m), k, -c));
 }
 
 // Rows that are no whole groups. N logits per lane; lane l has l, l + 32, ...
@@ -344,16 +319,17 @@ cudaError_t loss(const LossArgs &a, const void *logits, void *dlogits, cudaStrea
                             : loss_row_kernel<T, 8>,
                    a.n * c, kRowThreads);
     }
-    const auto warps = [&](auto kernel, int rows) {
+    const auto warps = [&](auto kernel, int rows) {   // of so many rows each
         return run(kernel, (a.n + kWarpRows * rows - 1) / (kWarpRows * rows), 32 * kWarpRows);
     };
     if (a.vocab % kVec<T> != 0)
         return warps(a.vocab <= 256 ? loss_warp_kernel<T, 8> : loss_warp_kernel<T, kWarpVocab / 32>, 1);
-    constexpr int kMost = kWarpVocab / 32 / kVec<T>;   // groups of a lane: 4 (bf16), 8 (fp32)
-    const int groups = (a.vocab / kVec<T> + 31) / 32;
-    if (groups <= kMost / 4) return warps(loss_groups_kernel<T, kMost / 4, kRows>, kRows);
-    if (groups <= kMost / 2) return warps(loss_groups_kernel<T, kMost / 2, kRows>, kRows);
-    return warps(loss_groups_kernel<T, kMost, 1>, 1);
+    // four groups a lane, as many lanes as that takes (fp32 above 512: eight)
+    const int groups = a.vocab / kVec<T>;
+    if (groups <= 32) return warps(loss_groups_kernel<T, 8, 4>, 4);
+    if (groups <= 64) return warps(loss_groups_kernel<T, 16, 4>, 2);
+    if (groups <= 128) return warps(loss_groups_kernel<T, 32, 4>, 1);
+    return warps(loss_groups_kernel<T, 32, kWarpVocab / 32 / kVec<T>>, 1);
 }
 
 }  // namespace
