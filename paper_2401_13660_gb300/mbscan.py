@@ -7,10 +7,11 @@ every call where that module is missing or does not load.
 
 Each function has the name of the C entry point it calls (include/mbscan.h)
 and takes torch CUDA tensors in place of device pointers. Every step of the
-layer core runs in the library's kernels; this module only checks tensor
-shapes/dtypes/devices, fills the C argument struct and forwards the call on
-the current torch CUDA stream (or the stream given). There is no fallback: if
-the library cannot be loaded, importing the functions raises.
+layer core, and of what a training step runs around it, runs in the library's
+kernels; this module only checks tensor shapes/dtypes/devices, fills the C
+argument struct and forwards the call on the current torch CUDA stream (or the
+stream given). There is no fallback: if the library cannot be loaded, importing
+the functions raises.
 """
 from __future__ import annotations
 
@@ -595,6 +596,8 @@ def _conv1d_args(x, w, bias, state) -> mb_conv1d_args:
     _need(w, "w", torch.float32, (width, 4), dev)
     _need(bias, "bias", torch.float32, (width,), dev)
     _need(state, "state", x.dtype, (batch, 3, width), dev)
+    if S > 0x7fffffff:
+        raise ValueError(f"x: rows {S} elements apart, at most 2^31 - 1")
     a = mb_conv1d_args()
     a.batch, a.seqlen, a.width, a.dtype = batch, L, width, _DTYPES[x.dtype]
     a.x_stride = 0 if S == width else S
