@@ -142,6 +142,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) norm_kernel(const __grid
         if (e.flags & kInBf16) sum_range<__nv_bfloat16>(e, lo, hi, q);
         else sum_range<float>(e, lo, hi, q);
     });
+    pdl_trigger();   // clipping may set up
     const int lane = threadIdx.x & 31;
     const double mine = q.warp_total();
     if (lane == 0) red[threadIdx.x / 32] = mine;

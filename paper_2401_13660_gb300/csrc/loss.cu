@@ -22,9 +22,11 @@ constexpr int kWarpVocab = 1024, kSms = 152;
 // Warps of a CTA. 65536 x 256 bf16, eight lanes to a row: 1, 2, 4, 8 11.5, 11.4, 11.5, 12.1 us; a whole warp to a row, two
 // rows side by side 14.3; warps that stay and fetch rows ahead 19.
 constexpr int kWarpRows = 2;
-// Threads of a long row, 16-byte groups loaded at once by each. 1003 x 32001 fp32: 512 and 8 43.3 us, 4 51.1, 16 51.2;
-// 1024 and 4 47.3, 256 and 8 51.5.
-constexpr int kRowThreads = 512, kAhead = 8;
+// Threads of a row that is read twice, and the 16-byte groups that each loads at once: 32 elements, and two CTAs per SM
+// (64 registers). 1003 x 32001 fp32 with 512 threads and 16, 32, 64 elements 51, 43, 51 us, with 256 or 1024 threads 47 to
+// 55. Rows that are read once keep 8 groups for each of 128 or 256 threads: 1000 x 16000 bf16 12.5 us, read twice 19.
+constexpr int kRowThreads = 512, kOnceGroups = 8;
+template <typename T, bool kOnce> constexpr int kAhead = kOnce ? kOnceGroups : 32 / kVec<T>;
 
 struct LossArgs {
     const void *targets;
@@ -199,12 +201,13 @@ struct Running {
 };
 
 // A row per cluster of C CTAs: each takes a contiguous part of the row's whole 16-byte groups, the first and the last
-// also the elements before and behind them (rows of odd length begin at any element).
-template <typename T, int C>
-__global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kRowThreads) loss_row_kernel(const T *logits, T *dlogits,
-                                                                                       const LossArgs a) {
+// also the elements before and behind them (rows of odd length begin at any element). With kOnce a thread's groups, at
+// most kOnceGroups, stay in its registers for the gradient.
+template <typename T, int kThreads, int C, bool kOnce>
+__global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kThreads, kOnce ? 1 : 2)
+    loss_row_kernel(const T *logits, T *dlogits, const LossArgs a) {
     constexpr int V = kVec<T>, P = kPairs<T>;
-    __shared__ float sm[kRowThreads / 32], ss[kRowThreads / 32], mine[2];
+    __shared__ float sm[kThreads / 32], ss[kThreads / 32], mine[2];
     pdl_wait();
     const int tid = threadIdx.x, part = blockIdx.x % C;
     const int64_t row = blockIdx.x / C;
@@ -223,7 +226,7 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kRowThreads) loss_ro
         if (tid == 0 && part == 0) a.loss[row] = 0.f;
         if (!d) return;
         if (odd >= 0) d[odd] = from_f32<T>(0.f);
-        for (int g = g0 + tid; g < g1; g += kRowThreads)
+        for (int g = g0 + tid; g < g1; g += kThreads)
             *reinterpret_cast<uint4 *>(d + head + (int64_t)g * V) = make_uint4(0, 0, 0, 0);
         return;
     }
@@ -234,14 +237,14 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kRowThreads) loss_ro
         const float2 x[1] = {make_float2(own, -INFINITY)};
         run.add(x);
     }
-    for (int g = g0 + tid; g < g1; g += kAhead * kRowThreads) {
-        uint4 raw[kAhead];
-        float2 x[kAhead * P];
+    uint4 raw[kAhead<T, kOnce>];
+    for (int g = g0 + tid; g < g1; g += kAhead<T, kOnce> * kThreads) {
+        float2 x[kAhead<T, kOnce> * P];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k)
-            raw[k] = g + k * kRowThreads < g1 ? ld16(l + head + (int64_t)(g + k * kRowThreads) * V) : masked<T>();
+        for (int k = 0; k < kAhead<T, kOnce>; ++k)
+            raw[k] = g + k * kThreads < g1 ? ld16(l + head + (int64_t)(g + k * kThreads) * V) : masked<T>();
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
+        for (int k = 0; k < kAhead<T, kOnce>; ++k) {
             float2 v[P];
             to_pairs<T>(raw[k], v);
 #pragma unroll
@@ -262,7 +265,7 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kRowThreads) loss_ro
     run.m = sm[0];
     run.s = ss[0];
 #pragma unroll
-    for (int i = 1; i < kRowThreads / 32; ++i) run.join(sm[i], ss[i]);
+    for (int i = 1; i < kThreads / 32; ++i) run.join(sm[i], ss[i]);
     if constexpr (C > 1) {
         if (tid == 0) {
             mine[0] = run.m;
@@ -281,15 +284,14 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kRowThreads) loss_ro
     if (d) {
         const T hot = from_f32<T>(fmaf(exp_of(at - m), k, -c));
         if (odd >= 0) d[odd] = odd == y ? hot : from_f32<T>(exp_of(own - m) * k);
-        for (int g = g0 + tid; g < g1; g += kAhead * kRowThreads) {
-            uint4 raw[kAhead];
+        for (int g = g0 + tid; g < g1; g += kAhead<T, kOnce> * kThreads) {
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q)
-                if (g + q * kRowThreads < g1) raw[q] = ld16(l + head + (int64_t)(g + q * kRowThreads) * V);
+            for (int q = 0; q < kAhead<T, kOnce>; ++q)
+                if (!kOnce && g + q * kThreads < g1) raw[q] = ld16(l + head + (int64_t)(g + q * kThreads) * V);
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q) {
-                if (g + q * kRowThreads >= g1) break;
-                const int v0 = head + (g + q * kRowThreads) * V;
+            for (int q = 0; q < kAhead<T, kOnce>; ++q) {
+                if (g + q * kThreads >= g1) break;
+                const int v0 = head + (g + q * kThreads) * V;
                 float2 v[P];
                 to_pairs<T>(raw[q], v);
 #pragma unroll
@@ -310,13 +312,17 @@ cudaError_t loss(const LossArgs &a, const void *logits, void *dlogits, cudaStrea
         return launch_pdl(true, kernel, dim3((unsigned)ctas), dim3(threads), 0, st, l, d, a);
     };
     if (a.vocab > kWarpVocab) {
-        // CTAs of a row: as many as there are SMs for, each with two groups per thread at least
+        // Rows of up to kOnceGroups groups for each of 128 (256) threads are read once. Longer ones take 512, and where there
+        // are SMs for it several CTAs, each with two groups per thread at least.
+        const int groups = a.vocab / kVec<T>;
+        if (groups <= 128 * kOnceGroups) return run(loss_row_kernel<T, 128, 1, true>, a.n, 128);
+        if (groups <= 256 * kOnceGroups) return run(loss_row_kernel<T, 256, 1, true>, a.n, 256);
         int c = 1;
-        while (c < 8 && a.n * c * 2 <= kSms && a.vocab / kVec<T> >= 4 * c * kRowThreads) c *= 2;
-        return run(c == 1   ? loss_row_kernel<T, 1>
-                   : c == 2 ? loss_row_kernel<T, 2>
-                   : c == 4 ? loss_row_kernel<T, 4>
-                            : loss_row_kernel<T, 8>,
+        while (c < 8 && a.n * c * 2 <= kSms && groups >= 4 * c * kRowThreads) c *= 2;
+        return run(c == 1   ? loss_row_kernel<T, kRowThreads, 1, false>
+                   : c == 2 ? loss_row_kernel<T, kRowThreads, 2, false>
+                   : c == 4 ? loss_row_kernel<T, kRowThreads, 4, false>
+                            : loss_row_kernel<T, kRowThreads, 8, false>,
                    a.n * c, kRowThreads);
     }
     const auto warps = [&](auto kernel, int rows) {   // of so many rows each
