@@ -332,7 +332,6 @@ __global__ void __launch_bounds__(kBwdThreads, kBwdCtas<T>)
     // Sum over the CTA's chunks, in their order. Rows of tx + 4 floats let the sums read channels (8 or 4 rows apart)
     // without bank conflicts; narrow ones (narrow inputs) stay tight, so that ty * 5 * V of them fit in the ring.
     copy_wait<0>();
-    pdl_trigger();     // the sums' CTAs may set up
     __syncthreads();   // the ring is free
     float *red = reinterpret_cast<float *>(smem);   // [ty][5][V][pitch]
     const int pitch = s.tx >= 8 ? s.tx + 4 : s.tx;
@@ -371,7 +370,6 @@ __global__ void __launch_bounds__(kSumCols *kSumRows) conv_sum_kernel(const floa
     const int64_t c = (int64_t)blockIdx.x * kSumCols + col;   // k * width + channel
     float sum = 0.f;
     if (c < 5 * width)
-#pragma unroll 4
         for (int64_t i = row; i < parts; i += kSumRows) sum += part[i * 5 * width + c];
     red[row][col] = sum;
     __syncthreads();

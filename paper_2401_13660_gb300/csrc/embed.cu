@@ -299,10 +299,11 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
 
 // ---- sums of the sorted rows
 // A thread's rows come through a ring of asynchronous copies of its own, kSumStages stages of four rows. 65536 x 1024
-// fp32, 256 threads with 2 stages and 4 CTAs per SM 59.6 us in all, 3 and 3 60.3; 128 threads with 2 and 8 59.8, 4 and 5
-// 61.1 (and 8200 x 1792 of 32001 tokens 52.9, 52.9; 58.9, 59.1); eight rows at a time in registers 64.
-constexpr int kSumThreads = 256, kSumCtas = 4, kSumStage = 4, kSumStages = 2;
-constexpr int kMostTy = kSumThreads / 4, kMostRows = 1024, kLongest = 192;   // pieces, positions of a CTA; positions of a piece
+// fp32 in all, pieces for so many CTAs of 256 threads per SM: with 3 stages 2 57.3 us, 3 60.4; with 2 stages 3 58.3, 4
+// 59.3, 8 67.7; with 4 stages 2 58.0; 128 threads 59.8 to 61; eight rows at a time in registers 64.
+constexpr int kSumThreads = 256, kSumCtas = 3, kSumStage = 4, kSumStages = 3;
+constexpr int kPieceCtas = 2;   // per SM; the third's room is for CTAs that clear
+constexpr int kMostTy = kSumThreads / 4, kMostRows = 1024, kLongest = 320;   // pieces, positions of a CTA; positions of a piece
 
 struct SumArgs {
     const int *keys, *perm;   // sorted
@@ -496,8 +497,8 @@ cudaError_t lookup(const LookupArgs &a, const void *table, void *out, cudaStream
 
 int64_t round256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// How the sums are cut: into as many equal pieces as CTAs are resident, of 16 positions at least (few tokens: more CTAs)
-// and kLongest at most; no more than kMostRows positions in a CTA.
+// How the sums are cut: into equal pieces for kPieceCtas CTAs per SM, of 16 positions at least (few tokens: more CTAs) and
+// kLongest at most; no more than kMostRows positions in a CTA.
 struct Pieces {
     int piece, tx;
     int64_t pieces, tiles;
@@ -506,7 +507,7 @@ Pieces cut_rows(int64_t n, int64_t width, int vec) {
     Pieces c{};
     c.tx = threads_for(width / vec, kSumThreads);
     c.tiles = (width / vec + c.tx - 1) / c.tx;
-    const int64_t ty = kSumThreads / c.tx, slots = std::max<int64_t>(kSms * kSumCtas / c.tiles, 1) * ty;
+    const int64_t ty = kSumThreads / c.tx, slots = std::max<int64_t>(kSms * kPieceCtas / c.tiles, 1) * ty;
     const int64_t piece = (n + slots - 1) / slots;
     c.piece = (int)std::min<int64_t>(std::max<int64_t>(piece, 16), std::min<int64_t>(kLongest, kMostRows / ty));
     c.pieces = (n + c.piece - 1) / c.piece;

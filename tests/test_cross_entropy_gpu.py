@@ -180,3 +180,11 @@ def test_refusals():
             mb.mb_cross_entropy(*a, **kw)
     with pytest.raises(mb.MbError):   # losses inside the logits
         mb.mb_cross_entropy(logits, tgt, logits.view(-1)[:6])
+
+
+@pytest.mark.parametrize("V", [4096, 4097, 8191, 8192, 8193, 16384, 16385])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [3, 70, 310])
+def test_sizes_where_rows_change_hands(n, V, dtype):
+    # rows kept in the registers of 128 or 256 threads, read twice, by one CTA or several
+    test_loss_and_gradient((n, V, dtype, "i64"), True)
