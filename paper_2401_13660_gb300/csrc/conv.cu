@@ -30,7 +30,7 @@ constexpr int kStage = 4;   // rows per stage of the ring (the taps' registers g
 template <typename T> constexpr int kStages = sizeof(T) == 2 ? 4 : 3;
 template <typename T> constexpr int kGroup = 16 / (int)sizeof(T);   // channels of a thread
 constexpr int kFwdThreads = 256, kFwdCtas = 2, kBwdThreads = 128;
-template <typename T> constexpr int kBwdCtas = sizeof(T) == 2 ? 2 : 3;   // by their registers (236 and 144)
+template <typename T> constexpr int kBwdCtas = sizeof(T) == 2 ? 2 : 3;   // by their registers (234 and 144)
 // Steps of a chunk at most, where there are enough of them. 8 x 8192 x 2048 bf16, forward with 24, 32, 48, 64, 96:
 // 89, 85, 84, 85, 90 us; backward (sums to hand over) with 64, 128, 192, 256: 148, 139, 134, 129.
 constexpr int kFwdLongest = 48, kBwdLongest = 256;
@@ -141,7 +141,8 @@ __global__ void __launch_bounds__(kFwdThreads, kFwdCtas)
     const int64_t group = bx * s.tx + threadIdx.x % s.tx;
     const int64_t item = by * (kFwdThreads / s.tx) + threadIdx.x / s.tx;
     if (group >= s.groups || item >= s.items) return;
-    const int64_t b = item / s.chunks, chunk = item - b * s.chunks, d0 = group * V;
+    const int64_t b = (uint32_t)item / (uint32_t)s.chunks;   // at most 2^28 items
+    const int64_t chunk = item - b * s.chunks, d0 = group * V;
     const int64_t t0 = chunk * s.rows;
     const int n = (int)min((int64_t)s.rows, s.L - t0);
     uint4 *mine = smem + threadIdx.x;
@@ -220,7 +221,8 @@ __global__ void __launch_bounds__(kBwdThreads, kBwdCtas<T>)
 #pragma unroll
         for (int i = 0; i < P; ++i) acc[k][i] = splat(0.f);
     if (group < s.groups && item < s.items) {
-        const int64_t b = item / s.chunks, chunk = item - b * s.chunks, d0 = group * V;
+        const int64_t b = (uint32_t)item / (uint32_t)s.chunks;   // at most 2^28 items
+        const int64_t chunk = item - b * s.chunks, d0 = group * V;
         const int64_t t0 = chunk * s.rows;
         const int n = (int)min((int64_t)s.rows, s.L - t0);        // steps of the chunk
         const int m = (int)min((int64_t)s.rows + 3, s.L - t0);    // and of the three after it
