@@ -14,6 +14,7 @@
 #include <algorithm>
 
 #include "cluster.cuh"
+#include "runs.h"
 #include "tokens.cuh"
 #include "vec.cuh"
 
@@ -331,21 +332,16 @@ template <int V> __device__ __forceinline__ void put_row(const SumArgs &a, int k
     stf(row, v);
 }
 
-// The first q of [lo, hi] for which `from(q)` (a sorted key) is at least k, by a whole warp.
-template <typename F> __device__ __forceinline__ int64_t first_at(int64_t lo, int64_t hi, int k, F from) {
-    while (lo < hi) {
-        const int64_t step = (hi - lo + 31) / 32, at = lo + step * (threadIdx.x & 31);
-        const int below = __popc(__ballot_sync(kFull, at < hi && from(at) < k));   // a prefix of the lanes
-        if (below == 0) break;
-        hi = min(hi, lo + step * below);
-        lo = lo + step * (below - 1) + 1;
+// The lanes of this warp for which f holds.
+struct Votes {
+    template <typename F> __device__ __forceinline__ unsigned operator()(const F &f) const {
+        return __ballot_sync(kFull, f((int)(threadIdx.x & 31)));
     }
-    return lo;
-}
+};
 
 // Clear the row of a token that does not occur (a warp).
 __device__ __forceinline__ void clear_row(const SumArgs &a, int64_t v) {
-    const int64_t at = first_at(0, a.n, (int)v, [&](int64_t i) { return a.keys[i]; });
+    const int64_t at = first_at(Votes{}, 0, a.n, (int)v, [&](int64_t i) { return a.keys[i]; });
     if (at < a.n && a.keys[at] == v) return;
     const float zero[4] = {0.f, 0.f, 0.f, 0.f};
     for (int64_t c = (threadIdx.x & 31) * 4; c < a.width; c += 128) stf(a.dtable + v * a.width + c, zero);
@@ -405,17 +401,10 @@ __global__ void __launch_bounds__(kSumThreads, kSumCtas) embed_sum_kernel(const 
     const int lane = threadIdx.x & 31;
     // while the first rows are on their way, a warp per piece finds where the runs at its ends lie
     for (int g = threadIdx.x / 32; g < ty; g += kSumThreads / 32) {
-        const int64_t p = piece0 + g, q0 = p * a.piece, q1 = q0 + a.piece;
-        const int enters = key_at(q0), leaves = key_at(q1 - 1);
-        const int back = key_at(q0 - 1 - (int64_t)lane * a.piece), ahead = key_at(q1 + (int64_t)lane * a.piece);
-        const unsigned b = __ballot_sync(kFull, back != enters), f = __ballot_sync(kFull, ahead != leaves);
-        int64_t begin = p - (b ? __ffs(b) - 1 : 32), end = p + (f ? __ffs(f) - 1 : 32);
-        if (!b) begin = first_at(0, begin, enters, [&](int64_t q) { return a.keys[(q + 1) * a.piece - 1]; });
-        if (leaves < 0) end = p;   // the last piece, cut short
-        else if (!f) end = first_at(end + 1, a.pieces, leaves + 1, [&](int64_t q) { return a.keys[q * a.piece]; }) - 1;
+        const RunEnds r = run_ends(Votes{}, [&](int64_t i) { return a.keys[i]; }, a.n, a.piece, a.pieces, piece0 + g);
         if (lane == 0) {
-            begin_of[g] = begin;
-            end_of[g] = end;
+            begin_of[g] = r.begin;
+            end_of[g] = r.end;
         }
     }
     bool whole = keys[1] != keys[0];   // the run began here
