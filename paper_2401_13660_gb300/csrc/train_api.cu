@@ -178,6 +178,7 @@ mb_status mb_embed(const void *tokens, int32_t token_type, const void *table, in
 
 size_t mb_embed_backward_workspace_size(int64_t n, int64_t vocab, int64_t width) {
     if (check_embed(n, vocab, width) != MB_OK) return 0;
+    if (n == 0 || vocab == 0 || width == 0) return mbscan::kStatusBytes;   // nothing to sort or add
     return mbscan::kStatusBytes + mbscan::embed_backward_scratch(n, width);
 }
 
