@@ -181,7 +181,10 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
-def _stream(stream):
+def _stream(stream, dev):
+    """The stream of a call whose tensors are on `dev`. Every launch asks here: host memory's addresses go no further."""
+    if dev.type != "cuda":
+        raise ValueError(f"tensors on {dev}, expected a CUDA device")
     if stream is None:
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
@@ -307,7 +310,7 @@ def mb_scan_prefill(x, dt, B, C, A, y, *, z=None, D=None, dt_bias=None, h0=None,
     if ws is None:
         ws = new_workspace(a, x.device)
     rc = load_library().mb_scan_prefill(ctypes.byref(a), _ptr(h_last), _ptr(ws), ws.numel(),
-                                        _stream(stream))
+                                        _stream(stream, x.device))
     _check(rc, "mb_scan_prefill")
     return y, h_last
 
@@ -325,7 +328,7 @@ def mb_scan_verify(x, dt, B, C, A, y, h_all, *, z=None, D=None, dt_bias=None, h0
     if ws is None:
         ws = new_workspace(a, x.device)
     rc = load_library().mb_scan_verify(ctypes.byref(a), _ptr(h_all), _ptr(ws), ws.numel(),
-                                       _stream(stream))
+                                       _stream(stream, x.device))
     _check(rc, "mb_scan_verify")
     return y, h_all
 
@@ -352,7 +355,7 @@ def mb_scan_verify_resume(x, dt, B, C, A, y, h_all, h_all_prev, accept, *, z=Non
     if ws is None:
         ws = new_workspace(a, x.device)
     rc = load_library().mb_scan_verify_resume(ctypes.byref(a), _ptr(h_all_prev), _ptr(accept), h_all_prev.shape[1],
-                                              _ptr(h_all), _ptr(ws), ws.numel(), _stream(stream))
+                                              _ptr(h_all), _ptr(ws), ws.numel(), _stream(stream, x.device))
     _check(rc, "mb_scan_verify_resume")
     return y, h_all
 
@@ -370,7 +373,7 @@ def mb_rollback(h0, h_all, accept, h_out, *, ws=None, stream=None):
     _need(h_out, "h_out", torch.float32, (batch, Dn, N), h_all.device)
     _need(accept, "accept", torch.int32, (batch,), h_all.device)
     rc = load_library().mb_rollback(_ptr(h0), _ptr(h_all), _ptr(accept), _ptr(h_out), batch, k,
-                                    Dn, N, _ptr(ws), _stream(stream))
+                                    Dn, N, _ptr(ws), _stream(stream, h_all.device))
     _check(rc, "mb_rollback")
     return h_out
 
@@ -389,7 +392,7 @@ def mb_step(x, dt, B, C, A, y, state, *, z=None, D=None, dt_bias=None, ws=None, 
     _need(state, "state", torch.float32, (a.batch, a.d_inner, a.d_state), x.device)
     _need(ws, "ws", torch.uint8, None, x.device)
     nbytes = 0 if ws is None else ws.numel()
-    rc = load_library().mb_step(ctypes.byref(a), _ptr(state), _ptr(ws), nbytes, _stream(stream))
+    rc = load_library().mb_step(ctypes.byref(a), _ptr(state), _ptr(ws), nbytes, _stream(stream, x.device))
     _check(rc, "mb_step")
     return y, state
 
@@ -414,7 +417,7 @@ def mb_scan_prefill_ckpt(x, dt, B, C, A, y, h_ckpt=None, *, z=None, D=None, dt_b
     if ws is None:
         ws = new_workspace(a, x.device)
     rc = load_library().mb_scan_prefill_ckpt(ctypes.byref(a), _ptr(h_last), _ptr(h_ckpt), _ptr(ws),
-                                             ws.numel(), _stream(stream))
+                                             ws.numel(), _stream(stream, x.device))
     _check(rc, "mb_scan_prefill_ckpt")
     return y, h_last, h_ckpt
 
@@ -454,7 +457,7 @@ def mb_scan_backward(x, dt, B, C, A, h_ckpt, dout, *, z=None, D=None, dt_bias=No
     if ws is None:
         ws = new_workspace(a, dev)
     rc = load_library().mb_scan_backward(ctypes.byref(a), _ptr(h_ckpt), _ptr(dout), _ptr(dh_last),
-                                         ctypes.byref(st), _ptr(ws), ws.numel(), _stream(stream))
+                                         ctypes.byref(st), _ptr(ws), ws.numel(), _stream(stream, dev))
     _check(rc, "mb_scan_backward")
     return g
 
@@ -476,7 +479,7 @@ def mb_rmsnorm(residual, w, out, *, add=None, eps=1e-5, stream=None):
     _need(out, "out", out.dtype, (batch, width), dev)
     _need(add, "add", out.dtype, (batch, width), dev)
     rc = load_library().mb_rmsnorm(_ptr(add), _ptr(residual), _ptr(w), float(eps), _ptr(out), batch, width,
-                                   _DTYPES[out.dtype], _stream(stream))
+                                   _DTYPES[out.dtype], _stream(stream, dev))
     _check(rc, "mb_rmsnorm")
     return out
 
@@ -500,7 +503,7 @@ def mb_conv1d_step(x, state, w, out, *, bias=None, stream=None):
     _need(bias, "bias", torch.float32, (width,), dev)
     _need(out, "out", x.dtype, (batch, width), dev)
     rc = load_library().mb_conv1d_step(_ptr(x), _ptr(state), _ptr(w), _ptr(bias), _ptr(out), batch, width,
-                                       _DTYPES[x.dtype], _stream(stream))
+                                       _DTYPES[x.dtype], _stream(stream, dev))
     _check(rc, "mb_conv1d_step")
     return out
 
@@ -533,7 +536,7 @@ def mb_conv_xproj(x, state, w, W, xc, out, ws, *, bias=None, stream=None):
     _need(out, "out", bf, (batch, n_out), dev)
     _need(ws, "ws", torch.uint8, None, dev)
     rc = load_library().mb_conv_xproj(_ptr(x), _ptr(state), _ptr(w), _ptr(bias), _ptr(W), _ptr(xc), _ptr(out),
-                                      batch, width, n_out, MB_BF16, _ptr(ws), ws.numel(), _stream(stream))
+                                      batch, width, n_out, MB_BF16, _ptr(ws), ws.numel(), _stream(stream, x.device))
     _check(rc, "mb_conv_xproj")
     return out
 
@@ -558,7 +561,7 @@ def mb_step_resume(x, dt, B, C, A, y, h_all, accept, state, *, z=None, D=None, d
     _need(state, "state", torch.float32, (a.batch, a.d_inner, a.d_state), x.device)
     nbytes = 0 if ws is None else ws.numel()
     rc = load_library().mb_step_resume(ctypes.byref(a), _ptr(h_all), _ptr(accept), h_all.shape[1],
-                                       _ptr(state), _ptr(ws), nbytes, _stream(stream))
+                                       _ptr(state), _ptr(ws), nbytes, _stream(stream, x.device))
     _check(rc, "mb_step_resume")
     return y, state
 
@@ -582,7 +585,7 @@ def mb_accept_topk(logits, drafted, beta, accept=None, stream=None):
         accept = torch.empty(streams, dtype=torch.int32, device=logits.device)
     _need(accept, "accept", torch.int32, (streams,), logits.device)
     rc = load_library().mb_accept_topk(_ptr(logits), _DTYPES[logits.dtype], _ptr(drafted), streams, k,
-                                       int(beta), _ptr(accept), _stream(stream))
+                                       int(beta), _ptr(accept), _stream(stream, logits.device))
     _check(rc, "mb_accept_topk")
     return accept
 
@@ -620,7 +623,7 @@ def mb_conv1d(x, w, out, *, bias=None, state=None, state_out=None, stream=None):
     a = _conv1d_args(x, w, bias, state)
     _need(out, "out", x.dtype, tuple(x.shape), x.device)
     _need(state_out, "state_out", x.dtype, (a.batch, 3, a.width), x.device)
-    rc = load_library().mb_conv1d(ctypes.byref(a), _ptr(out), _ptr(state_out), _stream(stream))
+    rc = load_library().mb_conv1d(ctypes.byref(a), _ptr(out), _ptr(state_out), _stream(stream, x.device))
     _check(rc, "mb_conv1d")
     return out
 
@@ -664,7 +667,7 @@ def mb_conv1d_backward(x, w, dout, *, bias=None, state=None, dstate_out=None, gr
         ws = torch.zeros(max(mb_conv1d_backward_workspace_size(batch, L, width), 256), dtype=torch.uint8, device=dev)
     _need(ws, "ws", torch.uint8, None, dev)
     rc = load_library().mb_conv1d_backward(ctypes.byref(a), _ptr(dout), _ptr(dstate_out), ctypes.byref(st), _ptr(ws),
-                                           ws.numel(), _stream(stream))
+                                           ws.numel(), _stream(stream, dev))
     _check(rc, "mb_conv1d_backward")
     return g
 
@@ -696,7 +699,7 @@ def mb_embed(tokens, table, out, *, scale=1.0, stream=None):
     _need(table, "table")
     _need(out, "out", None, (*tokens.shape, width), dev)
     rc = load_library().mb_embed(_ptr(tokens), tt, _ptr(table), _DTYPES[table.dtype], float(scale), _ptr(out),
-                                 _DTYPES[out.dtype], tokens.numel(), vocab, width, _stream(stream))
+                                 _DTYPES[out.dtype], tokens.numel(), vocab, width, _stream(stream, dev))
     _check(rc, "mb_embed")
     return out
 
@@ -729,7 +732,7 @@ def mb_embed_backward(tokens, dout, dtable, *, scale=1.0, accumulate=False, ws=N
     _need(ws, "ws", torch.uint8, None, dev)
     rc = load_library().mb_embed_backward(_ptr(tokens), tt, _ptr(dout), _DTYPES[dout.dtype], float(scale),
                                           int(bool(accumulate)), _ptr(dtable), n, vocab, width, _ptr(ws), ws.numel(),
-                                          _stream(stream))
+                                          _stream(stream, dev))
     _check(rc, "mb_embed_backward")
     return dtable
 
@@ -757,7 +760,7 @@ def mb_cross_entropy(logits, targets, loss, dlogits=None, *, weight=None, scale=
     _need(dlogits, "dlogits", logits.dtype, tuple(logits.shape), dev)
     rc = load_library().mb_cross_entropy(_ptr(logits), _DTYPES[logits.dtype], _ptr(targets), tt, _ptr(weight),
                                          float(scale), _ptr(loss), _ptr(dlogits), targets.numel(), vocab,
-                                         _stream(stream))
+                                         _stream(stream, dev))
     _check(rc, "mb_cross_entropy")
     return loss, dlogits
 
@@ -809,7 +812,7 @@ def mb_grad_norm(tensors, norm=None, *, ws=None, stream=None):
     if ws is None:
         ws = torch.zeros(mb_grad_norm_workspace_size(), dtype=torch.uint8, device=dev)
     _need(ws, "ws", torch.uint8, None, dev)
-    rc = load_library().mb_grad_norm(lst.array, len(lst), _ptr(norm), _ptr(ws), ws.numel(), _stream(stream))
+    rc = load_library().mb_grad_norm(lst.array, len(lst), _ptr(norm), _ptr(ws), ws.numel(), _stream(stream, dev))
     _check(rc, "mb_grad_norm")
     return norm
 
@@ -834,7 +837,7 @@ def mb_grad_clip(tensors, norm, max_norm, *, out=None, stream=None):
             raise ValueError(f"tensor on {t.device}, expected {lst.tensors[0].device}")
     _need(norm, "norm", torch.float32, (1,))
     rc = load_library().mb_grad_clip(lst.array, None if o is None else o.array, len(lst), _ptr(norm), float(max_norm),
-                                     _stream(stream))
+                                     _stream(stream, norm.device))
     _check(rc, "mb_grad_clip")
     return tensors if out is None else out
 
@@ -844,12 +847,12 @@ def mb_selftest_timeout(ws, wait_cycles, stream=None):
     a barrier nothing arrives on and records MB_ERR_TIMEOUT in ws (read it with
     mb_check)."""
     _need(ws, "ws", torch.uint8)
-    rc = load_library().mb_selftest_timeout(_ptr(ws), ws.numel(), int(wait_cycles), _stream(stream))
+    rc = load_library().mb_selftest_timeout(_ptr(ws), ws.numel(), int(wait_cycles), _stream(stream, ws.device))
     _check(rc, "mb_selftest_timeout")
 
 
 def mb_check(ws, stream=None):
     """Read and clear the workspace status block: (status, detail)."""
     detail = ctypes.c_int64(-1)
-    rc = load_library().mb_check(_ptr(ws), _stream(stream), ctypes.byref(detail))
+    rc = load_library().mb_check(_ptr(ws), _stream(stream, ws.device), ctypes.byref(detail))
     return int(rc), int(detail.value)

@@ -4,6 +4,7 @@ import subprocess
 import sys
 
 import pytest
+import torch
 
 from paper_2401_13660_gb300 import mbscan as mb
 
@@ -24,3 +25,35 @@ def test_embed_backward_workspace_of_nothing(n, vocab, width):
     need, lib = int(r.stdout), mb.load_library()
     call = lambda wb: lib.mb_embed_backward(_at(0), 0, _at(1), 0, 1.0, 1, _at(2), n, vocab, width, _at(3), wb, None)
     assert call(need) == mb.MB_OK   # nothing to add, so nothing is launched
+
+
+def _cpu_calls():
+    t, u = torch.zeros, torch.uint8
+    x, w, tok = t(1, 2, 8), t(8, 4), t(2, dtype=u)
+    ws = t(1 << 16, dtype=u)
+    return dict(
+        conv1d=lambda **k: mb.mb_conv1d(x, w, t(1, 2, 8), **k),
+        conv1d_backward=lambda **k: mb.mb_conv1d_backward(x, w, t(1, 2, 8), **k),
+        conv1d_backward_ws=lambda **k: mb.mb_conv1d_backward(x, w, x, grads=dict(dx=t(1, 2, 8), dw=t(8, 4)), ws=ws, **k),
+        embed=lambda **k: mb.mb_embed(tok, t(4, 8), t(2, 8), **k),
+        embed_backward=lambda **k: mb.mb_embed_backward(tok, t(2, 8), t(4, 8), **k),
+        embed_backward_ws=lambda **k: mb.mb_embed_backward(tok, t(2, 8), t(4, 8), ws=ws, **k),
+        cross_entropy=lambda **k: mb.mb_cross_entropy(t(2, 4), tok, t(2), **k),
+        grad_norm=lambda **k: mb.mb_grad_norm([t(3)], **k),
+        grad_norm_list=lambda **k: mb.mb_grad_norm(mb.mb_tensor_list([t(3)]), t(1), ws=ws, **k),
+        grad_norm_empty=lambda **k: mb.mb_grad_norm([], t(1), **k),
+        grad_clip=lambda **k: mb.mb_grad_clip([t(3)], t(1), 0.5, **k),
+        grad_clip_out=lambda **k: mb.mb_grad_clip(mb.mb_tensor_list([t(3)]), t(1), 0.5, out=mb.mb_tensor_list([t(3)]), **k),
+        grad_clip_empty=lambda **k: mb.mb_grad_clip([], t(1), 0.5, **k),
+        rmsnorm=lambda **k: mb.mb_rmsnorm(t(1, 8), t(8), t(1, 8), **k),
+        conv1d_step=lambda **k: mb.mb_conv1d_step(t(1, 8), t(1, 3, 8), w, t(1, 8), **k),
+        prefill=lambda **k: mb.mb_scan_prefill(x, x, t(1, 2, 16), t(1, 2, 16), t(8, 16), t(1, 2, 8), **k),
+        check=lambda **k: mb.mb_check(ws, **k))
+
+
+@pytest.mark.parametrize("name", _cpu_calls())
+@pytest.mark.parametrize("stream", [None, 0])
+def test_host_tensors_are_refused(name, stream):
+    # they agree with each other in every way; no launch may see their addresses
+    with pytest.raises(ValueError, match="expected a CUDA device"):
+        _cpu_calls()[name](stream=stream)
