@@ -31,14 +31,19 @@ from .decoder import CONFIGS, STORED_KEYS, DecoderConfig, init_weights
 
 
 class Workspace:
-    """One device buffer for the calls of a model, which follow each other on one stream; grows as asked."""
+    """One device buffer for the calls of a model, which follow each other on one stream; grows as asked and keeps its
+    status block then, with what earlier calls have recorded there."""
+
+    STATUS = 256
 
     def __init__(self, device):
-        self.buffer = torch.zeros(256, dtype=torch.uint8, device=device)
+        self.buffer = torch.zeros(self.STATUS, dtype=torch.uint8, device=device)
 
     def get(self, nbytes: int) -> torch.Tensor:
         if self.buffer.numel() < nbytes:
+            status = self.buffer[:self.STATUS]
             self.buffer = torch.zeros(nbytes, dtype=torch.uint8, device=self.buffer.device)
+            self.buffer[:self.STATUS] = status
         return self.buffer
 
 
@@ -177,13 +182,15 @@ class Trainer:
         self.optimizer = torch.optim.AdamW(model.parameters, lr=lr, betas=(0.9, 0.95), weight_decay=0.0)
 
     def train_step(self, tokens, targets, counted: int | None = None):
-        """One step; returns the loss and the gradient norm before clipping (device tensors)."""
+        """One step; returns the loss and the gradient norm before clipping (device tensors). Waits for the gradients
+        and raises, with the model as it was, if a scan recorded a device-side error."""
         for g in self.grads.tensors:
             g.zero_()
         loss = self.model.loss(tokens, targets, counted)
         loss.backward()
         mb.mb_grad_norm(self.grads, self.norm, ws=self.norm_ws)
         mb.mb_grad_clip(self.grads, self.norm, self.max_norm)
+        self.model.check()
         self.optimizer.step()
         return loss.detach(), self.norm
 

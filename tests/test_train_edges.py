@@ -57,3 +57,13 @@ def test_host_tensors_are_refused(name, stream):
     # they agree with each other in every way; no launch may see their addresses
     with pytest.raises(ValueError, match="expected a CUDA device"):
         _cpu_calls()[name](stream=stream)
+
+
+def test_a_workspace_that_grows_keeps_its_status():
+    from paper_2401_13660_gb300.trainer import Workspace
+    ws = Workspace("cpu")
+    first = ws.get(300)
+    first[:] = torch.arange(300, dtype=torch.int32).to(torch.uint8)
+    assert ws.get(256) is first
+    grown = ws.get(5000)
+    assert grown is ws.buffer and grown.numel() >= 5000 and torch.equal(grown[:256], first[:256])
