@@ -183,7 +183,8 @@ class Trainer:
 
     def train_step(self, tokens, targets, counted: int | None = None):
         """One step; returns the loss and the gradient norm before clipping (device tensors). Waits for the gradients
-        and raises, with the model as it was, if a scan recorded a device-side error."""
+        and leaves the model as it was if their norm is not finite (one overflow would stay in the weights and moments
+        for good), or raises if a scan recorded a device-side error."""
         for g in self.grads.tensors:
             g.zero_()
         loss = self.model.loss(tokens, targets, counted)
@@ -191,7 +192,8 @@ class Trainer:
         mb.mb_grad_norm(self.grads, self.norm, ws=self.norm_ws)
         mb.mb_grad_clip(self.grads, self.norm, self.max_norm)
         self.model.check()
-        self.optimizer.step()
+        if bool(torch.isfinite(self.norm)):
+            self.optimizer.step()
         return loss.detach(), self.norm
 
 

@@ -42,3 +42,21 @@ def test_a_device_side_error_stops_the_step(L):
     assert _same(before, _state(trainer))
     trainer.train_step(_rows(2, L), _rows(3, L))       # read and cleared: steps go on
     assert not _same(before, _state(trainer))
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_norm_that_is_not_finite_skips_the_step(bad):
+    model, trainer = _trainer()
+    for i in range(2):
+        trainer.train_step(_rows(i), _rows(i + 1))
+    before = _state(trainer)
+    with torch.no_grad():
+        keep = model.layers[0]["D"][3].clone()
+        model.layers[0]["D"][3] = bad
+    _, norm = trainer.train_step(_rows(2), _rows(3))
+    assert not torch.isfinite(norm).any()
+    with torch.no_grad():
+        model.layers[0]["D"][3] = keep
+    assert _same(before, _state(trainer))              # weights, moments and step counts
+    loss, norm = trainer.train_step(_rows(2), _rows(3))
+    assert torch.isfinite(loss).all() and torch.isfinite(norm).all() and not _same(before, _state(trainer))
