@@ -500,7 +500,8 @@ mb_status mb_grad_norm(const mb_tensor *list, int64_t count, float *norm, void *
  * left as they are). Each product is rounded once.
  *   list : the gradients; out: as many tensors of the same numel, each of
  *          either dtype (e.g. fp32 for an optimizer), not overlapping the list
- *          unless out[i] is list[i]; or NULL: in place
+ *          unless out[i] is list[i]; or NULL: in place. What is written must not
+ *          overlap itself: in place, no tensor is listed twice.
  *   max_norm > 0
  */
 mb_status mb_grad_clip(const mb_tensor *list, const mb_tensor *out, int64_t count, const float *norm,

@@ -67,3 +67,53 @@ def test_a_workspace_that_grows_keeps_its_status():
     assert ws.get(256) is first
     grown = ws.get(5000)
     assert grown is ws.buffer and grown.numel() >= 5000 and torch.equal(grown[:256], first[:256])
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if torch.cuda.is_available():
+        pytest.skip("stand-in addresses: only where nothing can be launched")
+    return mb.load_library()
+
+
+def _lst(*entries):
+    return (mb.mb_tensor * len(entries))(*(mb.mb_tensor(*e, 0) for e in entries))
+
+
+def test_clipping_refuses_tensors_over_each_other(lib):
+    F, B = mb.MB_F32, mb.MB_BF16
+    run, bad = (mb.MB_OK, mb.MB_ERR_CUDA), mb.MB_ERR_INVALID_ARG
+
+    def clip(entries, out=None):
+        return lib.mb_grad_clip(_lst(*entries), None if out is None else _lst(*out), len(entries), _at(9), 1.0, None)
+    two = [(_at(0), 10, F), (_at(1), 20, B)]
+    away = [(_at(2), 10, F), (_at(3), 20, F)]
+    assert clip(two) in run and clip(two, away) in run and clip(two, two) in run
+    assert clip(two, [(_at(0), 10, F), (_at(3), 20, B)]) in run          # one in place, one not
+    assert clip(two, [(_at(0) + 40, 10, F), (_at(1) + 40, 20, B)]) in run   # right behind the list
+    assert clip(two, [away[0], (away[0][0] + 40, 20, F)]) in run            # right behind each other
+    assert clip([(_at(0), 10, F), (_at(0), 10, F)], away[:1] + [(_at(3), 10, F)]) in run   # read twice, written apart
+    assert clip([(None, 0, F), (_at(0), 0, F), *two], [(None, 0, F), (_at(0), 0, F), *two]) in run
+    assert clip(two, [(_at(2), 10, F), (_at(0), 20, B)]) == bad             # over the list's other tensor
+    assert clip(two, [(_at(1), 10, F), (_at(3), 20, F)]) == bad
+    assert clip(two, [(_at(1) + 38, 10, F), (_at(3), 20, F)]) == bad        # its last element
+    assert clip(two, [(_at(1), 10, F), (_at(0), 20, B)]) == bad             # changed about
+    assert clip(two, [(_at(2), 10, F), (_at(2) + 36, 20, F)]) == bad        # over each other
+    assert clip(two, [(_at(2), 10, F), (_at(2), 20, F)]) == bad
+    assert clip([(_at(0), 10, F), (_at(0), 10, F)]) == bad                  # scaled twice, by two CTAs at once
+    assert clip([(_at(0), 10, F), (_at(0) + 36, 10, F)]) == bad
+    assert clip([(_at(0), 10, F), (_at(0) + 36, 10, F)], [(_at(0), 10, F), (_at(2), 10, F)]) == bad
+
+
+@pytest.mark.parametrize("n", [3, 100, 101, 2500])
+def test_clipping_finds_one_overlap_in_a_long_list(lib, n):
+    # tensors of 16 elements, 64 bytes, packed; the outputs in another order
+    ins = [(_at(0) + 64 * i, 16, mb.MB_F32) for i in range(n)]
+    out = [(_at(1) + 64 * (i * 7919 % n), 16, mb.MB_F32) for i in range(n)]
+    assert len({o[0] for o in out}) == n
+    call = lambda o: lib.mb_grad_clip(_lst(*ins), None if o is None else _lst(*o), n, _at(9), 1.0, None)
+    assert call(out) in (mb.MB_OK, mb.MB_ERR_CUDA) and call(None) in (mb.MB_OK, mb.MB_ERR_CUDA)
+    for at, to in ((0, out[n - 1][0]), (n // 2, out[0][0] + 60), (n - 1, ins[0][0]), (1, ins[n - 1][0] + 4)):
+        wrong = list(out)
+        wrong[at] = (to, 16, mb.MB_F32)
+        assert call(wrong) == mb.MB_ERR_INVALID_ARG
