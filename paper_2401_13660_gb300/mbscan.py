@@ -640,19 +640,19 @@ def mb_conv1d_backward(x, w, dout, *, bias=None, state=None, dstate_out=None, gr
     dbias [width] fp32 (None without a bias, unless given), dstate [batch, 3,
     width] (None without a state, unless given). What is missing from `grads`
     is allocated, and ws too."""
-    if ws is not None and stream is None and grads is not None and "dx" in grads and "dw" in grads and             (bias is None or "dbias" in grads) and (state is None or "dstate" in grads):
-        rc = (_fast or _native()).conv1d_backward(x, w, dout, bias, state, dstate_out, grads["dx"], grads["dw"],
-                                                  grads.get("dbias"), grads.get("dstate"), ws)
+    wanted = {"dx": True, "dw": True, "dbias": bias is not None, "dstate": state is not None}
+    g = {k: (grads or {}).get(k) for k in wanted}
+    if ws is not None and stream is None and all(g[k] is not None for k, want in wanted.items() if want):
+        rc = (_fast or _native()).conv1d_backward(x, w, dout, bias, state, dstate_out, g["dx"], g["dw"], g["dbias"],
+                                                  g["dstate"], ws)
         if rc >= 0:
             _check(rc, "mb_conv1d_backward")
-            return {k: grads.get(k) for k in ("dx", "dw", "dbias", "dstate")}
+            return g
     a = _conv1d_args(x, w, bias, state)
     batch, L, width = x.shape
     dev = x.device
     _need(dout, "dout", x.dtype, (batch, L, width), dev)
     _need(dstate_out, "dstate_out", x.dtype, (batch, 3, width), dev)
-    g = {k: (grads or {}).get(k) for k in ("dx", "dw", "dbias", "dstate")}
-    wanted = {"dx": True, "dw": True, "dbias": bias is not None, "dstate": state is not None}
     shapes = {"dx": ((batch, L, width), x.dtype), "dw": ((width, 4), torch.float32),
               "dbias": ((width,), torch.float32), "dstate": ((batch, 3, width), x.dtype)}
     for k, (shape, dtype) in shapes.items():
