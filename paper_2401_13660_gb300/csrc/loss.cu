@@ -26,6 +26,9 @@ constexpr int kWarpRows = 2;
 // (64 registers). 1003 x 32001 fp32 with 512 threads and 16, 32, 64 elements 51, 43, 51 us, with 256 or 1024 threads 47 to
 // 55. Rows that are read once keep 8 groups for each of 128 or 256 threads: 1000 x 16000 bf16 12.5 us, read twice 19.
 constexpr int kRowThreads = 512, kOnceGroups = 8;
+// CTAs per SM that the registers of a row that is read once leave room for (fp32: 6 x 128 threads of 80, without that 5:
+// 3000 x 5001 38 us instead of 29).
+template <typename T, int kThreads> constexpr int kOnceCtas = sizeof(T) == 4 ? 768 / kThreads : 1;
 template <typename T, bool kOnce> constexpr int kAhead = kOnce ? kOnceGroups : 32 / kVec<T>;
 
 struct LossArgs {
@@ -44,13 +47,25 @@ __device__ __forceinline__ int target_of(const LossArgs &a, int64_t row, float &
     return w == 0.f ? -1 : y;
 }
 
-// e^x for x = l - m <= 0, both types: on the SFU, within (1.5 |x| + 4) 2^-24 relative. What is far below the maximum
-// weighs as little in the sums as its error does in the gradient (expf takes four times the instructions).
-__device__ __forceinline__ float2 exp2_of(float2 l, float2 minus_m) {
-    const float2 t = mul2(add2(l, minus_m), splat(kLog2e));
+// e^x for x = l - m <= 0 on the SFU, within (1.5 |x| + 4) 2^-24 relative: for bf16 logits, whose gradient is rounded to
+// 2^-9, and for sums that join others, where what is far below the maximum weighs as little as its error does.
+__device__ __forceinline__ float exp_sfu(float x) { return ex2(x * kLog2e); }
+// e^x of the logits: of fp32 ones to the precision of their gradient, down to e^-150 = 0 (masked).
+template <typename T> __device__ __forceinline__ float2 exp2_of(float2 l, float2 minus_m) {
+    const float2 c = add2(l, minus_m);
+    if constexpr (sizeof(T) == 4) return exp_carried(make_float2(max_nan(c.x, -150.f), max_nan(c.y, -150.f)));
+    const float2 t = mul2(c, splat(kLog2e));
     return make_float2(ex2(t.x), ex2(t.y));
 }
-__device__ __forceinline__ float exp_of(float x) { return ex2(x * kLog2e); }
+template <typename T> __device__ __forceinline__ float exp_of(float x) {
+    if constexpr (sizeof(T) == 4) return exp_carried(max_nan(x, -150.f));
+    return exp_sfu(x);
+}
+// w scale / s, the factor of a row's gradient.
+template <typename T> __device__ __forceinline__ float factor(float c, float s) {
+    if constexpr (sizeof(T) == 4) return c / s;
+    return __fdividef(c, s);
+}
 
 // A 16-byte group as pairs.
 template <typename T> constexpr int kPairs = kVec<T> / 2;
@@ -107,14 +122,14 @@ __global__ void __launch_bounds__(32 * kWarpRows) loss_groups_kernel(const T *lo
     for (int g = 0; g < G; ++g)
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            x[g][j] = exp2_of(x[g][j], splat(-m));
+            x[g][j] = exp2_of<T>(x[g][j], splat(-m));
             sum = add2(sum, x[g][j]);
         }
     float s = sum.x + sum.y;
 #pragma unroll
     for (int o = L / 2; o > 0; o /= 2) s += __shfl_xor_sync(kFull, s, o);
     if (!in) return;
-    const float c = w * a.scale, k = __fdividef(c, s);
+    const float c = w * a.scale, k = factor<T>(c, s);
     if (lane == 0) a.loss[row] = y >= 0 ? w * ((m - at) + logf(s)) : 0.f;
     if (!dlogits) return;
     T *d = dlogits + base;
@@ -128,7 +143,7 @@ __global__ void __launch_bounds__(32 * kWarpRows) loss_groups_kernel(const T *lo
         *reinterpret_cast<uint4 *>(d + (g * L + lane) * V) = q;
     }
     // over what this lane has just stored
-    if (y >= 0 && y / V % L == lane) d[y] = from_f32<T>(fmaf(exp_of(at - m), k, -c));
+    if (y >= 0 && y / V % L == lane) d[y] = from_f32<T>(fmaf(exp_of<T>(at - m), k, -c));
 }
 
 // Rows that are no whole groups. N logits per lane; lane l has l, l + 32, ...
@@ -162,12 +177,12 @@ __global__ void __launch_bounds__(32 * kWarpRows) loss_warp_kernel(const T *logi
     at = __shfl_sync(kFull, at, y & 31);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-        x[j] = exp_of(x[j] - m);
+        x[j] = exp_of<T>(x[j] - m);
         s += x[j];
     }
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) s += __shfl_xor_sync(kFull, s, o);
-    const float c = w * a.scale, k = __fdividef(c, s);
+    const float c = w * a.scale, k = factor<T>(c, s);
     if (lane == 0) a.loss[row] = w * ((m - at) + logf(s));
     if (!d) return;
 #pragma unroll
@@ -178,7 +193,7 @@ __global__ void __launch_bounds__(32 * kWarpRows) loss_warp_kernel(const T *logi
 }
 
 // Running maximum m and sum s of exp(x - m); nothing yet: m = -inf, s = 0. A NaN stays in s.
-struct Running {
+template <typename T> struct Running {
     float m = -INFINITY, s = 0.f;
     // masked logits only, so far: their exp(-inf - 0) = 0
     static __device__ __forceinline__ float reference(float top) { return top == -INFINITY ? 0.f : top; }
@@ -187,15 +202,15 @@ struct Running {
 #pragma unroll
         for (int j = 0; j < N; ++j) top = fmaxf(top, fmaxf(x[j].x, x[j].y));
         const float ref = reference(top);
-        float2 sum = make_float2(s * exp_of(m - ref), 0.f);
+        float2 sum = make_float2(s * exp_sfu(m - ref), 0.f);
 #pragma unroll
-        for (int j = 0; j < N; ++j) sum = add2(sum, exp2_of(x[j], splat(-ref)));
+        for (int j = 0; j < N; ++j) sum = add2(sum, exp2_of<T>(x[j], splat(-ref)));
         s = sum.x + sum.y;
         m = top;
     }
     __device__ __forceinline__ void join(float m2, float s2) {
         const float top = fmaxf(m, m2), ref = reference(top);
-        s = s * exp_of(m - ref) + s2 * exp_of(m2 - ref);
+        s = s * exp_sfu(m - ref) + s2 * exp_sfu(m2 - ref);
         m = top;
     }
 };
@@ -204,7 +219,7 @@ struct Running {
 // also the elements before and behind them (rows of odd length begin at any element). With kOnce a thread's groups, at
 // most kOnceGroups, stay in its registers for the gradient.
 template <typename T, int kThreads, int C, bool kOnce>
-__global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kThreads, kOnce ? 1 : 2)
+__global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kThreads, kOnce ? kOnceCtas<T, kThreads> : 2)
     loss_row_kernel(const T *logits, T *dlogits, const LossArgs a) {
     constexpr int V = kVec<T>, P = kPairs<T>;
     __shared__ float sm[kThreads / 32], ss[kThreads / 32], mine[2];
@@ -232,7 +247,7 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kThreads, kOnce ? 1 
     }
     const float at = to_f32(l[y]);
     const float own = odd >= 0 ? to_f32(l[odd]) : -INFINITY;
-    Running run;
+    Running<T> run;
     {
         const float2 x[1] = {make_float2(own, -INFINITY)};
         run.add(x);
@@ -273,17 +288,17 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kThreads, kOnce ? 1 
         }
         cluster_arrive();
         cluster_wait();
-        Running all;
+        Running<T> all;
 #pragma unroll
         for (int i = 0; i < C; ++i) all.join(cluster_load(&mine[0], i), cluster_load(&mine[1], i));
         run = all;
         cluster_arrive();   // has read the others'; waited for at the end
     }
-    const float c = w * a.scale, k = __fdividef(c, run.s), m = run.m;
+    const float c = w * a.scale, k = factor<T>(c, run.s), m = run.m;
     if (tid == 0 && part == 0) a.loss[row] = w * ((m - at) + logf(run.s));
     if (d) {
-        const T hot = from_f32<T>(fmaf(exp_of(at - m), k, -c));
-        if (odd >= 0) d[odd] = odd == y ? hot : from_f32<T>(exp_of(own - m) * k);
+        const T hot = from_f32<T>(fmaf(exp_of<T>(at - m), k, -c));
+        if (odd >= 0) d[odd] = odd == y ? hot : from_f32<T>(exp_of<T>(own - m) * k);
         for (int g = g0 + tid; g < g1; g += kAhead<T, kOnce> * kThreads) {
 #pragma unroll
             for (int q = 0; q < kAhead<T, kOnce>; ++q)
@@ -295,7 +310,7 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kThreads, kOnce ? 1 
                 float2 v[P];
                 to_pairs<T>(raw[q], v);
 #pragma unroll
-                for (int j = 0; j < P; ++j) v[j] = mul2(exp2_of(v[j], splat(-m)), splat(k));
+                for (int j = 0; j < P; ++j) v[j] = mul2(exp2_of<T>(v[j], splat(-m)), splat(k));
                 *reinterpret_cast<uint4 *>(d + v0) = from_pairs<T>(v);
                 if (y >= v0 && y < v0 + V) d[y] = hot;   // over what this thread has just stored
             }

@@ -46,6 +46,28 @@ __device__ __forceinline__ float rcp(float x) {   // 1 / x on the SFU
     return y;
 }
 
+constexpr float kLog2eLow = 1.9259629911e-8f;   // log2(e) - kLog2e
+
+// e^c within 2^-21 relative, |c| <= 150: 2^x on the SFU, whose argument's rounding is carried along (expf takes twice the
+// instructions).
+__device__ __forceinline__ float2 exp_carried(float2 c) {
+    const float2 t = mul2(c, splat(-kLog2e));
+    float2 low = fma2(c, splat(kLog2e), t);
+    low = fma2(c, splat(kLog2eLow), low);
+    return mul2(make_float2(ex2(-t.x), ex2(-t.y)), fma2(low, splat(kLn2), splat(1.f)));
+}
+__device__ __forceinline__ float exp_carried(float c) {
+    const float t = c * -kLog2e;
+    return ex2(-t) * fmaf(fmaf(c, kLog2eLow, fmaf(c, kLog2e, t)), kLn2, 1.f);
+}
+
+// The larger one, or NaN if either is (fmaxf drops it).
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
 // softplus(v) of a pair given u = e^v and o = 1 + u: the same three ranges as softplus() of common.cuh
 __device__ __forceinline__ float2 softplus_of(float2 v, float2 u, float2 o) {
     float2 r = fma2(u, splat(0.33333334f), splat(-0.5f));
