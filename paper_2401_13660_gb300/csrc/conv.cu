@@ -72,24 +72,22 @@ struct ConvShape {
     int rows, tx, gx;
 };
 
-// sigmoid(p) of a pair; e^-p of the accuracy that T wants.
-template <typename T> __device__ __forceinline__ float2 sigmoid2(float2 p);
-template <> __device__ __forceinline__ float2 sigmoid2<__nv_bfloat16>(float2 p) {
-    const float2 a = mul2(p, make_float2(-kLog2e, -kLog2e));
-    const float2 q = add2(make_float2(ex2(a.x), ex2(a.y)), make_float2(1.f, 1.f));
+// 2^64 sigmoid(p) of a pair, as 1 / (2^-64 + 2^-64 e^-p): the SFU's reciprocal flushes results below 2^-126, where
+// p sigmoid(p) is a normal number still (p = -88: -5e-37). e^-p of the accuracy that T wants.
+constexpr float kDown = 0x1p-64f;
+__device__ __forceinline__ float2 sigmoid_of(float2 e) {
+    const float2 q = fma2(e, splat(kDown), splat(kDown));
     return make_float2(rcp(q.x), rcp(q.y));
 }
-// fp32: the rounding of the exponent's product is carried along (2^-22 relative in all; expf takes twice the
-// instructions). Beyond +-100 the result is 1 or 0 to the last bit.
+template <typename T> __device__ __forceinline__ float2 sigmoid2(float2 p);
+template <> __device__ __forceinline__ float2 sigmoid2<__nv_bfloat16>(float2 p) {
+    const float2 a = mul2(p, splat(-kLog2e));
+    return sigmoid_of(make_float2(ex2(a.x), ex2(a.y)));
+}
+// fp32: within 2^-21 relative. Beyond +-100 the result is 1 or 0 to the last bit.
 template <> __device__ __forceinline__ float2 sigmoid2<float>(float2 p) {
-    constexpr float kLog2eLow = 1.9259629911e-8f;   // log2(e) - kLog2e
     const float2 c = make_float2(fminf(fmaxf(p.x, -100.f), 100.f), fminf(fmaxf(p.y, -100.f), 100.f));
-    const float2 t = mul2(c, splat(-kLog2e));
-    float2 low = fma2(c, splat(-kLog2e), make_float2(-t.x, -t.y));
-    low = fma2(c, splat(-kLog2eLow), low);
-    const float2 e = mul2(make_float2(ex2(t.x), ex2(t.y)), fma2(low, splat(kLn2), splat(1.f)));
-    const float2 q = add2(e, splat(1.f));
-    return make_float2(rcp(q.x), rcp(q.y));
+    return sigmoid_of(exp_carried(make_float2(-c.x, -c.y)));
 }
 
 // A 16-byte group as pairs of channels.
@@ -176,7 +174,7 @@ __global__ void __launch_bounds__(kFwdThreads, kFwdCtas)
             float2 p = bv[i];
 #pragma unroll
             for (int k = 0; k < 4; ++k) p = fma2(wv[k][i], u[(j + k) & 3][i], p);
-            o[i] = mul2(p, sigmoid2<T>(p));
+            o[i] = mul2(p, mul2(sigmoid2<T>(p), splat(kDown)));
         }
         put_pairs<T>(dst, o);
         dst += s.width;
@@ -268,7 +266,7 @@ __global__ void __launch_bounds__(kBwdThreads, kBwdCtas<T>)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) p = fma2(wv[k][i], u[(j + k) & 3][i], p);
                 const float2 sg = sigmoid2<T>(p);
-                const float2 h = fma2(p, fma2(sg, splat(-1.f), splat(1.f)), splat(1.f));
+                const float2 h = fma2(p, fma2(sg, splat(-kDown * kDown), splat(kDown)), splat(kDown));   // 2^-64 (1 + p (1 - s))
                 g[(j + 3) & 3][i] = mul2(go[i], mul2(sg, h));
             }
         };
