@@ -12,9 +12,8 @@
     rmsnorm, tied byte head, next-byte cross entropy                 mb_cross_entropy
 
 Each library call is an autograd function whose backward is the library's
-(mb_scan_backward, mb_conv1d_backward, mb_embed_backward; the loss leaves its
-gradient in the forward), so torch composes them with the projections and norms.
-`train_step` ends with mb_grad_norm and mb_grad_clip over all gradients and an
+(mb_scan_backward, mb_conv1d_backward, mb_embed_backward, mb_cross_entropy), so
+torch composes them with the projections and norms. `train_step` ends with mb_grad_norm and mb_grad_clip over all gradients and an
 optimizer step. Weights are those of decoder.init_weights: projections in
 `dtype`, the rest fp32; the residual stream is fp32.
 
@@ -115,14 +114,19 @@ class CrossEntropy(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, targets, scale):
         loss = torch.empty(targets.shape, device=logits.device)
-        _, dlogits = mb.mb_cross_entropy(logits, targets, loss, torch.empty_like(logits), scale=scale)
-        ctx.save_for_backward(dlogits)
+        mb.mb_cross_entropy(logits, targets, loss)
+        ctx.save_for_backward(logits, targets)
+        ctx.scale = scale
         return loss.sum() * scale
 
     @staticmethod
     def backward(ctx, dloss):
-        (dlogits,) = ctx.saved_tensors
-        return dlogits * dloss.to(dlogits.dtype), None, None
+        # the incoming gradient as every row's weight: multiplied in fp32, in the pass that makes dlogits
+        logits, targets = ctx.saved_tensors
+        weight = dloss.expand(targets.shape).contiguous()
+        _, dlogits = mb.mb_cross_entropy(logits, targets, torch.empty_like(weight), torch.empty_like(logits),
+                                         weight=weight, scale=ctx.scale)
+        return dlogits, None, None
 
 
 def rmsnorm(residual, w, eps, dtype):
