@@ -24,6 +24,7 @@ from __future__ import annotations
 import argparse
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import mbscan as mb
 from .decoder import CONFIGS, STORED_KEYS, DecoderConfig, init_weights
@@ -57,6 +58,7 @@ class Embed(torch.autograd.Function):
         return mb.mb_embed(tokens, table, out, scale=scale)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         (tokens,) = ctx.saved_tensors
         shape, dtype = ctx.table
@@ -77,6 +79,7 @@ class Conv1d(torch.autograd.Function):
         return mb.mb_conv1d(x, w, out, bias=bias)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         x, w, bias = ctx.saved_tensors
         g = dict(dx=torch.empty(x.shape, dtype=x.dtype, device=x.device), dw=torch.empty_like(w),
@@ -100,6 +103,7 @@ class Scan(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, z, dt, B, C, A, D, dt_bias, ckpt = ctx.saved_tensors
         g = mb.mb_scan_backward(x, dt, B, C, A, ckpt, dy.contiguous(), z=z, D=D, dt_bias=dt_bias,
@@ -120,6 +124,7 @@ class CrossEntropy(torch.autograd.Function):
         return loss.sum() * scale
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dloss):
         # the incoming gradient as every row's weight: multiplied in fp32, in the pass that makes dlogits
         logits, targets = ctx.saved_tensors

@@ -35,3 +35,28 @@ def test_gradient_of_a_scaled_loss_is_rounded_once(dtype, dloss):
     got = to_np(logits.grad)
     assert np.all((lo <= got) & (got <= hi))
     assert abs(float(loss.detach()) - scale * rl.sum()) <= 1e-5 * scale * np.abs(rl).sum()
+
+
+def _function_calls():
+    ws = tr.Workspace(DEV)
+    g = torch.Generator(device=DEV).manual_seed(6)
+    rnd = lambda *s: torch.randn(*s, device=DEV, generator=g)
+    leaf = lambda *s: rnd(*s).requires_grad_()
+    tokens = torch.randint(0, 256, (2, 20), device=DEV, generator=g)
+    A = (-torch.rand(16, 16, device=DEV, generator=g) - 0.5).requires_grad_()
+    return dict(
+        Embed=lambda x: tr.Embed.apply(x, tokens, 2.0, ws),
+        Conv1d=lambda x: tr.Conv1d.apply(x, leaf(16, 4), leaf(16), ws),
+        Scan=lambda x: tr.Scan.apply(x, leaf(2, 20, 16), leaf(2, 20, 16), leaf(2, 20, 16), leaf(2, 20, 16), A, leaf(16), leaf(16), ws),
+        CrossEntropy=lambda x: tr.CrossEntropy.apply(x, tokens, 0.1))
+
+
+@pytest.mark.parametrize("name, shape", [("Embed", (256, 16)), ("Conv1d", (2, 20, 16)), ("Scan", (2, 20, 16)),
+                                         ("CrossEntropy", (2, 20, 256))])
+def test_a_second_derivative_is_an_error(name, shape):
+    # the kernels give first derivatives only: a backward through a backward would drop what it leaves out
+    x = torch.randn(*shape, device=DEV, generator=torch.Generator(device=DEV).manual_seed(7)).requires_grad_()
+    out = (_function_calls()[name](x) ** 2).sum()
+    (d,) = torch.autograd.grad(out, x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        d.square().sum().backward()
