@@ -47,13 +47,20 @@ class Workspace:
         return self.buffer
 
 
+class Tied:
+    """What the two uses of a tied table share in one pass: the head's part of its gradient, fp32, until the lookup's is
+    added to it."""
+    grad = None
+
+
 class Embed(torch.autograd.Function):
-    """scale * table[tokens] in fp32 (the residual stream)."""
+    """scale * table[tokens] in fp32 (the residual stream). With `tied`, its backward pass, which follows the head's, gives
+    the table's whole gradient: the lookup's part is added to the head's in fp32 and the sum rounded once."""
 
     @staticmethod
-    def forward(ctx, table, tokens, scale, ws):
+    def forward(ctx, table, tokens, scale, ws, tied=None):
         ctx.save_for_backward(tokens)
-        ctx.scale, ctx.ws, ctx.table = scale, ws, (table.shape, table.dtype)
+        ctx.scale, ctx.ws, ctx.tied, ctx.table = scale, ws, tied, (table.shape, table.dtype)
         out = torch.empty(*tokens.shape, table.shape[1], device=table.device)
         return mb.mb_embed(tokens, table, out, scale=scale)
 
@@ -62,10 +69,33 @@ class Embed(torch.autograd.Function):
     def backward(ctx, dout):
         (tokens,) = ctx.saved_tensors
         shape, dtype = ctx.table
-        d = torch.empty(shape, device=dout.device)
+        d = None
+        if ctx.tied is not None:
+            d, ctx.tied.grad = ctx.tied.grad, None
+        add = d is not None
+        if not add:
+            d = torch.empty(shape, device=dout.device)
         ws = ctx.ws.get(mb.mb_embed_backward_workspace_size(tokens.numel(), *shape))
-        mb.mb_embed_backward(tokens, dout.contiguous(), d, scale=ctx.scale, ws=ws)
-        return d.to(dtype), None, None, None
+        mb.mb_embed_backward(tokens, dout.contiguous(), d, scale=ctx.scale, accumulate=add, ws=ws)
+        return d.to(dtype), None, None, None, None
+
+
+class Head(torch.autograd.Function):
+    """h table^T, through cuBLAS both ways; the table's gradient goes to the lookup's backward pass (Embed)."""
+
+    @staticmethod
+    def forward(ctx, h, table, tied):
+        ctx.save_for_backward(h, table)
+        ctx.tied = tied
+        return h @ table.t()
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dlogits):
+        h, table = ctx.saved_tensors
+        d, rows = dlogits.flatten(0, -2).t(), h.flatten(0, -2)
+        ctx.tied.grad = torch.mm(d, rows) if h.dtype == torch.float32 else torch.mm(d, rows, out_dtype=torch.float32)
+        return dlogits @ table, None, None
 
 
 class Conv1d(torch.autograd.Function):
@@ -156,7 +186,8 @@ class Model:
     def logits(self, tokens):
         """tokens [batch, L] (uint8, int32 or int64) -> [batch, L, vocab]."""
         cfg, R, N = self.cfg, self.cfg.dt_rank, self.cfg.d_state
-        residual = Embed.apply(self.emb, tokens, cfg.d_model ** 0.5, self.ws)
+        tied = Tied()
+        residual = Embed.apply(self.emb, tokens, cfg.d_model ** 0.5, self.ws, tied)
         for L in self.layers:
             h = rmsnorm(residual, L["norm_w"], cfg.eps, self.dtype)
             xc = Conv1d.apply(h @ L["W_in"][0].t(), L["conv_w"], L["conv_b"], self.ws)
@@ -164,7 +195,7 @@ class Model:
             y = Scan.apply(xc, h @ L["W_in"][1].t(), rows[..., :R] @ L["W_dt"].t(), rows[..., R:R + N], rows[..., R + N:],
                            L["A"], L["D"], L["dt_bias"], self.ws)
             residual = residual + (y @ L["W_out"].t()).float()
-        return rmsnorm(residual, self.norm_f, cfg.eps, self.dtype) @ self.emb.t()
+        return Head.apply(rmsnorm(residual, self.norm_f, cfg.eps, self.dtype), self.emb, tied)
 
     def loss(self, tokens, targets, counted: int | None = None):
         """Mean loss (nats per byte) of predicting targets [batch, L]; `counted`: how many of them are bytes."""

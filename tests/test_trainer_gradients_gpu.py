@@ -60,3 +60,31 @@ def test_a_second_derivative_is_an_error(name, shape):
     (d,) = torch.autograd.grad(out, x, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         d.square().sum().backward()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradient_of_the_tied_table_is_rounded_once(dtype, monkeypatch):
+    # The head's part and the lookup's are fp32 sums of at most n terms each, joined before anything is rounded: the
+    # gradient lies between the roundings of the ends of 2 (n + 4) u times the sum of the terms' magnitudes.
+    from paper_2401_13660_gb300.decoder import CONFIGS
+    model = tr.Model(CONFIGS["tiny_2x64"], DEV, dtype=dtype, seed=8)
+    g = torch.Generator(device=DEV).manual_seed(9)
+    tokens = torch.randint(0, 40, (2, 40), device=DEV, generator=g)
+    tokens[1, 30:] = -1
+    d = torch.randn(2, 40, 256, device=DEV, generator=g).to(dtype)
+    douts, hs = [], []
+    backward, norm = tr.mb.mb_embed_backward, tr.rmsnorm
+    monkeypatch.setattr(tr.mb, "mb_embed_backward", lambda t, dout, *a, **k: (douts.append(dout.clone()), backward(t, dout, *a, **k))[1])
+    monkeypatch.setattr(tr, "rmsnorm", lambda *a: (hs.append(norm(*a)), hs[-1])[1])
+    logits = model.logits(tokens)
+    t, dn, hn = tokens.cpu().numpy(), to_np(d).reshape(80, 256), to_np(hs[-1]).reshape(80, -1)
+    scale = float(np.float32(model.cfg.d_model ** 0.5))
+    for again in (True, False):   # twice through one graph (the scan's gradients have no fixed order: each by its own)
+        model.emb.grad = None
+        logits.backward(d, retain_graph=again)
+        out, x = to_np(douts[-1]), to_np(model.emb.grad)
+        ref = dn.T @ hn + train.embed_backward(t, out, 256, scale)
+        off = 2 * (80 + 4) * 2.0 ** -24 * (np.abs(dn).T @ np.abs(hn) + train.embed_backward(t, np.abs(out), 256, scale))
+        lo, hi = (to_np(torch.from_numpy(ref + s * off).to(dtype)) for s in (-1, 1))
+        assert np.all((lo <= x) & (x <= hi)), float(np.mean((lo > x) | (x > hi)))
+    assert len(douts) == 2
