@@ -390,7 +390,7 @@ ConvShape shape_of(const ConvParams &p, const Cut &c) {
     return s;
 }
 
-// Dynamic shared memory beyond 48 KB has to be asked for, once per device.
+// Dynamic shared memory beyond 48 KB has to be asked for, on the device that the launch goes to (here: at every call).
 template <typename K> cudaError_t allow_smem(K kernel, size_t bytes) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }

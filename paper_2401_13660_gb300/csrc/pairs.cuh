@@ -1,4 +1,4 @@
-// Helpers of the scans that put two adjacent steps into each packed fp32 operation (forward.cu, backward.cu).
+// Helpers that put two adjacent steps (scans) or elements (convolution, losses) into each packed fp32 operation.
 #pragma once
 
 #include "common.cuh"

@@ -66,10 +66,4 @@ template <int N> __device__ __forceinline__ void stf(float *p, const float (&v)[
     for (int j = 0; j < N; j += 4) *reinterpret_cast<float4 *>(p + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
 }
 
-// e^x for a result that is rounded to T: on the SFU for bf16 (relative error
-// below |x| 1e-7 + 2^-22), the full fp32 function for fp32.
-template <typename T> __device__ __forceinline__ float exp_for(float x);
-template <> __device__ __forceinline__ float exp_for<__nv_bfloat16>(float x) { return ex2(x * kLog2e); }
-template <> __device__ __forceinline__ float exp_for<float>(float x) { return expf(x); }
-
 }  // namespace mbscan
