@@ -169,9 +169,11 @@ class Decoder:
 
     def step(self, tokens, trace=None):
         """Feed one byte per stream (int64 [batch]); returns the logits of the
-        next byte [batch, 256] (bf16). With a list `trace` (eager decoders
-        only), host copies of every block's inputs and outputs are appended
-        to it, one dict per layer."""
+        next byte [batch, 256] (bf16). A token outside the vocabulary is no
+        error: it is looked up as zeros (mb_embed), as for a stream that has
+        nothing to say, and touches no other stream. With a list `trace` (eager
+        decoders only), host copies of every block's inputs and outputs are
+        appended to it, one dict per layer."""
         self.tokens.copy_(tokens)
         if self.graph is not None:
             if trace is not None:
