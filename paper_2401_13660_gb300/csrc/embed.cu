@@ -337,6 +337,11 @@ struct Votes {
     template <typename F> __device__ __forceinline__ unsigned operator()(const F &f) const {
         return __ballot_sync(kFull, f((int)(threadIdx.x & 31)));
     }
+    template <typename F, typename G> __device__ __forceinline__ void operator()(const F &f, const G &g, unsigned &b, unsigned &c) const {
+        const bool x = f((int)(threadIdx.x & 31)), y = g((int)(threadIdx.x & 31));
+        b = __ballot_sync(kFull, x);
+        c = __ballot_sync(kFull, y);
+    }
 };
 
 // Clear the row of a token that does not occur (a warp).

@@ -1,7 +1,7 @@
 // Runs of equal values in sorted keys that are cut into pieces of equal length,
 // looked up by a whole warp. `vote(f)` gives a bit for each lane l whose f(l)
-// holds (a ballot; all else is the same in every lane), `key(i)` is the i-th
-// key. No CUDA in here: the host compiles it too, with keys that check their index.
+// holds (a ballot; all else is the same in every lane), `vote(f, g, b, c)` both
+// at once, `key(i)` is the i-th key. No CUDA in here: the host compiles it too, with keys that check their index.
 #pragma once
 
 #include <stdint.h>
@@ -57,8 +57,9 @@ MB_HOST_DEVICE RunEnds run_ends(const Vote &vote, const Key &key, int64_t n, int
     const auto key_at = [&](int64_t i) { return i >= 0 && i < n ? key(i) : -1; };
     const int64_t q0 = p * piece, q1 = q0 + piece;
     const int enters = key_at(q0), leaves = key_at(q1 - 1);
-    const unsigned b = vote([&](int lane) { return key_at(q0 - 1 - lane * piece) != enters; });
-    const unsigned f = vote([&](int lane) { return key_at(q1 + lane * piece) != leaves; });
+    unsigned b, f;   // both at once: the keys' loads overlap
+    vote([&](int lane) { return key_at(q0 - 1 - lane * piece) != enters; },
+         [&](int lane) { return key_at(q1 + lane * piece) != leaves; }, b, f);
     RunEnds r = {p - (b ? lowest_bit(b) : 32), p + (f ? lowest_bit(f) : 32)};
     if (!b) r.begin = first_at(vote, 0, r.begin, enters, [&](int64_t q) { return key((q + 1) * piece - 1); });
     if (leaves < 0) r.end = p;   // the last piece, cut short

@@ -23,6 +23,10 @@ struct Warp {
         for (int lane = 0; lane < 32; ++lane) v |= (unsigned)f(lane) << lane;
         return v;
     }
+    template <typename F, typename G> void operator()(const F &f, const G &g, unsigned &b, unsigned &c) const {
+        b = (*this)(f);
+        c = (*this)(g);
+    }
 };
 
 static void check(const std::vector<int> &keys, int piece, int per_cta) {
