@@ -97,9 +97,31 @@ mb_status check_list(const mb_tensor *list, int64_t count) {
 }
 Range tensor_range(const mb_tensor &t) { return range_of(t.data, t.numel * elem_size(t.dtype)); }
 
+// Outputs that lie in the order of the list, those of each type by themselves, and away from everything else, as slices of
+// one buffer per type do: a look at every tensor shows it (532 tensors 0.8 us of a call, sorted and searched 5).
+bool plainly_apart(const mb_tensor *list, const mb_tensor *out, int64_t count) {
+    Range all[2] = {};   // of the outputs of a type
+    for (int64_t i = 0; i < count; ++i) {
+        if (out[i].numel == 0) continue;
+        const Range r = tensor_range(out[i]);
+        Range &a = all[out[i].dtype == MB_BF16];
+        if (r.lo < a.hi) return false;
+        if (a.lo == 0) a.lo = r.lo;
+        a.hi = r.hi;
+    }
+    if (overlap(all[0], all[1])) return false;
+    for (int64_t i = 0; i < count; ++i) {
+        if (list[i].numel == 0 || (out[i].data == list[i].data && out[i].dtype == list[i].dtype)) continue;
+        const Range r = tensor_range(list[i]);
+        if (overlap(r, all[0]) || overlap(r, all[1])) return false;
+    }
+    return true;
+}
+
 // Whether each out[i] shares no memory with another output, nor with any tensor of the list but list[i] where it is
-// list[i] itself. (532 tensors: 4 us where the outputs lie in the order of their addresses, 20 where not.)
+// list[i] itself.
 mb_status check_apart(const mb_tensor *list, const mb_tensor *out, int64_t count) {
+    if (plainly_apart(list, out, count)) return MB_OK;
     constexpr int64_t kFew = 128;
     Range few[kFew];
     std::unique_ptr<Range[]> many;
@@ -111,8 +133,7 @@ mb_status check_apart(const mb_tensor *list, const mb_tensor *out, int64_t count
     Range *end = outs;
     for (int64_t i = 0; i < count; ++i)
         if (out[i].numel > 0) *end++ = tensor_range(out[i]);
-    const auto by_lo = [](const Range &a, const Range &b) { return a.lo < b.lo; };
-    if (!std::is_sorted(outs, end, by_lo)) std::sort(outs, end, by_lo);
+    std::sort(outs, end, [](const Range &a, const Range &b) { return a.lo < b.lo; });
     for (Range *r = outs; r + 1 < end; ++r)
         if (r->hi > r[1].lo) return MB_ERR_INVALID_ARG;
     for (int64_t i = 0; i < count; ++i) {

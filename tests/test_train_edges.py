@@ -117,3 +117,21 @@ def test_clipping_finds_one_overlap_in_a_long_list(lib, n):
         wrong = list(out)
         wrong[at] = (to, 16, mb.MB_F32)
         assert call(wrong) == mb.MB_ERR_INVALID_ARG
+
+
+def test_clipping_accepts_outputs_between_the_list(lib):
+    # gradients and their copies allocated in turn, one buffer per type, and both with the types mixed
+    F, B, n = mb.MB_F32, mb.MB_BF16, 300
+    call = lambda i, o: lib.mb_grad_clip(_lst(*i), _lst(*o), n, _at(9), 1.0, None)
+    turn = [[(_at(0) + 128 * k + 64 * side, 16, F) for k in range(n)] for side in (0, 1)]
+    types = [F if k % 3 else B for k in range(n)]
+    flat = [(_at(1 if t == F else 2) + 64 * k, 16, t) for k, t in enumerate(types)]
+    ins = [(_at(0) + 64 * k, 16, t) for k, t in enumerate(types)]
+    for i, o in ((turn[0], turn[1]), (turn[1], turn[0][::-1]), (ins, flat), (flat, flat), (flat, ins), (ins[::-1], flat[::-1])):
+        assert call(i, o) in (mb.MB_OK, mb.MB_ERR_CUDA)
+        for at in (0, 7, n - 1):
+            wrong = list(o)
+            wrong[at] = (o[(at + 5) % n][0], 16, o[at][2])
+            assert call(i, wrong) == mb.MB_ERR_INVALID_ARG
+            wrong[at] = (i[(at + 5) % n][0] + 4, 12, o[at][2])
+            assert call([(*x[:1], 12, x[2]) if k == at else x for k, x in enumerate(i)], wrong) == mb.MB_ERR_INVALID_ARG
