@@ -854,5 +854,6 @@ def mb_selftest_timeout(ws, wait_cycles, stream=None):
 def mb_check(ws, stream=None):
     """Read and clear the workspace status block: (status, detail)."""
     detail = ctypes.c_int64(-1)
-    rc = load_library().mb_check(_ptr(ws), _stream(stream, ws.device), ctypes.byref(detail))
+    dev = torch.device("cuda") if ws is None else ws.device   # no workspace: the library's answer
+    rc = load_library().mb_check(_ptr(ws), _stream(stream, dev), ctypes.byref(detail))
     return int(rc), int(detail.value)

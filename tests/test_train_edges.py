@@ -135,3 +135,7 @@ def test_clipping_accepts_outputs_between_the_list(lib):
             assert call(i, wrong) == mb.MB_ERR_INVALID_ARG
             wrong[at] = (i[(at + 5) % n][0] + 4, 12, o[at][2])
             assert call([(*x[:1], 12, x[2]) if k == at else x for k, x in enumerate(i)], wrong) == mb.MB_ERR_INVALID_ARG
+
+
+def test_the_status_of_no_workspace():
+    assert mb.mb_check(None, stream=0) == (mb.MB_ERR_INVALID_ARG, -1)
