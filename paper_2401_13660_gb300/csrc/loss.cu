@@ -23,11 +23,12 @@ constexpr int kWarpVocab = 1024, kSms = 152;
 // rows side by side 14.3; warps that stay and fetch rows ahead 19.
 constexpr int kWarpRows = 2;
 // Threads of a row that is read twice, and the 16-byte groups that each loads at once: 32 elements, and two CTAs per SM
-// (64 registers). 1003 x 32001 fp32 with 512 threads and 16, 32, 64 elements 51, 43, 51 us, with 256 or 1024 threads 47 to
-// 55. Rows that are read once keep 8 groups for each of 128 or 256 threads: 1000 x 16000 bf16 12.5 us, read twice 19.
+// (64 registers). 1003 x 32001 fp32 44 us; with plainer exponentials 512 threads and 16, 32, 64 elements took 51, 43, 51,
+// 256 or 1024 threads 47 to 55. Rows that are read once keep 8 groups for each of 128 or 256 threads: 3000 x 5001 fp32 30 us,
+// read twice 47; 1000 x 16000 bf16 18.4, read twice 19.6 (with everything in L2 13.0 and 15.2).
 constexpr int kRowThreads = 512, kOnceGroups = 8;
-// CTAs per SM that the registers of a row that is read once leave room for (fp32: 6 x 128 threads of 80, without that 5:
-// 3000 x 5001 38 us instead of 29).
+// CTAs per SM that the registers of a row that is read once leave room for (fp32: 768 threads of 80 registers; of the 86 that
+// the compiler would take 5 CTAs of 128 or 2 of 256 fit: 3000 x 5001 37 us instead of 30).
 template <typename T, int kThreads> constexpr int kOnceCtas = sizeof(T) == 4 ? 768 / kThreads : 1;
 template <typename T, bool kOnce> constexpr int kAhead = kOnce ? kOnceGroups : 32 / kVec<T>;
 
