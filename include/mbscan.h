@@ -507,6 +507,96 @@ mb_status mb_grad_norm(const mb_tensor *list, int64_t count, float *norm, void *
 mb_status mb_grad_clip(const mb_tensor *list, const mb_tensor *out, int64_t count, const float *norm,
                        float max_norm, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Decoding on 8-bit projections, and the drawn token. A matrix in 8 bits is
+ *   q      : [rows, width] bytes, e4m3 (largest 448, no infinities)
+ *   scales : powers of two, one byte each (2^(byte - 127); 255: NaN), for
+ *            128 consecutive columns of one row (block_rows 1: activations) or
+ *            of 128 rows (block_rows 128: weights): [ceil(rows / block_rows),
+ *            mb_q8_scale_stride(width)] bytes; the last blocks of a row of
+ *            scales may be short, the bytes behind them are 127 and are not used
+ * and stands for q * 2^(byte - 127). Rounding x to it: the scale is the
+ * smallest 2^E, E >= -126, with max |x| <= 448 * 2^E over the block (1 where
+ * the block is all zeros), and q = x * 2^-E to nearest, ties to even. NaN and
+ * infinities become NaN and leave the maximum as it is.
+ *   width % 16 == 0 (MB_ERR_UNSUPPORTED otherwise), rows * width <= 2^31;
+ *   scales 4-byte aligned, everything else 16-byte aligned
+ * There are no gradients: what is rounded to 8 bits here is for inference.
+ * ------------------------------------------------------------------------ */
+
+/* Bytes between rows of scales, 4 * ceil(width / 512); 0: width not accepted. */
+int64_t mb_q8_scale_stride(int64_t width);
+
+/*
+ * mb_rmsnorm with its output in 8 bits (block_rows 1):
+ *   residual[b] += add[b]            (skipped when add == NULL)
+ *   q, scales[b] = residual[b] * w / sqrt(mean_j residual[b, j]^2 + eps), rounded once
+ * residual: fp32 [rows, width], read and written; add: dtype [rows, width];
+ * w: fp32 [width]. No argument may overlap another.
+ */
+mb_status mb_rmsnorm_q8(const void *add, int32_t dtype, float *residual, const float *w, float eps, uint8_t *q,
+                        uint8_t *scales, int64_t rows, int64_t width, void *stream);
+
+/*
+ * Round x [rows, width] (dtype) to 8 bits; rows of x start x_stride elements
+ * apart (0 means width; otherwise >= width with x_stride * element size a
+ * multiple of 16 bytes). block_rows: 1 or 128. Outputs must not overlap.
+ */
+mb_status mb_quantize_q8(const void *x, int32_t dtype, int64_t x_stride, int32_t block_rows, uint8_t *q, uint8_t *scales,
+                         int64_t rows, int64_t width, void *stream);
+
+/* The values back: out [rows, width] (dtype, rounded once; exact in fp32 but below its range). */
+mb_status mb_dequantize_q8(const uint8_t *q, const uint8_t *scales, int32_t block_rows, void *out, int32_t dtype,
+                           int64_t rows, int64_t width, void *stream);
+
+/*
+ * Projection in 8 bits on the tensor cores:
+ *   out[m, n] = sum_k A[m, k] W[n, k]
+ * with A [rows, width] (a, a_scales: block_rows 1) and W [n_out, width] (w,
+ * w_scales: block_rows 128) the values that stand in 8 bits; products are
+ * exact, sums fp32 in an order that depends on the sizes only, out rounded once.
+ *   out  : [n_out / part, rows, part], out_dtype: columns n of the product in
+ *          groups of `part` (0: n_out, one group), each a matrix of its own:
+ *          [x | z] of one projection come apart. part % 128 == 0 and n_out % part
+ *          == 0, unless part is n_out
+ *   n_out % 8 == 0 (MB_ERR_UNSUPPORTED otherwise); rows * n_out, n_out * width <= 2^31
+ *   ws, ws_bytes : workspace (at least 256 bytes, 256-byte aligned, its status
+ *          block zeroed once after allocation) or NULL. A bounded wait that
+ *          gives up records MB_ERR_TIMEOUT there (mb_check).
+ * out and ws must not overlap anything else. NaN in a row of A, or in W, shows
+ * in every sum it is part of.
+ */
+mb_status mb_matmul_q8(const uint8_t *a, const uint8_t *a_scales, const uint8_t *w, const uint8_t *w_scales, void *out,
+                       int32_t out_dtype, int64_t rows, int64_t n_out, int64_t width, int64_t part, void *ws,
+                       size_t ws_bytes, void *stream);
+
+/*
+ * Draw the next token of every stream from its logits and a given random
+ * number. Per row, with weights w_i = exp((l_i - max l) / temperature) and the
+ * tokens in the order of falling logits (of equal ones the lower index first):
+ *   1. the first top_k tokens are kept (0 or less: all);
+ *   2. of these, those before which there is less than top_p of their mass
+ *      (1 or more: all; always the first);
+ *   3. of these, those with w_i >= min_p (0 or less: all; at least 1: those
+ *      with the largest logit);
+ *   token = the lowest index up to which there is more than u of the mass left.
+ *   logits : [n, vocab], dtype, contiguous (any vocab from 1 to 2^30; n * vocab
+ *            <= 2^31). -inf is a masked token, NaN counts as -inf, +inf as the type's
+ *            largest finite number
+ *   u      : [n] fp32 in [0, 1) (1 or more: the last token left; below 0 or NaN: the first)
+ *   temperature, top_p, min_p : [n] fp32, top_k : [n] int32, or NULL: 1, 1, 0, 0.
+ *            A temperature of 0 (or less, or NaN) takes the largest logit; NaN
+ *            in top_p or min_p switches that one off
+ *   tokens : [n], MB_TOKEN_I32 or MB_TOKEN_I64; -1 where every token is masked
+ *   prob   : [n] fp32 or NULL: the probability the token was drawn with (0 with -1)
+ * Weights are within 2^-32 of their value and all sums and comparisons exact:
+ * the draw is reproducible, and differs from that of exact arithmetic only
+ * where a border is as near as that. tokens and prob must not overlap anything else.
+ */
+mb_status mb_sample(const void *logits, int32_t dtype, const float *u, const float *temperature, const int32_t *top_k,
+                    const float *top_p, const float *min_p, void *tokens, int32_t token_type, float *prob, int64_t n,
+                    int64_t vocab, void *stream);
+
 /*
  * Read and clear the status block of a workspace (blocking: waits for
  * `stream`). Returns MB_OK, or the first device-side error recorded by

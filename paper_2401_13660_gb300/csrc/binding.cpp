@@ -11,6 +11,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -40,6 +41,11 @@ struct Api {
     decltype(&mb_cross_entropy) cross_entropy;
     decltype(&mb_grad_norm) grad_norm;
     decltype(&mb_grad_clip) grad_clip;
+    decltype(&mb_rmsnorm_q8) rmsnorm_q8;
+    decltype(&mb_quantize_q8) quantize_q8;
+    decltype(&mb_dequantize_q8) dequantize_q8;
+    decltype(&mb_matmul_q8) matmul_q8;
+    decltype(&mb_sample) sample;
 } api;
 
 // One call's tensors and whether all of them are as they should be.
@@ -545,6 +551,129 @@ PyObject *grad_clip(ARGS) {
     });
 }
 
+// An 8-bit matrix [rows, width] at i and its scales at `scales_at`.
+struct Q8 {
+    uint8_t *q = nullptr, *scales = nullptr;
+    int64_t rows = 0, width = 0;
+};
+bool fill_q8(Call &c, Q8 &m, int i, int scales_at, int64_t block_rows) {
+    const at::Tensor *t = c.get(i);
+    if (!t || t->dim() != 2 || (t->scalar_type() != at::kFloat8_e4m3fn && t->scalar_type() != at::kByte)) return false;
+    m.rows = t->size(0);
+    m.width = t->size(1);
+    m.q = static_cast<uint8_t *>(c.must(i, t->scalar_type(), {}, true));
+    const int64_t words = (m.width + 511) / 512;
+    m.scales = static_cast<uint8_t *>(c.must(scales_at, at::kByte, {(m.rows + block_rows - 1) / block_rows, 4 * words}));
+    return c.ok;
+}
+// The call's tensors are on the current device, whose stream it takes.
+bool here(const Call &c) { return c.dev.index() == c10::cuda::current_device(); }
+
+bool block_rows_of(PyObject *o, int32_t &block_rows) {
+    if (!PyLong_CheckExact(o)) return false;
+    int over = 0;
+    const long n = PyLong_AsLongAndOverflow(o, &over);
+    block_rows = (int32_t)n;
+    return !over && (n == 1 || n == 128);
+}
+
+// residual, w, q, scales, add, eps
+PyObject *rmsnorm_q8(ARGS) {
+    return guarded(n, 6, [&]() -> long {
+        Call c{v};
+        Q8 m;
+        if (!fill_q8(c, m, 2, 3, 1) || !PyFloat_CheckExact(v[5])) return -1;
+        float *res = static_cast<float *>(c.must(0, kF32, {m.rows, m.width}));
+        const float *w = static_cast<const float *>(c.must(1, kF32, {m.width}));
+        const at::Tensor *add = c.get(4);
+        int32_t dt = MB_BF16;
+        if (add && !dtype_of(add, dt)) return -1;
+        const void *ap = add ? c.must(4, add->scalar_type(), {m.rows, m.width}) : nullptr;
+        if (!c.ok || !here(c)) return -1;
+        const float eps = (float)PyFloat_AS_DOUBLE(v[5]);
+        return call([&](void *s) { return api.rmsnorm_q8(ap, dt, res, w, eps, m.q, m.scales, m.rows, m.width, s); });
+    });
+}
+
+// x, q, scales, block_rows
+PyObject *quantize_q8(ARGS) {
+    return guarded(n, 4, [&]() -> long {
+        Call c{v};
+        Q8 m;
+        int32_t br, dt;
+        const at::Tensor *x = c.get(0);
+        if (!block_rows_of(v[3], br) || !fill_q8(c, m, 1, 2, br) || !dtype_of(x, dt)) return -1;
+        if (x->dim() != 2 || x->size(0) != m.rows || x->size(1) != m.width || !c.on(*x) || !here(c)) return -1;
+        if (!x->is_contiguous() && (x->stride(1) != 1 || x->stride(0) < m.width)) return -1;
+        const int64_t S = x->is_contiguous() || m.rows == 1 ? m.width : x->stride(0);
+        const void *xp = c.ptr(x);
+        if (!c.ok) return -1;
+        return call([&](void *s) { return api.quantize_q8(xp, dt, S, br, m.q, m.scales, m.rows, m.width, s); });
+    });
+}
+
+// q, scales, out, block_rows
+PyObject *dequantize_q8(ARGS) {
+    return guarded(n, 4, [&]() -> long {
+        Call c{v};
+        Q8 m;
+        int32_t br, dt;
+        const at::Tensor *o = c.get(2);
+        if (!block_rows_of(v[3], br) || !fill_q8(c, m, 0, 1, br) || !dtype_of(o, dt)) return -1;
+        void *op = c.must(2, o->scalar_type(), {m.rows, m.width});
+        if (!c.ok || !here(c)) return -1;
+        return call([&](void *s) { return api.dequantize_q8(m.q, m.scales, br, op, dt, m.rows, m.width, s); });
+    });
+}
+
+// a, a_scales, w, w_scales, out, ws
+PyObject *matmul_q8(ARGS) {
+    return guarded(n, 6, [&]() -> long {
+        Call c{v};
+        Q8 a, w;
+        int32_t dt;
+        const at::Tensor *o = c.get(4);
+        if (!fill_q8(c, a, 0, 1, 1) || !fill_q8(c, w, 2, 3, 128) || !dtype_of(o, dt) || a.width != w.width) return -1;
+        void *op;
+        int64_t part = w.rows;
+        if (o->dim() == 2) op = c.must(4, o->scalar_type(), {a.rows, w.rows});
+        else if (o->dim() == 3) {
+            part = o->size(2);
+            if (o->size(0) * part != w.rows) return -1;
+            op = c.must(4, o->scalar_type(), {o->size(0), a.rows, part});
+        } else return -1;
+        size_t wb;
+        void *ws = workspace(c, 5, wb, true);
+        if (!c.ok || !here(c)) return -1;
+        return call([&](void *s) {
+            return api.matmul_q8(a.q, a.scales, w.q, w.scales, op, dt, a.rows, w.rows, a.width, part, ws, wb, s);
+        });
+    });
+}
+
+// logits, u, tokens, temperature, top_k, top_p, min_p, prob
+PyObject *sample(ARGS) {
+    return guarded(n, 8, [&]() -> long {
+        Call c{v};
+        const at::Tensor *l = c.get(0), *tok = c.get(2);
+        int32_t dt, tt;
+        if (!dtype_of(l, dt) || l->dim() != 2 || !token_type(tok, tt) || tt == MB_TOKEN_U8) return -1;
+        const int64_t rows = l->size(0), vocab = l->size(1);
+        const void *lp = c.must(0, l->scalar_type(), {rows, vocab});
+        const float *u = static_cast<const float *>(c.must(1, kF32, {rows}));
+        void *tp = c.must(2, tok->scalar_type(), {rows});
+        const float *temperature = static_cast<const float *>(c.need(3, kF32, {rows}));
+        const int32_t *top_k = static_cast<const int32_t *>(c.need(4, at::kInt, {rows}));
+        const float *top_p = static_cast<const float *>(c.need(5, kF32, {rows}));
+        const float *min_p = static_cast<const float *>(c.need(6, kF32, {rows}));
+        float *prob = static_cast<float *>(c.need(7, kF32, {rows}));
+        if (!c.ok || !here(c)) return -1;
+        return call([&](void *s) {
+            return api.sample(lp, dt, u, temperature, top_k, top_p, min_p, tp, tt, prob, rows, vocab, s);
+        });
+    });
+}
+
 // init(addresses of the entry points, in Api's order)
 PyObject *init(ARGS) {
     constexpr Py_ssize_t kN = sizeof(Api) / sizeof(void *);
@@ -567,6 +696,7 @@ PyMethodDef methods[] = {DEF(init),     DEF(step),          DEF(step_resume), DE
                          DEF(verify),   DEF(verify_resume), DEF(rollback),    DEF(accept_topk), DEF(rmsnorm),
                          DEF(conv1d_step), DEF(conv_xproj), DEF(conv1d), DEF(conv1d_backward),
                          DEF(embed), DEF(embed_backward), DEF(cross_entropy), DEF(grad_norm), DEF(grad_clip),
+                         DEF(rmsnorm_q8), DEF(quantize_q8), DEF(dequantize_q8), DEF(matmul_q8), DEF(sample),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mbcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -98,10 +98,6 @@ __device__ __forceinline__ float reduce_rows(const float (&part)[kStepRows], int
     return keep + __shfl_xor_sync(kFull, send, 1);
 }
 
-__device__ __forceinline__ void mbar_arrive(uint64_t *bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-
 // Four consecutive shared-memory elements of the input dtype, widened.
 __device__ __forceinline__ float4 lds4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
 __device__ __forceinline__ float4 lds4(const __nv_bfloat16 *p) {

@@ -59,8 +59,8 @@ constexpr int kMaxRank = 256;
 constexpr int kDState = 16;
 constexpr int kCkptSteps = 16;   // steps between the state checkpoints of the training forward
 
-// Encode a tiled TMA tensor map over `base` (bf16 when elem_bytes == 2, else
-// fp32): dims innermost first, strides[i] = byte stride of dimension i + 1,
+// Encode a tiled TMA tensor map over `base` (bytes when elem_bytes == 1,
+// bf16 when 2, else fp32): dims innermost first, strides[i] = byte stride of dimension i + 1,
 // box = tile extent per dimension. Out-of-range elements load as zeros.
 // swizzle: 0 (rows stored as they are), 64 or 128: rows of the box (that
 // many bytes) stored with that swizzle, 16-byte chunk j of row i at chunk
@@ -179,6 +179,39 @@ size_t conv_xproj_partial_bytes(int64_t batch, int64_t width, int n_out);
 cudaError_t launch_conv_xproj(const void *x, void *state, const float *w, const float *bias, const void *W,
                               void *xc, void *out, int64_t batch, int64_t width, int n_out, float *part,
                               StatusBlock *status, cudaStream_t s);
+// 8-bit values with block scales (quant.cu). rows, width > 0.
+constexpr int kQuantBlock = 128;                     // columns (and, of weights, rows) that share a scale
+constexpr int64_t quant_stride(int64_t width) {      // bytes between rows of scales: whole 32-bit words
+    return 4 * ((width + 4 * kQuantBlock - 1) / (4 * kQuantBlock));
+}
+cudaError_t launch_rmsnorm_q8(const void *add, bool bf16, float *residual, const float *w, float eps, uint8_t *q,
+                              uint8_t *scales, int64_t rows, int64_t width, cudaStream_t s);
+cudaError_t launch_quantize(const void *x, bool bf16, int64_t x_stride, bool blocks, uint8_t *q, uint8_t *scales, int64_t rows,
+                            int64_t width, cudaStream_t s);
+cudaError_t launch_dequantize(const uint8_t *q, const uint8_t *scales, bool blocks, void *out, bool bf16, int64_t rows,
+                              int64_t width, cudaStream_t s);
+// Product of 8-bit matrices (matmul.cu). rows, n_out, width > 0.
+struct MatmulParams {
+    const uint8_t *a, *a_scales;   // [rows, width], [rows, quant_stride(width)]
+    const uint8_t *w, *w_scales;   // [n_out, width], [ceil(n_out / 128), quant_stride(width)]
+    void *out;                     // [n_out / part, rows, part]
+    int64_t rows, n_out, width, part;
+    StatusBlock *status;           // may be null
+};
+cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t s);
+// Draws from next-token distributions (sample.cu). n, vocab > 0.
+struct SampleParams {
+    const void *logits;
+    const float *u, *temperature;  // all but u may be null
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+    void *tokens;
+    bool wide;                     // int64 tokens
+    float *prob;                   // may be null
+    int64_t n;
+    int vocab;
+};
+cudaError_t launch_sample(const SampleParams &p, bool bf16, cudaStream_t s);
 cudaError_t launch_step(const ScanParams &p, bool bf16, cudaStream_t s);
 // One step from the state kept after accept[s] drafted bytes: p.h0 (may be
 // null = zeros) when accept[s] == 0, else h_all[s, accept[s]-1]; the new state

@@ -1,0 +1,288 @@
+// Product of 8-bit matrices with block scales (quant.cu) on the fifth-generation tensor cores:
+//   out[m, n] = sum_b 2^(sa[m, b] + sw[n / 128, b] - 254) sum_{k in block b} a[m, k] w[n, k]
+// The scales are powers of two, so the tensor core applies them to its own products (block-scaled tcgen05.mma; its scale
+// granularity is 32 columns, a block of 128 is four instructions with the same scale), and the sum over all blocks stays in
+// fp32 in tensor memory: no pass over partial sums.
+//
+// The weights are the instruction's A operand (128 output features in the 128 lanes), the rows of a its B operand (16 to
+// 240 of them, the columns of the sum in tensor memory): one row costs an eighth of a tile then, not 127 idle lanes, and a
+// decode step streams each weight through one tile.
+//
+// Eight warps: one issues the TMA copies of both operands into a ring of stages (128 columns of the sum each, 128-byte
+// swizzle), one the products, one lays out scales for the tensor core (512 columns' worth at a time: the four scales of a
+// word go to one column of tensor memory), and four move finished sums to global memory while the next tile's products run
+// into the other half of tensor memory. CTAs take tiles in turn. Where tiles are few, a cluster of CTAs shares each tile's
+// sum, every one over part of it, and they add their parts up in order through distributed shared memory.
+#include "../../include/mbscan.h"
+#include "cluster.cuh"
+#include "common.cuh"
+#include "umma.cuh"
+
+namespace mbscan {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kFeatures = 128;       // output features of a tile: lanes of tensor memory
+constexpr int kMaxRows = 240;        // rows of a tile: two sums and the scales fit 512 columns
+constexpr int kK = kQuantBlock;      // columns of the sum in a stage
+constexpr int kMaxStages = 12;
+constexpr int kSlots = 4;            // of the ring of scales
+constexpr int kSlotBytes = 512 + 1024;   // a tile's features, then 256 rows
+constexpr int kScaleColumns = 4 + 8;
+constexpr int kMaxSplit = 8;
+
+struct Tiles {
+    int features, rows;       // tiles across
+    int height;               // rows of a tile, a multiple of 16
+    int blocks;               // 128-column blocks of the sum
+    int split, stages;
+    uint32_t columns;         // of tensor memory
+};
+
+struct Args {
+    CUtensorMap a, w;
+    MatmulParams p;
+    Tiles t;
+    int stride;               // bytes between rows of scales
+};
+
+struct Barriers {
+    uint64_t full[kMaxStages], empty[kMaxStages];
+    uint64_t scales_full[kSlots], scales_empty[kSlots];
+    uint64_t sum_full[2], sum_empty[2];
+    uint32_t tmem;
+};
+
+template <typename T> __device__ __forceinline__ T *out_at(const MatmulParams &p, int64_t row, int64_t n) {
+    const int64_t part = n / p.part;
+    return static_cast<T *>(p.out) + (part * p.rows + row) * p.part + (n - part * p.part);
+}
+
+__device__ __forceinline__ float4 cluster_load4(uint32_t address) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(address)
+                 : "memory");
+    return v;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_constant__ Args g) {
+    extern __shared__ unsigned char dyn[];
+    __shared__ Barriers bar;
+    unsigned char *const smem = dyn + ((1024u - (smem_u32(dyn) & 1023u)) & 1023u);
+    const Tiles &t = g.t;
+    const uint32_t a_bytes = (uint32_t)t.height * kK, stage_bytes = kFeatures * kK + a_bytes;
+    unsigned char *const scales = smem + (size_t)t.stages * stage_bytes;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = (int)(blockIdx.x % (unsigned)t.split), first = (int)(blockIdx.x / (unsigned)t.split);
+    const int step = (int)(gridDim.x / (unsigned)t.split), tiles = t.features * t.rows;
+    const int k0 = (int)((int64_t)t.blocks * rank / t.split), k1 = (int)((int64_t)t.blocks * (rank + 1) / t.split);
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < t.stages; ++i) {
+            mbar_init(&bar.full[i], 1);
+            mbar_init(&bar.empty[i], 1);
+        }
+        for (int i = 0; i < kSlots; ++i) {
+            mbar_init(&bar.scales_full[i], 32);
+            mbar_init(&bar.scales_empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&bar.sum_full[i], 1);
+            mbar_init(&bar.sum_empty[i], 128);
+        }
+        fence_mbar_init();
+        // this CTA's first weights are on their way to L2 while the kernel before drains
+        for (int k = k0; k < k1; ++k) tma_prefetch_2d(&g.w, k * kK, first % t.features * kFeatures);
+    }
+    if (warp == 0) tmem_alloc(&bar.tmem, t.columns);
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t tmem = bar.tmem, tmem_w = tmem + 2 * t.height, tmem_a = tmem_w + 4;
+    pdl_trigger();
+    pdl_wait();
+
+    bool ok = true;
+    if (warp == 0) {
+        if (lane == 0) {
+            int issued = 0;
+            for (int tile = first; tile < tiles && ok; tile += step) {
+                const int n0 = tile % t.features * kFeatures, m0 = tile / t.features * t.height;
+                for (int k = k0; k < k1; ++k, ++issued) {
+                    const int s = issued % t.stages;
+                    if (!(ok = mbar_wait(&bar.empty[s], (issued / t.stages & 1) ^ 1))) break;
+                    unsigned char *at = smem + (size_t)s * stage_bytes;
+                    mbar_arrive_expect_tx(&bar.full[s], stage_bytes);
+                    tma_load_2d(at, &g.w, &bar.full[s], k * kK, n0);
+                    tma_load_2d(at + kFeatures * kK, &g.a, &bar.full[s], k * kK, m0);
+                }
+            }
+            // a failed CTA must not end with copies in flight
+            for (int i = issued > t.stages ? issued - t.stages : 0; !ok && i < issued; ++i)
+                if (!mbar_wait(&bar.full[i % t.stages], i / t.stages & 1)) break;
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            int used = 0, group = 0, count = 0;
+            for (int tile = first; tile < tiles && ok; tile += step, ++count) {
+                const uint32_t sum = tmem + (count & 1) * t.height;
+                if (!(ok = mbar_wait(&bar.sum_empty[count & 1], (count >> 1 & 1) ^ 1))) break;
+                tmem_fence_after();
+                for (int k = k0; k < k1; ++k, ++used) {
+                    const int slot = group % kSlots, s = used % t.stages;
+                    if (k == k0 || k % 4 == 0) {
+                        if (!(ok = mbar_wait(&bar.scales_full[slot], group / kSlots & 1))) break;
+                        const uint32_t at = smem_u32(scales) + slot * kSlotBytes;
+                        tmem_copy_scales(tmem_w, umma_desc_rows16(at));
+                        tmem_copy_scales(tmem_a, umma_desc_rows16(at + 512));
+                        if (t.height > 128) tmem_copy_scales(tmem_a + 4, umma_desc_rows16(at + 1024));
+                    }
+                    if (!(ok = mbar_wait(&bar.full[s], used / t.stages & 1))) break;
+                    tmem_fence_after();
+                    const uint32_t at = smem_u32(smem) + s * stage_bytes;
+                    const uint64_t dw = umma_desc_128(at), da = umma_desc_128(at + kFeatures * kK);
+                    const uint32_t word = umma_word_q8(kFeatures, t.height, k % 4);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) umma_q8(sum, dw + 2 * j, da + 2 * j, word, tmem_w, tmem_a, k > k0 || j > 0);
+                    umma_commit(&bar.empty[s]);
+                    if (k == k1 - 1 || k % 4 == 3) {
+                        umma_commit(&bar.scales_empty[slot]);
+                        ++group;
+                    }
+                }
+                if (ok) umma_commit(&bar.sum_full[count & 1]);
+            }
+        }
+    } else if (warp == 2) {
+        int group = 0;
+        for (int tile = first; tile < tiles && ok; tile += step) {
+            const int n0 = tile % t.features, m0 = tile / t.features * t.height;
+            for (int q = k0 / 4; q <= (k1 - 1) / 4; ++q, ++group) {
+                const int slot = group % kSlots;
+                if (!(ok = __all_sync(kFull, mbar_wait(&bar.scales_empty[slot], (group / kSlots & 1) ^ 1)))) break;
+                const uint32_t w = *reinterpret_cast<const uint32_t *>(g.p.w_scales + (int64_t)n0 * g.stride + 4 * q);
+                uint4 *at = reinterpret_cast<uint4 *>(scales + slot * kSlotBytes);
+                at[lane] = make_uint4(w, w, w, w);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t v[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int64_t row = m0 + 128 * half + 32 * j + lane;
+                        v[j] = row < g.p.rows ? *reinterpret_cast<const uint32_t *>(g.p.a_scales + row * g.stride + 4 * q) : 0x7f7f7f7fu;
+                    }
+                    at[32 + 32 * half + lane] = make_uint4(v[0], v[1], v[2], v[3]);
+                }
+                fence_proxy_async_smem();
+                mbar_arrive(&bar.scales_full[slot]);
+            }
+        }
+    } else if (warp >= 4) {
+        int count = 0;
+        for (int tile = first; tile < tiles && ok; tile += step, ++count) {
+            const int64_t n = (int64_t)(tile % t.features) * kFeatures + (warp - 4) * 32 + lane;
+            const int64_t m0 = (int64_t)(tile / t.features) * t.height;
+            if (!(ok = __all_sync(kFull, mbar_wait(&bar.sum_full[count & 1], count >> 1 & 1)))) break;
+            tmem_fence_after();
+            const uint32_t sum = tmem + (count & 1) * t.height + ((uint32_t)(warp - 4) * 32 << 16);
+            const int rows = (int)(g.p.rows - m0 < t.height ? g.p.rows - m0 : t.height);
+            for (int c = 0; c < rows; c += 16) {
+                uint32_t v[16];
+                tmem_load16(sum + c, v);
+                tmem_load_wait(v);
+                if (t.split > 1) {   // this CTA's part of the sum, where the ring was
+                    float *part = reinterpret_cast<float *>(smem) + c * kFeatures + (warp - 4) * 32 + lane;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) part[j * kFeatures] = __uint_as_float(v[j]);
+                } else if (n < g.p.n_out) {
+                    T *o = out_at<T>(g.p, m0 + c, n);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (c + j < rows) o[j * g.p.part] = from_f32<T>(__uint_as_float(v[j]));
+                }
+            }
+            tmem_fence_before();
+            mbar_arrive(&bar.sum_empty[count & 1]);
+        }
+    }
+    if (!ok) report(g.p.status, MB_ERR_TIMEOUT, blockIdx.x);
+    __syncthreads();
+    if (t.split > 1) {   // the parts in the order of their ranks, every CTA for its share of the rows
+        cluster_arrive();
+        cluster_wait();
+        const int64_t m0 = (int64_t)(first / t.features) * t.height, n0 = (int64_t)(first % t.features) * kFeatures;
+        const int r0 = t.height * rank / t.split, r1 = t.height * (rank + 1) / t.split;
+        for (int i = r0 * 32 + threadIdx.x; i < r1 * 32; i += kThreads) {
+            const int64_t m = m0 + i / 32, n = n0 + i % 32 * 4;
+            if (m >= g.p.rows || n >= g.p.n_out) continue;
+            const float *part = reinterpret_cast<const float *>(smem) + 4 * i;
+            float4 v[kMaxSplit];
+#pragma unroll
+            for (int s = 0; s < kMaxSplit; ++s)
+                if (s < t.split) v[s] = cluster_load4(cluster_address(part, s));
+#pragma unroll
+            for (int s = 1; s < kMaxSplit; ++s)
+                if (s < t.split) {
+                    v[0].x += v[s].x; v[0].y += v[s].y; v[0].z += v[s].z; v[0].w += v[s].w;
+                }
+            T *o = out_at<T>(g.p, m, n);
+            const float f[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = from_f32<T>(f[j]);
+        }
+        cluster_arrive();   // nobody ends while its part is read
+        cluster_wait();
+    }
+    if (warp == 0) tmem_free(tmem, t.columns);
+}
+
+}  // namespace
+
+cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t s) {
+    const DeviceLimits *lim = device_limits();
+    if (!lim) return cudaErrorInvalidDevice;
+    Args g;
+    g.p = p;
+    g.stride = (int)quant_stride(p.width);
+    Tiles &t = g.t;
+    t.features = (int)((p.n_out + kFeatures - 1) / kFeatures);
+    t.rows = (int)((p.rows + kMaxRows - 1) / kMaxRows);
+    t.height = (int)(((p.rows + t.rows - 1) / t.rows + 15) / 16 * 16);
+    t.blocks = (int)((p.width + kK - 1) / kK);
+    const int64_t tiles = (int64_t)t.features * t.rows;
+    t.split = 1;
+    while (t.split < kMaxSplit && tiles * t.split * 2 <= lim->sms && t.blocks >= 4 * t.split) t.split *= 2;
+    const int stage = (kFeatures + t.height) * kK;
+    const size_t room = lim->smem_optin - 1024 - sizeof(Barriers) - 64 - kSlots * kSlotBytes;
+    t.stages = (int)(room / stage);
+    if (t.stages > kMaxStages) t.stages = kMaxStages;
+    size_t smem = 1024 + (size_t)t.stages * stage + kSlots * kSlotBytes;
+    for (t.columns = 32; (int)t.columns < 2 * t.height + kScaleColumns; t.columns *= 2) {}
+    const uint64_t wd[2] = {(uint64_t)p.width, (uint64_t)p.n_out}, ad[2] = {(uint64_t)p.width, (uint64_t)p.rows};
+    const uint64_t st[1] = {(uint64_t)p.width};
+    const uint32_t wb[2] = {kK, kFeatures}, ab[2] = {kK, (uint32_t)t.height};
+    if (!encode_tmap(&g.w, p.w, 1, 2, wd, st, wb, 128) || !encode_tmap(&g.a, p.a, 1, 2, ad, st, ab, 128))
+        return cudaErrorInvalidValue;
+    auto kern = out_bf16 ? matmul_q8_kernel<__nv_bfloat16> : matmul_q8_kernel<float>;
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(lim->smem_optin - sizeof(Barriers) - 64));
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(t.split > 1 ? tiles * t.split : tiles < lim->sms ? tiles : lim->sms));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = MB_PDL;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)t.split;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = t.split > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, g);
+}
+
+}  // namespace mbscan

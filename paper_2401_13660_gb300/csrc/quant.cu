@@ -1,0 +1,284 @@
+// 8-bit values with block scales, for projections whose products run in 8 bits
+// (matmul.cu). A block of 128 consecutive columns (of one row: activations; of
+// 128 rows: weights) shares a power of two, so that the largest value it holds
+// fits e4m3's range (448 = 1.75 * 2^8):
+//   E = the smallest integer >= -126 with max |x| <= 448 * 2^E   (0 where the block is all zeros)
+//   q = e4m3(x * 2^-E), to nearest, ties to even; scale byte E + 127
+// A power of two costs no accuracy where e4m3 is normal (the product x * 2^-E
+// is exact), and the tensor cores apply it to their products themselves. NaN
+// and infinities become NaN and take no part in the maximum, so that the rest
+// of their block keeps its values and the error shows in what is computed from
+// them.
+//
+// All of these are streaming kernels bound by memory: a warp takes a block at a
+// time, four columns a lane (16-byte loads of fp32, 8 of bf16, 4-byte stores),
+// and finds the block's maximum in one integer reduction (the bits of
+// non-negative floats are ordered as they are).
+#include <cuda_fp8.h>
+
+#include "common.cuh"
+#include "vec.cuh"
+
+namespace mbscan {
+namespace {
+
+constexpr int kBlock = kQuantBlock;
+constexpr int kWord = 4;   // blocks whose scales share a 32-bit word
+
+__device__ __forceinline__ float4 load4(const float *p) { return gld4(p); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16 *p) {
+    const uint2 u = *reinterpret_cast<const uint2 *>(p);
+    return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                       __uint_as_float(u.y & 0xffff0000u));
+}
+
+// The bits of |x|, 0 for what is not finite.
+__device__ __forceinline__ unsigned magnitude(float x) {
+    const unsigned b = __float_as_uint(x) & 0x7fffffffu;
+    return b < 0x7f800000u ? b : 0u;
+}
+__device__ __forceinline__ unsigned magnitude(const float4 &v) {
+    return max(max(magnitude(v.x), magnitude(v.y)), max(magnitude(v.z), magnitude(v.w)));
+}
+
+// E of a block from the bits of its largest magnitude m * 2^k, 1 <= m < 2: k - 8 for m <= 1.75, else k - 7
+// (fp32's own subnormals end at the lower limit).
+__device__ __forceinline__ int block_exponent(unsigned top) {
+    if (top == 0u) return 0;
+    const int k = (int)(top >> 23) - 127;
+    return max((top & 0x7fffffu) > 0x600000u ? k - 7 : k - 8, -126);
+}
+__device__ __forceinline__ float exp2i(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }   // -126 <= e <= 127
+
+// Four values times 2^-E as e4m3, the first in the lowest byte.
+__device__ __forceinline__ unsigned round4(const float4 &v, float inv) {
+    const auto one = [&](float x) { return fabsf(x) <= 3.402823466e38f ? x * inv : __uint_as_float(0x7fffffffu); };
+    const unsigned lo = __nv_cvt_float2_to_fp8x2(make_float2(one(v.x), one(v.y)), __NV_SATFINITE, __NV_E4M3);
+    const unsigned hi = __nv_cvt_float2_to_fp8x2(make_float2(one(v.z), one(v.w)), __NV_SATFINITE, __NV_E4M3);
+    return lo | hi << 16;
+}
+
+__device__ __forceinline__ unsigned warp_max(unsigned v) { return __reduce_max_sync(kFull, v); }
+
+// residual[row] += add[row] (when given); q, scales = the 8-bit form of residual[row] * w / sqrt(mean residual[row]^2 + eps).
+// One CTA per row: warp i takes the words (four blocks) i, i + warps, ..., or single blocks with kPer = 1 (few rows:
+// latency counts, and a row spread over four times the warps is there sooner). The first kPer blocks of a warp stay in
+// registers between the sum of squares and the rounding; wider rows are read again.
+template <typename T, int kPer>
+__global__ void __launch_bounds__(1024) rmsnorm_q8_kernel(const T *add, float *residual, const float *w, float eps,
+                                                          uint8_t *q, uint8_t *scales, int width, int stride, bool early) {
+    __shared__ float red[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int64_t row = blockIdx.x;
+    float *r = residual + row * width;
+    const T *a = add ? add + row * width : nullptr;
+    const int step = warps * kPer;
+    float4 kept[kPer];
+    float ss = 0.f;
+    if (early) pdl_trigger();
+    pdl_wait();
+    for (int b0 = warp * kPer; b0 < stride; b0 += step) {
+        float4 v[kPer], d[kPer];
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const int c = (b0 + j) * kBlock + 4 * lane;
+            v[j] = c < width ? load4(r + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+            if (a && c < width) d[j] = load4(a + c);
+        }
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const int c = (b0 + j) * kBlock + 4 * lane;
+            if (a && c < width) {
+                v[j].x += d[j].x; v[j].y += d[j].y; v[j].z += d[j].z; v[j].w += d[j].w;
+                *reinterpret_cast<float4 *>(r + c) = v[j];
+            }
+            ss = fmaf(v[j].x, v[j].x, fmaf(v[j].y, v[j].y, fmaf(v[j].z, v[j].z, fmaf(v[j].w, v[j].w, ss))));
+            if (b0 < step) kept[j] = v[j];
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(kFull, ss, o);
+    if (lane == 0) red[warp] = ss;
+    __syncthreads();
+    float total = 0.f;
+    for (int i = 0; i < warps; ++i) total += red[i];
+    const float rstd = rsqrtf(total / (float)width + eps);
+    for (int b0 = warp * kPer; b0 < stride; b0 += step) {
+        unsigned word = 0;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const int c = (b0 + j) * kBlock + 4 * lane;
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (c < width) {
+                const float4 v = b0 < step ? kept[j] : load4(r + c), g = load4(w + c);
+                y = make_float4(v.x * rstd * g.x, v.y * rstd * g.y, v.z * rstd * g.z, v.w * rstd * g.w);
+            }
+            const int e = block_exponent(warp_max(magnitude(y)));
+            if (c < width) *reinterpret_cast<unsigned *>(q + row * width + c) = round4(y, exp2i(-e));
+            word |= (unsigned)(e + 127) << (8 * j);
+        }
+        if (lane == 0) {
+            if (kPer == kWord) *reinterpret_cast<unsigned *>(scales + row * stride + b0) = word;
+            else scales[row * stride + b0] = (uint8_t)word;
+        }
+    }
+}
+
+constexpr int kQuantThreads = 256;
+
+// Rows of x, a warp to a word of scales (512 columns).
+template <typename T>
+__global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const T *x, int64_t x_stride, uint8_t *q, uint8_t *scales,
+                                                                     int64_t rows, int width, int stride, bool early) {
+    const int lane = threadIdx.x & 31, words = stride / kWord;
+    const int64_t task = (int64_t)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
+    if (early) pdl_trigger();
+    pdl_wait();
+    if (task >= rows * words) return;
+    const int64_t row = task / words;
+    const int b0 = (int)(task - row * words) * kWord;
+    float4 v[kWord];
+#pragma unroll
+    for (int j = 0; j < kWord; ++j) {
+        const int c = (b0 + j) * kBlock + 4 * lane;
+        v[j] = c < width ? load4(x + row * x_stride + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    unsigned word = 0;
+#pragma unroll
+    for (int j = 0; j < kWord; ++j) {
+        const int c = (b0 + j) * kBlock + 4 * lane;
+        const int e = block_exponent(warp_max(magnitude(v[j])));
+        if (c < width) *reinterpret_cast<unsigned *>(q + row * width + c) = round4(v[j], exp2i(-e));
+        word |= (unsigned)(e + 127) << (8 * j);
+    }
+    if (lane == 0) *reinterpret_cast<unsigned *>(scales + row * stride + b0) = word;
+}
+
+// 128 x 128 blocks, one CTA each; it keeps its 64 values a thread in registers until the block's maximum is known. There is
+// a CTA for every byte of a row of scales: the bytes behind the last block become those of blocks of zeros.
+template <typename T>
+__global__ void __launch_bounds__(kQuantThreads) quantize_blocks_kernel(const T *x, int64_t x_stride, uint8_t *q, uint8_t *scales,
+                                                                       int64_t rows, int width, int stride) {
+    constexpr int kWarps = kQuantThreads / 32, kRows = kBlock / kWarps;
+    __shared__ unsigned red[kWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t down = blockIdx.x / stride, row0 = down * kBlock;
+    const int across = (int)(blockIdx.x - down * stride), c = across * kBlock + 4 * lane;
+    pdl_wait();
+    float4 v[kRows];
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int64_t row = row0 + i * kWarps + warp;
+        v[i] = row < rows && c < width ? load4(x + row * x_stride + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) top = max(top, magnitude(v[i]));
+    top = warp_max(top);
+    if (lane == 0) red[warp] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) top = max(top, red[i]);
+    const int e = block_exponent(top);
+    const float inv = exp2i(-e);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int64_t row = row0 + i * kWarps + warp;
+        if (row < rows && c < width) *reinterpret_cast<unsigned *>(q + row * width + c) = round4(v[i], inv);
+    }
+    if (threadIdx.x == 0) scales[blockIdx.x] = (uint8_t)(e + 127);
+}
+
+// The values that q and its scales stand for, 16 columns a thread.
+template <typename T>
+__global__ void __launch_bounds__(kQuantThreads) dequantize_kernel(const uint8_t *q, const uint8_t *scales, int shift, T *out,
+                                                                  int64_t rows, int width, int stride, bool early) {
+    const int groups = width / 16;
+    const int64_t i = (int64_t)blockIdx.x * kQuantThreads + threadIdx.x;
+    if (early) pdl_trigger();
+    pdl_wait();
+    if (i >= rows * groups) return;
+    const int64_t row = i / groups;
+    const int c = (int)(i - row * groups) * 16;
+    const uint4 u = ld16(q + row * width + c);
+    const unsigned s = scales[(row >> shift) * stride + c / kBlock];
+    // 2^(s - 127) in two factors: byte 0 is 2^-127, and 255 no number
+    const float f = s == 255u ? __uint_as_float(0x7fffffffu) : s == 0u ? __uint_as_float(1u << 22) : __uint_as_float(s << 23);
+    const unsigned word[4] = {u.x, u.y, u.z, u.w};
+    float v[16];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const __nv_fp8x2_storage_t two = (__nv_fp8x2_storage_t)(word[j / 2] >> (16 * (j & 1)));
+        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(two, __NV_E4M3);   // exact
+        const float2 p = __half22float2(__half2(h));
+        v[2 * j] = p.x * f;
+        v[2 * j + 1] = p.y * f;
+    }
+    T *o = out + row * width + c;
+#pragma unroll
+    for (int j = 0; j < 16; j += kVec<T>) {
+        float g[kVec<T>];
+#pragma unroll
+        for (int k = 0; k < kVec<T>; ++k) g[k] = v[j + k];
+        st16(o + j, g);
+    }
+}
+
+// Whether a grid leaves room for the next kernel's CTAs (see pdl_trigger's comment).
+bool leaves_room(int64_t ctas) { return ctas <= 2 * (int64_t)device_sms(); }
+
+unsigned ctas(int64_t n) { return (unsigned)((n + kQuantThreads - 1) / kQuantThreads); }
+
+template <typename T>
+cudaError_t norm(const void *add, float *residual, const float *w, float eps, uint8_t *q, uint8_t *scales, int64_t rows,
+                 int width, cudaStream_t s) {
+    const int stride = (int)quant_stride(width);
+    const bool few = rows <= 4 * (int64_t)device_sms();
+    const int warps = few ? (stride < 32 ? stride : 32) : (stride / kWord < 32 ? stride / kWord : 32);
+    return launch_pdl(true, few ? rmsnorm_q8_kernel<T, 1> : rmsnorm_q8_kernel<T, kWord>, dim3((unsigned)rows),
+                      dim3(32 * warps), 0, s, static_cast<const T *>(add), residual, w, eps, q, scales, width, stride,
+                      leaves_room(rows));
+}
+
+template <typename T>
+cudaError_t quantize(const void *x, int64_t x_stride, bool blocks, uint8_t *q, uint8_t *scales, int64_t rows, int width,
+                     cudaStream_t s) {
+    const int stride = (int)quant_stride(width);
+    if (!blocks) {
+        const int64_t tasks = rows * (stride / kWord);
+        return launch_pdl(true, quantize_rows_kernel<T>, dim3(ctas(tasks * 32)), dim3(kQuantThreads), 0, s,
+                          static_cast<const T *>(x), x_stride, q, scales, rows, width, stride,
+                          leaves_room(ctas(tasks * 32)));
+    }
+    const int64_t down = (rows + kBlock - 1) / kBlock;
+    return launch_pdl(true, quantize_blocks_kernel<T>, dim3((unsigned)(down * stride)), dim3(kQuantThreads), 0, s,
+                      static_cast<const T *>(x), x_stride, q, scales, rows, width, stride);
+}
+
+}  // namespace
+
+cudaError_t launch_rmsnorm_q8(const void *add, bool bf16, float *residual, const float *w, float eps, uint8_t *q,
+                              uint8_t *scales, int64_t rows, int64_t width, cudaStream_t s) {
+    return bf16 ? norm<__nv_bfloat16>(add, residual, w, eps, q, scales, rows, (int)width, s)
+                : norm<float>(add, residual, w, eps, q, scales, rows, (int)width, s);
+}
+
+cudaError_t launch_quantize(const void *x, bool bf16, int64_t x_stride, bool blocks, uint8_t *q, uint8_t *scales, int64_t rows,
+                            int64_t width, cudaStream_t s) {
+    return bf16 ? quantize<__nv_bfloat16>(x, x_stride, blocks, q, scales, rows, (int)width, s)
+                : quantize<float>(x, x_stride, blocks, q, scales, rows, (int)width, s);
+}
+
+cudaError_t launch_dequantize(const uint8_t *q, const uint8_t *scales, bool blocks, void *out, bool bf16, int64_t rows,
+                              int64_t width, cudaStream_t s) {
+    const int stride = (int)quant_stride(width), shift = blocks ? 7 : 0;
+    const dim3 grid(ctas(rows * (width / 16))), block(kQuantThreads);
+    const bool early = leaves_room(grid.x);
+    if (bf16)
+        return launch_pdl(true, dequantize_kernel<__nv_bfloat16>, grid, block, 0, s, q, scales, shift,
+                          static_cast<__nv_bfloat16 *>(out), rows, (int)width, stride, early);
+    return launch_pdl(true, dequantize_kernel<float>, grid, block, 0, s, q, scales, shift, static_cast<float *>(out), rows,
+                      (int)width, stride, early);
+}
+
+}  // namespace mbscan

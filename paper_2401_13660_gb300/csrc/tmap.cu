@@ -45,8 +45,9 @@ bool encode_tmap(CUtensorMap *m, const void *base, int elem_bytes, int rank, con
         es[i] = 1;
         if (i + 1 < rank) st[i] = strides[i];
     }
-    const CUtensorMapDataType dt = elem_bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
-                                                   : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+    const CUtensorMapDataType dt = elem_bytes == 1   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                   : elem_bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                     : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
     return enc(m, dt, (cuuint32_t)rank, const_cast<void *>(base), d, st, bx, es,
                CU_TENSOR_MAP_INTERLEAVE_NONE,
                swizzle == 128 ? CU_TENSOR_MAP_SWIZZLE_128B

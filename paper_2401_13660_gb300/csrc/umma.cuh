@@ -1,0 +1,84 @@
+// Thin wrappers over the sm_100 tensor-core instructions (tcgen05): matrix
+// products of operands in shared memory into tensor memory, with block scales
+// in tensor memory, and what moves scales and sums there and back. A tensor
+// memory address holds the lane in its upper 16 bits and the 32-bit column in
+// the lower ones.
+#pragma once
+
+#include "tma.cuh"
+
+namespace mbscan {
+
+// Columns are allocated by one warp, 32 to 512 at a time (a power of two), and freed by it.
+__device__ __forceinline__ void tmem_alloc(uint32_t *address, uint32_t columns) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(address)), "r"(columns)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_free(uint32_t address, uint32_t columns) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(address), "r"(columns));
+}
+
+// Order of this thread's tcgen05 operations against those of threads it synchronises with (before, after that).
+__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// Arrive on `bar` once every product and copy that this thread has issued is done.
+__device__ __forceinline__ void umma_commit(uint64_t *bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
+// Descriptor of an operand in shared memory whose rows are 128 bytes of the sum's dimension, swizzled as a
+// CU_TENSOR_MAP_SWIZZLE_128B copy leaves them (1024-byte aligned; groups of 8 rows 1024 bytes apart). The 32-byte column
+// block k of it starts 2 k further.
+__device__ __forceinline__ uint64_t umma_desc_128(uint32_t smem) {
+    return (uint64_t)((smem & 0x3ffffu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// The same of 32 rows of 16 bytes, one after the other.
+__device__ __forceinline__ uint64_t umma_desc_rows16(uint32_t smem) {
+    return (uint64_t)((smem & 0x3ffffu) >> 4) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+}
+
+// Copy 32 rows of 16 bytes to four columns of tensor memory, row l to lane l of each of the four quarters of the lanes.
+// In order with this thread's products.
+__device__ __forceinline__ void tmem_copy_scales(uint32_t column, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(column), "l"(desc) : "memory");
+}
+
+// Instruction word of a product of e4m3 operands, both with the sum's dimension innermost, m x n, with e8m0 scales. The
+// scales of a row of an operand are the four bytes of a 32-bit word; `scale` of them is taken for both operands.
+__device__ __forceinline__ uint32_t umma_word_q8(uint32_t m, uint32_t n, uint32_t scale) {
+    return scale << 4 | (n >> 3) << 17 | 1u << 23 | (m >> 4) << 24 | scale << 29;
+}
+
+// d (+)= (A sA)(B sB)^T over 32 columns of the sum: row i of A is lane i, row j of B column j of d. Scales of row r are in
+// lane r % 32 (of every quarter) of column r / 32. Issued by one thread.
+__device__ __forceinline__ void umma_q8(uint32_t d, uint64_t a, uint64_t b, uint32_t word, uint32_t a_scales, uint32_t b_scales,
+                                        bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(word), "r"(a_scales), "r"(b_scales), "r"((uint32_t)add)
+        : "memory");
+}
+
+// 16 columns of this warp's quarter of the lanes (the address's lane: 32 * (warp % 4)); wait before they are used.
+__device__ __forceinline__ void tmem_load16(uint32_t address, uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(address)
+        : "memory");
+}
+// Names the registers it waits for, so that no use of them moves in front.
+__device__ __forceinline__ void tmem_load_wait(uint32_t (&v)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]),
+                   "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+                 :
+                 : "memory");
+}
+
+}  // namespace mbscan

@@ -33,7 +33,8 @@ _fast = None   # csrc/binding.cpp, loaded with the library
 _FAST = ("mb_scan_prefill", "mb_scan_verify", "mb_scan_verify_resume", "mb_scan_prefill_ckpt", "mb_step",
          "mb_step_resume", "mb_rollback", "mb_accept_topk", "mb_rmsnorm", "mb_conv1d_step", "mb_conv_xproj",
          "mb_conv1d", "mb_conv1d_backward", "mb_embed", "mb_embed_backward", "mb_cross_entropy",
-         "mb_grad_norm", "mb_grad_clip")
+         "mb_grad_norm", "mb_grad_clip", "mb_rmsnorm_q8", "mb_quantize_q8", "mb_dequantize_q8", "mb_matmul_q8",
+         "mb_sample")
 
 MB_OK, MB_ERR_INVALID_ARG, MB_ERR_UNSUPPORTED, MB_ERR_CUDA, MB_ERR_TIMEOUT = range(5)
 MB_F32, MB_BF16 = 0, 1
@@ -157,11 +158,19 @@ def load_library(build_if_needed: bool = True) -> ctypes.CDLL:
             tp = ctypes.POINTER(mb_tensor)
             lib.mb_grad_norm.argtypes = [tp, i64, vp, vp, sz, vp]
             lib.mb_grad_clip.argtypes = [tp, tp, i64, vp, f32, vp]
+            lib.mb_q8_scale_stride.argtypes = [i64]
+            lib.mb_q8_scale_stride.restype = i64
+            lib.mb_rmsnorm_q8.argtypes = [vp, i32, vp, vp, f32, vp, vp, i64, i64, vp]
+            lib.mb_quantize_q8.argtypes = [vp, i32, i64, i32, vp, vp, i64, i64, vp]
+            lib.mb_dequantize_q8.argtypes = [vp, vp, i32, vp, i32, i64, i64, vp]
+            lib.mb_matmul_q8.argtypes = [vp, vp, vp, vp, vp, i32, i64, i64, i64, i64, vp, sz, vp]
+            lib.mb_sample.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, i32, vp, i64, i64, vp]
             for f in ("mb_scan_prefill", "mb_scan_verify", "mb_rollback", "mb_step", "mb_check",
                       "mb_accept_topk", "mb_step_resume", "mb_scan_prefill_ckpt", "mb_scan_backward",
                       "mb_rmsnorm", "mb_conv1d_step", "mb_selftest_timeout", "mb_scan_verify_resume",
                       "mb_conv_xproj", "mb_conv1d", "mb_conv1d_backward", "mb_embed", "mb_embed_backward",
-                      "mb_cross_entropy", "mb_grad_norm", "mb_grad_clip"):
+                      "mb_cross_entropy", "mb_grad_norm", "mb_grad_clip", "mb_rmsnorm_q8", "mb_quantize_q8",
+                      "mb_dequantize_q8", "mb_matmul_q8", "mb_sample"):
                 getattr(lib, f).restype = ctypes.c_int
             lib.mb_status_string.argtypes = [ctypes.c_int]
             lib.mb_status_string.restype = ctypes.c_char_p
@@ -840,6 +849,180 @@ def mb_grad_clip(tensors, norm, max_norm, *, out=None, stream=None):
                                      _stream(stream, norm.device))
     _check(rc, "mb_grad_clip")
     return tensors if out is None else out
+
+
+Q8_BLOCK = 128   # columns (and, of weights, rows) that share a scale of an 8-bit matrix
+
+
+def mb_q8_scale_stride(width: int) -> int:
+    """Bytes of scales of a row of an 8-bit matrix (0: width not accepted)."""
+    return int(load_library().mb_q8_scale_stride(width))
+
+
+def _here(dev):
+    """The new calls launch on a stream of the current device: their tensors are there."""
+    if dev.type == "cuda" and dev.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _need_q8(q, scales, name, block_rows, dev=None):
+    """Checks an 8-bit matrix: q [rows, width] (torch.float8_e4m3fn, or uint8 holding it) and its scales."""
+    for n, t in ((name, q), (name + "_scales", scales)):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{n} must be a torch.Tensor")
+    if q.dtype not in (torch.float8_e4m3fn, torch.uint8):
+        raise TypeError(f"{name}: dtype {q.dtype}, expected torch.float8_e4m3fn or torch.uint8")
+    if q.dim() != 2:
+        raise ValueError(f"{name}: shape {tuple(q.shape)}, expected [rows, width]")
+    _need(q, name, None, None, dev)
+    rows, width = q.shape
+    if width % 16 == 0:   # else the library refuses
+        _need(scales, name + "_scales", torch.uint8, (-(-rows // block_rows), 4 * -(-width // (4 * Q8_BLOCK))), q.device)
+    return rows, width
+
+
+def _block_rows(block_rows):
+    if block_rows not in (1, Q8_BLOCK):
+        raise ValueError(f"block_rows {block_rows}, expected 1 or {Q8_BLOCK}")
+    return int(block_rows)
+
+
+def mb_rmsnorm_q8(residual, w, q, scales, *, add=None, eps=1e-5, stream=None):
+    """residual [rows, width] fp32 (+= add), then its RMS norm times w [width]
+    fp32 in 8 bits: q [rows, width] (torch.float8_e4m3fn, or uint8) and scales
+    [rows, mb_q8_scale_stride(width)] uint8, one for 128 columns. add [rows,
+    width] fp32 or bf16."""
+    if stream is None:
+        rc = (_fast or _native()).rmsnorm_q8(residual, w, q, scales, add, eps)
+        if rc >= 0:
+            _check(rc, "mb_rmsnorm_q8")
+            return q, scales
+    dev = residual.device
+    rows, width = _need_q8(q, scales, "q", 1, dev)
+    _need(residual, "residual", torch.float32, (rows, width), dev)
+    _need(w, "w", torch.float32, (width,), dev)
+    if add is not None and add.dtype not in _DTYPES:
+        raise TypeError(f"add: unsupported dtype {add.dtype}")
+    _need(add, "add", None, (rows, width), dev)
+    _here(dev)
+    dt = MB_BF16 if add is None else _DTYPES[add.dtype]
+    rc = load_library().mb_rmsnorm_q8(_ptr(add), dt, _ptr(residual), _ptr(w), float(eps), _ptr(q), _ptr(scales), rows, width,
+                                      _stream(stream, dev))
+    _check(rc, "mb_rmsnorm_q8")
+    return q, scales
+
+
+def mb_quantize_q8(x, q, scales, *, block_rows=1, stream=None):
+    """x [rows, width] fp32 or bf16 (contiguous or a column block of wider rows)
+    in 8 bits: q [rows, width] (torch.float8_e4m3fn, or uint8), scales
+    [ceil(rows / block_rows), mb_q8_scale_stride(width)] uint8, one for 128
+    columns of block_rows rows: 1 (activations) or 128 (weights)."""
+    if stream is None:
+        rc = (_fast or _native()).quantize_q8(x, q, scales, block_rows)
+        if rc >= 0:
+            _check(rc, "mb_quantize_q8")
+            return q, scales
+    block_rows = _block_rows(block_rows)
+    rows, width = _need_q8(q, scales, "q", block_rows)
+    dev = q.device
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("x must be a torch.Tensor")
+    if x.dtype not in _DTYPES:
+        raise TypeError(f"x: unsupported dtype {x.dtype}")
+    if tuple(x.shape) != (rows, width) or x.device != dev:
+        raise ValueError(f"x: {tuple(x.shape)} on {x.device}, expected {(rows, width)} on {dev}")
+    S = width if x.is_contiguous() or rows == 1 and x.stride(1) == 1 else x.stride(0)
+    if S != width and (x.stride(1) != 1 or S < width):
+        raise ValueError("x must be contiguous or a column block of wider rows")
+    _here(dev)
+    rc = load_library().mb_quantize_q8(_ptr(x), _DTYPES[x.dtype], S, block_rows, _ptr(q), _ptr(scales), rows, width,
+                                       _stream(stream, dev))
+    _check(rc, "mb_quantize_q8")
+    return q, scales
+
+
+def mb_dequantize_q8(q, scales, out, *, block_rows=1, stream=None):
+    """The values that q and scales stand for: out [rows, width] fp32 or bf16."""
+    if stream is None:
+        rc = (_fast or _native()).dequantize_q8(q, scales, out, block_rows)
+        if rc >= 0:
+            _check(rc, "mb_dequantize_q8")
+            return out
+    block_rows = _block_rows(block_rows)
+    rows, width = _need_q8(q, scales, "q", block_rows)
+    if out.dtype not in _DTYPES:
+        raise TypeError(f"out: unsupported dtype {out.dtype}")
+    _need(out, "out", None, (rows, width), q.device)
+    _here(q.device)
+    rc = load_library().mb_dequantize_q8(_ptr(q), _ptr(scales), block_rows, _ptr(out), _DTYPES[out.dtype], rows, width,
+                                         _stream(stream, q.device))
+    _check(rc, "mb_dequantize_q8")
+    return out
+
+
+def mb_matmul_q8(a, a_scales, w, w_scales, out, *, ws=None, stream=None):
+    """out = A W^T of 8-bit matrices: a [rows, width] with a_scales (block_rows
+    1), w [n_out, width] with w_scales (block_rows 128). out fp32 or bf16:
+    [rows, n_out], or [parts, rows, n_out / parts] for the product's columns in
+    that many groups. ws: a workspace of 256 bytes (a wait that timed out is
+    recorded there) or None."""
+    if stream is None:
+        rc = (_fast or _native()).matmul_q8(a, a_scales, w, w_scales, out, ws)
+        if rc >= 0:
+            _check(rc, "mb_matmul_q8")
+            return out
+    rows, width = _need_q8(a, a_scales, "a", 1)
+    dev = a.device
+    n_out, k = _need_q8(w, w_scales, "w", Q8_BLOCK, dev)
+    if k != width:
+        raise ValueError(f"w: rows of {k}, expected {width}")
+    if out.dtype not in _DTYPES:
+        raise TypeError(f"out: unsupported dtype {out.dtype}")
+    part = out.shape[-1]
+    parts = out.shape[0] if out.dim() == 3 else 1
+    _need(out, "out", None, (rows, n_out) if out.dim() == 2 else (parts, rows, part), dev)
+    if parts * part != n_out:
+        raise ValueError(f"out: {parts} groups of {part} columns, expected {n_out} in all")
+    _need(ws, "ws", torch.uint8, None, dev)
+    _here(dev)
+    rc = load_library().mb_matmul_q8(_ptr(a), _ptr(a_scales), _ptr(w), _ptr(w_scales), _ptr(out), _DTYPES[out.dtype], rows,
+                                     n_out, width, part, _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream, dev))
+    _check(rc, "mb_matmul_q8")
+    return out
+
+
+def mb_sample(logits, u, tokens=None, *, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, stream=None):
+    """Draw a token of every row of logits [n, vocab] (fp32 or bf16) by the
+    random numbers u [n] fp32 in [0, 1): temperature, then the top_k likeliest
+    tokens, of these the nucleus of mass top_p, of these those at least min_p
+    times as likely as the likeliest; each [n] (fp32; top_k int32) or None.
+    tokens [n] int32 or int64 (None: a new int64 tensor): -1 where every token
+    is masked (-inf). prob [n] fp32 (if given): what the token was drawn with."""
+    if tokens is not None and stream is None:
+        rc = (_fast or _native()).sample(logits, u, tokens, temperature, top_k, top_p, min_p, prob)
+        if rc >= 0:
+            _check(rc, "mb_sample")
+            return tokens
+    if logits.dtype not in _DTYPES:
+        raise TypeError(f"logits: unsupported dtype {logits.dtype}")
+    n, vocab = logits.shape
+    dev = logits.device
+    _need(logits, "logits")
+    if tokens is None:
+        tokens = torch.empty(n, dtype=torch.int64, device=dev)
+    if tokens.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"tokens: dtype {tokens.dtype}, expected torch.int32 or torch.int64")
+    _need(tokens, "tokens", None, (n,), dev)
+    for name, t, dtype in (("u", u, torch.float32), ("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32), ("prob", prob, torch.float32)):
+        _need(t, name, dtype, (n,), dev)
+    if u is None:
+        raise TypeError("u must be a torch.Tensor")
+    _here(dev)
+    rc = load_library().mb_sample(_ptr(logits), _DTYPES[logits.dtype], _ptr(u), _ptr(temperature), _ptr(top_k), _ptr(top_p),
+                                  _ptr(min_p), _ptr(tokens), _TOKENS[tokens.dtype], _ptr(prob), n, vocab, _stream(stream, dev))
+    _check(rc, "mb_sample")
+    return tokens
 
 
 def mb_selftest_timeout(ws, wait_cycles, stream=None):
