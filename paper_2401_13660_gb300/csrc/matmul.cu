@@ -269,20 +269,8 @@ cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t 
     auto kern = out_bf16 ? matmul_q8_kernel<__nv_bfloat16> : matmul_q8_kernel<float>;
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(lim->smem_optin - sizeof(Barriers) - 64));
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(t.split > 1 ? tiles * t.split : tiles < lim->sms ? tiles : lim->sms));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = MB_PDL;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)t.split;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = t.split > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kern, g);
+    const int64_t grid = t.split > 1 ? tiles * t.split : tiles < lim->sms ? tiles : lim->sms;
+    return launch_cluster(true, kern, dim3((unsigned)grid), dim3(kThreads), t.split, smem, s, g);
 }
 
 }  // namespace mbscan

@@ -10,12 +10,15 @@
 // and u are taken exactly. A weight itself is within 2^-32 of its value (weight()): a draw differs from that of exact
 // arithmetic where u falls that near to a border.
 //
-// Rows of up to 256 tokens (bytes): one warp, eight tokens a lane, sorted in registers. Longer rows: one CTA, which keeps
-// the row in shared memory, finds where top_k and top_p end by histograms of counts and masses over the distance to the
-// maximum, and sorts out the one bin that holds the end.
+// Rows of up to 256 tokens (bytes): one warp, eight tokens a lane, sorted in registers. Longer rows: a CTA, or a
+// cluster of them where rows are few, which keeps the row in shared memory, finds where top_k and top_p end by histograms of
+// counts and masses over the distance to the maximum, and sorts out the one bin that holds the end.
 #include "../../include/mbscan.h"
+#include "cluster.cuh"
 #include "common.cuh"
 #include "vec.cuh"
+
+#include <math.h>
 
 namespace mbscan {
 namespace {
@@ -290,296 +293,441 @@ __global__ void __launch_bounds__(256) sample_short_kernel(const __grid_constant
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048;          // of the distance to the maximum, kPerOctave to a factor of two
 constexpr float kPerOctave = 32.f;
-constexpr int kList = 1024;          // tokens that are ranked one against the other
+constexpr int kList = 512;           // tokens that are ranked one against the other
+constexpr int kMaxCtas = 8;          // of a row
 
 struct alignas(16) Shared {
     u64 powers[256];
-    u64 mass[kBins];
-    unsigned count[kBins];
-    u64 warp_mass[kWarps];
-    unsigned warp_count[kWarps];
-    unsigned list_key[kList];
-    int list_index[kList];
+    unsigned low[kBins], high[kBins];   // masses of the bins; counts in `low` alone
+    u64 warp[kWarps];
+    u64 slot[2][kMaxCtas];
     u64 list_weight[kList];
-    u64 found_mass;
-    unsigned found_count, length, last_key;
-    int found, last_index;
+    float list_logit[kList];
+    int list_index[kList];
+    u64 found_before;
+    int found, length, last_index;
+    float last;
 };
 
-// A row's logits: where they are, and the tokens that are left of it, those of (key, index) not behind the last one.
-template <typename T> struct Row {
-    const T *l;
-    int vocab;
-    unsigned last_key = kMasked + 1;
-    int last_index = 0x7fffffff;
-    __device__ __forceinline__ unsigned key(int i) const { return key_of(clean<T>(to_f32(l[i]))); }
-    __device__ __forceinline__ bool in(unsigned k, int i) const { return k > last_key || (k == last_key && i <= last_index); }
-};
+// The CTAs of a row: one, or a cluster whose CTAs hold consecutive parts of it.
+template <bool kCluster> struct Team {
+    Shared &sh;
+    int rank, size, phase = 0;
 
-__device__ __forceinline__ void add64(u64 *p, u64 v) { atomicAdd(p, v); }
-
-// Prefix sums of the histogram's first `bins` (a multiple of kThreads, or fewer) by every thread of the CTA: finds the bin
-// in which the running sum of counts (of masses) reaches `goal`, the sum before it and what it holds.
-template <bool kMass> __device__ void find_bin(Shared &sh, int bins, u64 goal) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, each = (bins + kThreads - 1) / kThreads;
-    u64 mine = 0;
-    __syncthreads();
-    for (int j = 0; j < each; ++j) {
-        const int b = threadIdx.x * each + j;
-        if (b < bins) mine += kMass ? sh.mass[b] : sh.count[b];
+    __device__ __forceinline__ void sync() const {
+        if (kCluster) {
+            cluster_arrive();
+            cluster_wait();
+        } else {
+            __syncthreads();
+        }
     }
-    u64 before = warp_before(mine, lane);
-    if (lane == 31) sh.warp_mass[warp] = before + mine;
-    __syncthreads();
-    for (int i = 0; i < warp; ++i) before += sh.warp_mass[i];
-    if (before < goal && before + mine >= goal)
-        for (int j = 0; j < each; ++j) {
+    // Sum over the CTA.
+    __device__ u64 block_sum(u64 v) const {
+        v = warp_sum(v);
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) sh.warp[threadIdx.x >> 5] = v;
+        __syncthreads();
+        u64 s = 0;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) s += sh.warp[i];
+        return s;
+    }
+    // One number of each CTA, known to all its threads, to every CTA. Two sets of slots take turns: a CTA that is at the
+    // next exchange but one has seen every other leave this one.
+    __device__ const u64 *exchange(u64 mine) {
+        u64 *const slot = sh.slot[phase];
+        phase ^= 1;
+        if (kCluster) {
+            if ((int)threadIdx.x < size)
+                asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_address(&slot[rank], threadIdx.x)), "l"(mine) : "memory");
+        } else if (threadIdx.x == 0) {
+            slot[0] = mine;
+        }
+        sync();
+        return slot;
+    }
+    __device__ u64 sum(u64 mine, u64 &before) {   // over the CTAs, and over those before
+        const u64 *slot = exchange(mine);
+        u64 s = 0;
+        before = 0;
+        for (int i = 0; i < size; ++i) {
+            if (i == rank) before = s;
+            s += slot[i];
+        }
+        return s;
+    }
+    __device__ __forceinline__ unsigned peek(const unsigned *p, int cta) const {
+        return kCluster ? (unsigned)cluster_load(reinterpret_cast<const int *>(p), cta) : *p;
+    }
+    __device__ __forceinline__ void tell(u64 *p, u64 v) const {   // the same place of every CTA, by one thread
+        for (int i = 0; i < size; ++i)
+            if (kCluster) asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_address(p, i)), "l"(v) : "memory");
+            else *p = v;
+    }
+    __device__ __forceinline__ void tell(int *p, int v) const {
+        for (int i = 0; i < size; ++i)
+            if (kCluster) asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(cluster_address(p, i)), "r"(v) : "memory");
+            else *p = v;
+    }
+
+    // The bin in which the running sum of the histogram's masses (counts) reaches `goal`, and the sum before it: found,
+    // found_before. Every CTA has filled its own `bins` bins; each adds up an equal share of them over all CTAs.
+    template <bool kMass> __device__ void find_bin(int bins, u64 goal) {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        const int share = bins / size, each = (share + kThreads - 1) / kThreads;   // at most 4
+        sync();
+        u64 v[kBins / kThreads], mine = 0;
+#pragma unroll
+        for (int j = 0; j < kBins / kThreads; ++j) {
             const int b = threadIdx.x * each + j;
-            const u64 v = b < bins ? (kMass ? sh.mass[b] : sh.count[b]) : 0;
-            if (before < goal && before + v >= goal) {
-                sh.found = b;
-                sh.found_mass = before;
-                sh.found_count = sh.count[b];
+            v[j] = 0;
+            if (j < each && b < share)
+                for (int i = 0; i < size; ++i) {
+                    v[j] += peek(&sh.low[rank * share + b], i);
+                    if (kMass) v[j] += (u64)peek(&sh.high[rank * share + b], i) << 32;
+                }
+            mine += v[j];
+        }
+        u64 before = warp_before(mine, lane);
+        if (lane == 31) sh.warp[warp] = before + mine;
+        __syncthreads();
+        u64 all = 0;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) {
+            if (i < warp) before += sh.warp[i];
+            all += sh.warp[i];
+        }
+        u64 ahead;
+        sum(all, ahead);
+        before += ahead;
+        if (before < goal && before + mine >= goal) {
+#pragma unroll
+            for (int j = 0; j < kBins / kThreads; ++j) {
+                if (before < goal && before + v[j] >= goal) {
+                    tell(&sh.found, rank * share + (int)threadIdx.x * each + j);
+                    tell(&sh.found_before, before);
+                }
+                before += v[j];
             }
-            before += v;
         }
+        sync();
+    }
+};
+
+// The logits of this CTA's part of a row, in 16-byte groups as they lie in memory: in shared memory as they count, or
+// where they are (rows that do not fit). What a group holds beyond the row is masked.
+template <typename T> struct Row {
+    static constexpr int kPer = kVec<T>;
+    const uint4 *groups;   // null: read from global memory
+    const T *l;
+    int vocab, offset;     // the first group starts `offset` elements before the row
+    int g0, g1;            // this CTA's groups
+    // the tokens that are left: those not behind the last one
+    float last = -INFINITY;
+    int last_index = -1;
+
+    __device__ __forceinline__ int index(int g) const { return g * kPer - offset; }
+    __device__ __forceinline__ void load(int g, float (&f)[kPer]) const {
+        if (groups) {
+            widen(groups[g - g0], f);
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const int i = index(g) + j;
+            f[j] = i >= 0 && i < vocab ? clean<T>(to_f32(l[i])) : __uint_as_float(0xff800000u);
+        }
+    }
+    __device__ __forceinline__ bool in(float v, int i) const { return v > last || (v == last && i <= last_index); }
+    template <typename F> __device__ __forceinline__ void each(F &&f) const {   // f(logit, index) of what is left
+        for (int g = g0 + threadIdx.x; g < g1; g += kThreads) {
+            float v[kPer];
+            load(g, v);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (in(v[j], index(g) + j)) f(v[j], index(g) + j);
+        }
+    }
+};
+
+__device__ __forceinline__ void add_mass(Shared &sh, int b, u64 w) {   // 64 bits by two atomics of 32
+    const unsigned lo = (unsigned)w;
+    const unsigned was = atomicAdd(&sh.low[b], lo);
+    const unsigned hi = (unsigned)(w >> 32) + (was + lo < was ? 1u : 0u);
+    if (hi) atomicAdd(&sh.high[b], hi);
+}
+template <bool kMass> __device__ __forceinline__ void clear_bins(Shared &sh, int bins) {
+    for (int b = threadIdx.x; b < bins; b += kThreads) {
+        sh.low[b] = 0;
+        if (kMass) sh.high[b] = 0;
+    }
     __syncthreads();
 }
-
-// Sum over the CTA.
-__device__ u64 block_sum(Shared &sh, u64 v) {
-    v = warp_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) sh.warp_mass[threadIdx.x >> 5] = v;
-    __syncthreads();
-    u64 s = 0;
-    for (int i = 0; i < kWarps; ++i) s += sh.warp_mass[i];
-    return s;
+__device__ __forceinline__ int bin_of(const Scale &sc, float l) {
+    return (int)fminf(distance(sc, l) * kPerOctave, (float)(kBins - 1));
 }
 
-// The last token that stays where tokens stay as long as the sum of counts (kMass: of masses) before them is below `goal`.
-// The histograms are of the row's tokens that are left by now; their sum reaches the goal. Narrows the row.
-template <bool kMass, typename T>
-__device__ void cut(Shared &sh, Row<T> &row, const Scale &sc, u64 goal) {
-    find_bin<kMass>(sh, kBins, goal);
+// Narrows the row to the tokens before which the sum of masses (counts) is below the goal: `goal_of` the sum over all that
+// are left by now. Nothing changes where the sum does not reach the goal.
+template <bool kMass, bool kCluster, typename T, typename G>
+__device__ void cut(Team<kCluster> &team, Row<T> &row, const Scale &sc, G &&goal_of) {
+    Shared &sh = team.sh;
+    clear_bins<kMass>(sh, kBins);
+    u64 sum = 0;
+    row.each([&](float l, int) {
+        const int b = bin_of(sc, l);
+        if (kMass) {
+            const u64 w = weight(sc, l, sh.powers);
+            if (w) add_mass(sh, b, w);
+            sum += w;
+        } else {
+            atomicAdd(&sh.low[b], 1u);
+            ++sum;
+        }
+    });
+    u64 before;
+    const u64 total = team.sum(team.block_sum(sum), before), goal = goal_of(total);
+    if (total < goal) return;
+    team.template find_bin<kMass>(kBins, goal);
     const int bin = sh.found;
-    u64 before = sh.found_mass;
-    unsigned size = sh.found_count;
-    const auto bin_of = [&](unsigned k) { return (int)fminf(distance(sc, of_key(k)) * kPerOctave, (float)(kBins - 1)); };
+    before = sh.found_before;
     unsigned prefix = 0, known = 0;   // bits of the key that the tokens looked at share
-    // as long as they are many: by the next eight bits
-    while (size > kList && known != 0xffffffffu) {
+    const auto looked_at = [&](float l) { return bin_of(sc, l) == bin && (key_of(l) & known) == prefix; };
+    for (;;) {
+        // the tokens in question, to the first CTA
+        if (threadIdx.x == 0) sh.length = 0;
+        team.sync();
+        row.each([&](float l, int i) {
+            if (!looked_at(l)) return;
+            int at;
+            if (kCluster) {
+                asm volatile("atom.shared::cluster.add.s32 %0, [%1], 1;" : "=r"(at) : "r"(cluster_address(&sh.length, 0)) : "memory");
+                if (at >= kList) return;
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_address(&sh.list_logit[at], 0)), "f"(l) : "memory");
+                asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(cluster_address(&sh.list_index[at], 0)), "r"(i) : "memory");
+            } else {
+                at = atomicAdd(&sh.length, 1);
+                if (at >= kList) return;
+                sh.list_logit[at] = l;
+                sh.list_index[at] = i;
+            }
+        });
+        team.sync();
+        const int size = (int)team.peek(reinterpret_cast<const unsigned *>(&sh.length), 0);
+        if (size <= kList) {
+            // each against all others; the last that stays is the one at which the sum reaches the goal
+            if (team.rank == 0) {
+                if (kMass) {
+                    if ((int)threadIdx.x < size) sh.list_weight[threadIdx.x] = weight(sc, sh.list_logit[threadIdx.x], sh.powers);
+                    __syncthreads();
+                }
+                if ((int)threadIdx.x < size) {
+                    const float l = sh.list_logit[threadIdx.x];
+                    const int at = sh.list_index[threadIdx.x];
+                    u64 mine = before;
+#pragma unroll 4
+                    for (int j = 0; j < size; ++j) {
+                        const float o = sh.list_logit[j];
+                        if (o > l || (o == l && sh.list_index[j] < at)) mine += kMass ? sh.list_weight[j] : 1;
+                    }
+                    const u64 w = kMass ? sh.list_weight[threadIdx.x] : 1;
+                    if (mine < goal && mine + w >= goal) {
+                        team.tell(reinterpret_cast<int *>(&sh.last), __float_as_int(l));
+                        team.tell(&sh.last_index, at);
+                    }
+                }
+            }
+            break;
+        }
+        if (known == 0xffffffffu) {   // all the same: the first of them by index
+            const float l = of_key(prefix);
+            const u64 w = kMass ? weight(sc, l, sh.powers) : 1;
+            const u64 want = (goal - before + w - 1) / w;   // w > 0: the sum reaches the goal among them
+            u64 n = 0, ahead;
+            row.each([&](float o, int) { n += o == l; });
+            n = team.block_sum(n);
+            team.sum(n, ahead);
+            // the group that holds it by its order: a stretch of groups to a thread
+            if (ahead < want && ahead + n >= want) {
+                const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+                const int stretch = (row.g1 - row.g0 + kThreads - 1) / kThreads, a = row.g0 + (int)threadIdx.x * stretch;
+                const int b = min(row.g1, a + stretch);
+                u64 mine = 0;
+                const auto walk = [&](auto &&found) {
+                    for (int g = a; g < b; ++g) {
+                        float v[Row<T>::kPer];
+                        row.load(g, v);
+#pragma unroll
+                        for (int j = 0; j < Row<T>::kPer; ++j)
+                            if (v[j] == l && row.in(v[j], row.index(g) + j)) found(row.index(g) + j);
+                    }
+                };
+                walk([&](int) { ++mine; });
+                u64 upto = warp_before(mine, lane);
+                if (lane == 31) sh.warp[warp] = upto + mine;
+                __syncthreads();
+                for (int i = 0; i < warp; ++i) upto += sh.warp[i];
+                upto += ahead;
+                if (upto < want && upto + mine >= want)
+                    walk([&](int i) {
+                        if (++upto == want) {
+                            team.tell(reinterpret_cast<int *>(&sh.last), __float_as_int(l));
+                            team.tell(&sh.last_index, i);
+                        }
+                    });
+            }
+            break;
+        }
+        // too many: those that share the next eight bits of the key
         const int shift = known == 0 ? 24 : known == 0xff000000u ? 16 : known == 0xffff0000u ? 8 : 0;
-        __syncthreads();
-        for (int b = threadIdx.x; b < 256; b += kThreads) {
-            sh.mass[b] = 0;
-            sh.count[b] = 0;
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < row.vocab; i += kThreads) {
-            const unsigned k = row.key(i);
-            if (!row.in(k, i) || (k & known) != prefix || bin_of(k) != bin) continue;
-            const unsigned b = 255u - (k >> shift & 255u);
-            atomicAdd(&sh.count[b], 1u);
-            if (kMass) add64(&sh.mass[b], weight(sc, of_key(k), sh.powers));
-        }
-        __syncthreads();
-        find_bin<kMass>(sh, 256, goal - before);
-        before += sh.found_mass;
-        size = sh.found_count;
+        clear_bins<kMass>(sh, 256);
+        row.each([&](float l, int) {
+            if (!looked_at(l)) return;
+            const int b = (int)(255u - (key_of(l) >> shift & 255u));
+            if (kMass) add_mass(sh, b, weight(sc, l, sh.powers));
+            else atomicAdd(&sh.low[b], 1u);
+        });
+        team.template find_bin<kMass>(256, goal - before);
+        before += sh.found_before;
         prefix |= (255u - (unsigned)sh.found) << shift;
         known |= 255u << shift;
     }
-    __syncthreads();
-    if (size > kList) {   // all the same: the first of them by index
-        const u64 w = kMass ? weight(sc, of_key(prefix), sh.powers) : 1;
-        const u64 want = w ? (goal - before + w - 1) / w : size;   // at least 1: the goal is not reached before
-        // a stretch of indexes to a warp, and the one that holds it token by token
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        const int stretch = (row.vocab + kThreads - 1) / kThreads * 32, i0 = warp * stretch, i1 = min(row.vocab, i0 + stretch);
-        unsigned n = 0;
-        for (int i = i0 + lane; i < i1; i += 32) {
-            const unsigned k = row.key(i);
-            n += k == prefix && row.in(k, i);
-        }
-        n = __reduce_add_sync(kFull, n);
-        if (lane == 0) sh.warp_count[warp] = n;
-        __syncthreads();
-        u64 at = 0;
-        for (int i = 0; i < warp; ++i) at += sh.warp_count[i];
-        if (at < want && at + n >= want)
-            for (int c = i0; c < i1; c += 32) {
-                const unsigned k = c + lane < i1 ? row.key(c + lane) : 0u;
-                const unsigned here = __ballot_sync(kFull, k == prefix && row.in(k, c + lane));
-                const u64 mine = at + __popc(here & (0xffffffffu >> (31 - lane)));
-                if (mine == want && (here >> lane & 1u)) {
-                    sh.last_key = prefix;
-                    sh.last_index = c + lane;
-                }
-                at += __popc(here);
-            }
-        __syncthreads();
-        row.last_key = sh.last_key;
-        row.last_index = sh.last_index;
-        return;
-    }
-    if (threadIdx.x == 0) sh.length = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < row.vocab; i += kThreads) {
-        const unsigned k = row.key(i);
-        if (!row.in(k, i) || (k & known) != prefix || bin_of(k) != bin) continue;
-        const unsigned at = atomicAdd(&sh.length, 1u);
-        sh.list_key[at] = k;
-        sh.list_index[at] = i;
-        if (kMass) sh.list_weight[at] = weight(sc, of_key(k), sh.powers);
-    }
-    __syncthreads();
-    // each against all others; the last that stays is the one at which the sum reaches the goal
-    for (unsigned i = threadIdx.x; i < size; i += kThreads) {
-        const unsigned k = sh.list_key[i];
-        const int at = sh.list_index[i];
-        u64 sum = before;
-        for (unsigned j = 0; j < size; ++j) {
-            const unsigned o = sh.list_key[j];
-            if (o > k || (o == k && sh.list_index[j] < at)) sum += kMass ? sh.list_weight[j] : 1;
-        }
-        const u64 w = kMass ? sh.list_weight[i] : 1;
-        if (sum < goal && sum + w >= goal) {
-            sh.last_key = k;
-            sh.last_index = at;
-        }
-    }
-    __syncthreads();
-    row.last_key = sh.last_key;
+    team.sync();
+    row.last = sh.last;
     row.last_index = sh.last_index;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) sample_long_kernel(const __grid_constant__ SampleParams a, int drop, bool keep, bool early) {
+template <typename T, bool kCluster>
+__global__ void __launch_bounds__(kThreads, 2) sample_long_kernel(const __grid_constant__ SampleParams a, int drop, bool keep, int ctas,
+                                                                  bool early) {
     extern __shared__ __align__(16) unsigned char dyn[];
     Shared &sh = *reinterpret_cast<Shared *>(dyn);
+    if (kCluster) cluster_arrive();   // everybody is there before the first exchange
+    constexpr int kPer = kVec<T>;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     for (int i = threadIdx.x; i < 256; i += kThreads) sh.powers[i] = kPowers.v[i];
     if (early) pdl_trigger();
     pdl_wait();
-    const int64_t r = blockIdx.x;
+    const int64_t r = blockIdx.x / (unsigned)ctas;
+    Team<kCluster> team{sh, (int)(blockIdx.x % (unsigned)ctas), ctas};
     Row<T> row;
     row.l = static_cast<const T *>(a.logits) + r * a.vocab;
     row.vocab = a.vocab;
-    // the row to shared memory, as it lies in its 16-byte groups
-    const T *src = row.l;
-    constexpr int kPer = kVec<T>;
-    const int head = (int)((16 - (reinterpret_cast<uintptr_t>(src) & 15)) & 15) / (int)sizeof(T);
-    const int h = min(head, a.vocab), groups = (a.vocab - h) / kPer, tail = h + groups * kPer;
-    T *copy = reinterpret_cast<T *>(dyn + sizeof(Shared)) + (kPer - head) % kPer;
-    unsigned top = 0;
-    const auto take = [&](int i) {
-        const T v = src[i];
-        if (keep) copy[i] = v;
-        top = max(top, key_of(clean<T>(to_f32(v))));
-    };
-    if ((int)threadIdx.x < h) take(threadIdx.x);
-    for (int i = tail + threadIdx.x; i < a.vocab; i += kThreads) take(i);
+    row.offset = (int)(reinterpret_cast<uintptr_t>(row.l) & 15) / (int)sizeof(T);
+    row.groups = nullptr;
+    const int groups = (row.offset + a.vocab + kPer - 1) / kPer;
+    row.g0 = (int)((int64_t)groups * team.rank / ctas);
+    row.g1 = (int)((int64_t)groups * (team.rank + 1) / ctas);
+    uint4 *const copy = reinterpret_cast<uint4 *>(dyn + sizeof(Shared));
+    float top = __uint_as_float(0xff800000u);
 #pragma unroll 4
-    for (int i = threadIdx.x; i < groups; i += kThreads) {
-        const uint4 u = ld16(src + h + i * kPer);
-        if (keep) *reinterpret_cast<uint4 *>(copy + h + i * kPer) = u;
+    for (int g = row.g0 + threadIdx.x; g < row.g1; g += kThreads) {
+        const int i = row.index(g);
         float f[kPer];
-        widen(u, f);
+        if (i >= 0 && i + kPer <= a.vocab) {
+            widen(ld16(row.l + i), f);
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) top = max(top, key_of(clean<T>(f[j])));
+            for (int j = 0; j < kPer; ++j) f[j] = clean<T>(f[j]);
+        } else {
+            row.load(g, f);
+        }
+        if (keep) copy[g - row.g0] = narrow(f);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) top = fmaxf(top, f[j]);
     }
-    if (keep) row.l = copy;
-    top = __reduce_max_sync(kFull, top);
-    if (lane == 0) sh.warp_count[warp] = top;
-    __syncthreads();
-    for (int i = 0; i < kWarps; ++i) top = max(top, sh.warp_count[i]);
-    if (top <= kMasked) {
-        if (threadIdx.x == 0) put(a, r, -1, 0, 1);
+    if (keep) row.groups = copy;
+    {
+        const unsigned k = __reduce_max_sync(kFull, key_of(top));
+        if (lane == 0) sh.warp[warp] = k;
+        __syncthreads();
+        u64 best = 0;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) best = max(best, sh.warp[i]);
+        if (kCluster) cluster_wait();
+        const u64 *slot = team.exchange(best);
+        for (int i = 0; i < ctas; ++i) best = max(best, slot[i]);
+        top = of_key((unsigned)best);
+    }
+    if (!(top > __uint_as_float(0xff800000u))) {
+        if (team.rank == 0 && threadIdx.x == 0) put(a, r, -1, 0, 1);
         return;
     }
     const Settings st = settings_of(a, r, drop);
-    const float m = of_key(top);
     if (st.greedy || st.k == 1) {
-        if (threadIdx.x == 0) sh.found = 0x7fffffff;
+        int at = 0x7fffffff;
+        row.each([&](float l, int i) { at = l == top ? min(at, i) : at; });
+        at = __reduce_min_sync(kFull, at);
         __syncthreads();
-        for (int i = threadIdx.x; i < row.vocab; i += kThreads)
-            if (row.key(i) == top) {
-                atomicMin(&sh.found, i);
-                break;
-            }
+        if (lane == 0) sh.warp[warp] = (u64)at;
         __syncthreads();
-        if (threadIdx.x == 0) put(a, r, sh.found, 1, 1);
+        u64 first = 0x7fffffff;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) first = min(first, sh.warp[i]);
+        const u64 *slot = team.exchange(first);
+        for (int i = 0; i < ctas; ++i) first = min(first, slot[i]);
+        if (team.rank == 0 && threadIdx.x == 0) put(a, r, (int)first, 1, 1);
         return;
     }
-    const Scale sc = make_scale(st.temperature, m, drop);
-    const auto histograms = [&](bool masses) {
-        __syncthreads();
-        for (int b = threadIdx.x; b < kBins; b += kThreads) {
-            sh.count[b] = 0;
-            sh.mass[b] = 0;
-        }
-        __syncthreads();
-        u64 sum = 0;
-        for (int i = threadIdx.x; i < row.vocab; i += kThreads) {
-            const unsigned k = row.key(i);
-            if (!row.in(k, i)) continue;
-            const float l = of_key(k);
-            const int b = (int)fminf(distance(sc, l) * kPerOctave, (float)(kBins - 1));
-            atomicAdd(&sh.count[b], 1u);
-            if (masses) {
-                const u64 w = weight(sc, l, sh.powers);
-                if (w) add64(&sh.mass[b], w);
-                sum += w;
-            }
-        }
-        return block_sum(sh, sum);
-    };
-    if (st.k) {
-        histograms(false);
-        u64 alive = 0;
-        for (int b = threadIdx.x; b < kBins; b += kThreads) alive += sh.count[b];
-        if (block_sum(sh, alive) > (u64)st.k) cut<false>(sh, row, sc, st.k);
-    }
-    if (st.nucleus) {
-        const u64 total = histograms(true);
-        cut<true>(sh, row, sc, nucleus_mass(st.p, total));
-    }
-    // the draw: a stretch of indexes to a warp; the one that holds the token again, a sixteenth to a warp; then by one warp
-    int i0 = 0, i1 = row.vocab;
-    u64 t = 0, total = 0;
-    const auto left = [&](int i) -> u64 {
-        const unsigned k = row.key(i);
-        if (!row.in(k, i)) return 0;
-        const u64 w = weight(sc, of_key(k), sh.powers);
+    const Scale sc = make_scale(st.temperature, top, drop);
+    if (st.k) cut<false>(team, row, sc, [&](u64) { return (u64)st.k; });
+    if (st.nucleus) cut<true>(team, row, sc, [&](u64 total) { return nucleus_mass(st.p, total); });
+    // the draw: the CTA, then the warp that holds the token (by a stretch of groups each), then by groups of 32 lanes
+    const auto left = [&](float l, int i) -> u64 {
+        if (!row.in(l, i)) return 0;
+        const u64 w = weight(sc, l, sh.powers);
         return w >= st.least ? w : 0;
     };
+    int g0 = row.g0, g1 = row.g1;
+    u64 t = 0, total = 0;
     for (int level = 0; level < 2; ++level) {
-        const int stretch = ((i1 - i0 + kThreads - 1) / kThreads) * 32, b0 = i0 + warp * stretch, b1 = min(i1, b0 + stretch);
+        const int stretch = (g1 - g0 + kThreads - 1) / kThreads * 32, b0 = g0 + warp * stretch, b1 = min(g1, b0 + stretch);
         u64 sum = 0;
-        for (int i = b0 + lane; i < b1; i += 32) sum += left(i);
+        for (int g = b0 + lane; g < b1; g += 32) {
+            float v[kPer];
+            row.load(g, v);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) sum += left(v[j], row.index(g) + j);
+        }
         sum = warp_sum(sum);
         __syncthreads();
-        if (lane == 0) sh.warp_mass[warp] = sum;
+        if (lane == 0) sh.warp[warp] = sum;
         __syncthreads();
         if (level == 0) {
-            for (int i = 0; i < kWarps; ++i) total += sh.warp_mass[i];
+            u64 mine = 0, before;
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) mine += sh.warp[i];
+            total = team.sum(mine, before);
             t = __umul64hi(st.u, total);
+            if (t < before || t >= before + mine) return;   // another CTA's
+            t -= before;
         }
         int at = 0;
-        for (; at < kWarps - 1 && sh.warp_mass[at] <= t; ++at) t -= sh.warp_mass[at];
-        i0 += at * stretch;
-        i1 = min(i1, i0 + stretch);
+        for (; at < kWarps - 1 && sh.warp[at] <= t; ++at) t -= sh.warp[at];
+        g0 += at * stretch;
+        g1 = min(g1, g0 + stretch);
     }
-    if (warp == 0)
-        for (int c = i0; c < i1; c += 32) {
-            const u64 w = c + lane < i1 ? left(c + lane) : 0;
-            const u64 before = warp_before(w, lane);
-            if (before <= t && before + w > t) put(a, r, c + lane, w, total);
-            const u64 sum = __shfl_sync(kFull, before + w, 31);
-            if (sum > t) break;
-            t -= sum;
+    if (warp != 0) return;
+    for (int c = g0; c < g1; c += 32) {
+        float v[kPer];
+        u64 w[kPer], mine = 0;
+        const int g = min(c + lane, g1 - 1);
+        row.load(g, v);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            w[j] = c + lane < g1 ? left(v[j], row.index(g) + j) : 0;
+            mine += w[j];
         }
+        u64 upto = warp_before(mine, lane);
+        const u64 sum = __shfl_sync(kFull, upto + mine, 31);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            if (upto <= t && upto + w[j] > t) put(a, r, row.index(g) + j, w[j], total);
+            upto += w[j];
+        }
+        if (sum > t) break;
+        t -= sum;
+    }
 }
 
 template <typename T> cudaError_t launch(const SampleParams &p, cudaStream_t s) {
@@ -592,12 +740,20 @@ template <typename T> cudaError_t launch(const SampleParams &p, cudaStream_t s) 
         return launch_pdl(true, sample_short_kernel<T>, dim3((unsigned)((p.n + warps - 1) / warps)), dim3(32 * warps), 0, s, p,
                           bits, p.n <= 4 * (int64_t)lim->sms);
     }
-    const size_t row = ((size_t)p.vocab * sizeof(T) + 31) / 16 * 16;
-    const bool keep = sizeof(Shared) + row <= lim->smem_optin;
-    const cudaError_t e = cudaFuncSetAttribute(sample_long_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)lim->smem_optin);
+    // CTAs of a row: as many as leave each of them 2048 tokens and the GPU two to an SM, or as its logits need
+    constexpr int kPer = kVec<T>;
+    const auto bytes = [&](int ctas) { return sizeof(Shared) + ((size_t)p.vocab / kPer / ctas + 3) * 16; };
+    int ctas = 1;
+    while (ctas < kMaxCtas && (bytes(ctas) > lim->smem_optin ||
+                               (p.n * ctas * 2 <= 2 * (int64_t)lim->sms && p.vocab >= 4096 * ctas)))
+        ctas *= 2;
+    const bool keep = bytes(ctas) <= lim->smem_optin;
+    const auto kern = ctas > 1 ? sample_long_kernel<T, true> : sample_long_kernel<T, false>;
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)lim->smem_optin);
     if (e != cudaSuccess) return e;
-    return launch_pdl(true, sample_long_kernel<T>, dim3((unsigned)p.n), dim3(kThreads), sizeof(Shared) + (keep ? row : 0), s, p,
-                      bits, keep, p.n <= lim->sms);
+    if (p.n > INT32_MAX / ctas) return cudaErrorInvalidValue;
+    return launch_cluster(true, kern, dim3((unsigned)(p.n * ctas)), dim3(kThreads), ctas, keep ? bytes(ctas) : sizeof(Shared), s, p,
+                          bits, keep, ctas, p.n * ctas <= lim->sms);
 }
 
 }  // namespace
