@@ -63,42 +63,36 @@ __device__ __forceinline__ Scale make_scale(float temperature, float top, int dr
     s.drop = drop;
     return s;
 }
-// (top - l) log2(e) / T, without its lower part: never falls as l does.
-__device__ __forceinline__ float distance(const Scale &s, float l) { return fminf(s.top - l, 3.402823466e38f) * s.hi; }
-
 // 2^-y for y = (top - l) log2(e) / T. y is formed as a sum of two floats (the difference and the product with their
 // rounding errors); it is split at multiples of 1/256 (P. T. P. Tang's table method, 1989), and what is left, |r| < 1/500, goes
 // through the series of exp to the third power: the error is that of r's rounding, 2^-9 2^-24.
 __device__ __forceinline__ u64 weight(const Scale &s, float l, const u64 *powers) {
-    const float d = s.top - l;
+    const float d = fminf(s.top - l, 3.402823466e38f);
     const float b = d - s.top;
-    float e = (s.top - (d - b)) - (l + b);          // top - l = d + e
-    const bool huge = !(d <= 3.402823466e38f);
-    const float d1 = huge ? 3.402823466e38f : d;
-    e = huge ? 0.f : e;
-    const float y = d1 * s.hi;
-    if (!(y < 100.f)) return 0;
-    const float ylo = fmaf(d1, s.lo, fmaf(e, s.hi, fmaf(d1, s.hi, -y)));
-    const int i = __float2int_rn(y * 256.f);
-    const float r = fmaf((float)i, -1.f / 256.f, y) + ylo;
+    const float e = (s.top - (d - b)) - (l + b);          // top - l = d + e, where that is finite
+    const float y = d * s.hi;
+    const float ylo = fmaf(d, s.lo, fmaf(e, s.hi, fmaf(d, s.hi, -y)));
+    const float yc = fminf(y, 100.f);                     // nothing is left of it then
+    const int i = __float2int_rn(yc * 256.f);
+    const float r = fmaf((float)i, -1.f / 256.f, yc) + (d < 1e38f ? ylo : 0.f);
     const float x = r * -0.6931471805599453f;
     const float em = fmaf(x * x, fmaf(x, 1.f / 6.f, 0.5f), x);
     const u64 p = powers[i & 255];
-    const long long c = __float2ll_rn((float)(unsigned)(p >> 32) * 4294967296.f * em);
+    const long long c = (long long)(unsigned)(p >> 32) * __float2int_rn(em * 1099511627776.f) >> 8;   // em 2^40, |em| < 2^-9
     const int drop = s.drop + (i >> 8);
     return drop < 64 ? (p + (u64)c) >> drop : 0;
 }
 
 // ---- logits
 
-// A logit as it counts: NaN as -inf, +inf as the type's largest finite number, -0 as 0.
+// A logit as it counts: NaN as -inf, +inf as the type's largest finite number.
 template <typename T> __device__ __forceinline__ float clean(float l) {
     const float most = sizeof(T) == 2 ? __uint_as_float(0x7f7f0000u) : __uint_as_float(0x7f7fffffu);
-    return l == l ? fminf(l, most) + 0.f : __uint_as_float(0xff800000u);
+    return fminf(fmaxf(l, __uint_as_float(0xff800000u)), most);
 }
-// The order of floats as that of unsigned numbers.
+// The order of floats (-0 as 0) as that of unsigned numbers.
 __device__ __forceinline__ unsigned key_of(float l) {
-    const unsigned b = __float_as_uint(l);
+    const unsigned b = __float_as_uint(l + 0.f);
     return b ^ ((unsigned)((int)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float of_key(unsigned k) {
@@ -293,7 +287,8 @@ __global__ void __launch_bounds__(256) sample_short_kernel(const __grid_constant
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048;          // of the distance to the maximum, kPerOctave to a factor of two
 constexpr float kPerOctave = 32.f;
-constexpr int kList = 512;           // tokens that are ranked one against the other
+constexpr int kList = kThreads;      // tokens that are ranked one against the other
+constexpr int kHead = 256;           // tokens among which a row is finished at once
 constexpr int kMaxCtas = 8;          // of a row
 
 struct alignas(16) Shared {
@@ -301,13 +296,16 @@ struct alignas(16) Shared {
     unsigned low[kBins], high[kBins];   // masses of the bins; counts in `low` alone
     u64 warp[kWarps];
     u64 slot[2][kMaxCtas];
-    u64 list_weight[kList];
-    float list_logit[kList];
-    int list_index[kList];
-    u64 found_before;
-    int found, length, last_index;
-    float last;
+    u64 list[kList], head[kHead];       // tokens (place) of the bin that holds the end, and of those before it
+    u64 weight[kList];
+    u64 found_before, last;
+    int found, length, ahead;
 };
+
+// Logit and index of a token, larger for what comes first.
+__device__ __forceinline__ u64 place(float l, int i) { return (u64)key_of(l) << 32 | (unsigned)~i; }
+__device__ __forceinline__ float logit_at(u64 place) { return of_key((unsigned)(place >> 32)); }
+__device__ __forceinline__ int index_at(u64 place) { return (int)~(unsigned)place; }
 
 // The CTAs of a row: one, or a cluster whose CTAs hold consecutive parts of it.
 template <bool kCluster> struct Team {
@@ -359,6 +357,18 @@ template <bool kCluster> struct Team {
     }
     __device__ __forceinline__ unsigned peek(const unsigned *p, int cta) const {
         return kCluster ? (unsigned)cluster_load(reinterpret_cast<const int *>(p), cta) : *p;
+    }
+    __device__ __forceinline__ int peek(const int *p, int cta) const { return kCluster ? cluster_load(p, cta) : *p; }
+    // A token to a list of the first CTA, as long as that has room.
+    __device__ __forceinline__ void append(int *length, u64 *list, int room, u64 v) const {
+        if (kCluster) {
+            int at;
+            asm volatile("atom.shared::cluster.add.s32 %0, [%1], 1;" : "=r"(at) : "r"(cluster_address(length, 0)) : "memory");
+            if (at < room) asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_address(&list[at], 0)), "l"(v) : "memory");
+        } else {
+            const int at = atomicAdd(length, 1);
+            if (at < room) list[at] = v;
+        }
     }
     __device__ __forceinline__ void tell(u64 *p, u64 v) const {   // the same place of every CTA, by one thread
         for (int i = 0; i < size; ++i)
@@ -440,13 +450,15 @@ template <typename T> struct Row {
         }
     }
     __device__ __forceinline__ bool in(float v, int i) const { return v > last || (v == last && i <= last_index); }
-    template <typename F> __device__ __forceinline__ void each(F &&f) const {   // f(logit, index) of what is left
+    // f(logits, first index) of this thread's groups that may hold tokens that are left: no other is as large as the last
+    template <typename F> __device__ __forceinline__ void each_group(F &&f) const {
         for (int g = g0 + threadIdx.x; g < g1; g += kThreads) {
             float v[kPer];
             load(g, v);
+            float most = v[0];
 #pragma unroll
-            for (int j = 0; j < kPer; ++j)
-                if (in(v[j], index(g) + j)) f(v[j], index(g) + j);
+            for (int j = 1; j < kPer; ++j) most = fmaxf(most, v[j]);
+            if (most >= last) f(v, index(g));
         }
     }
 };
@@ -464,78 +476,134 @@ template <bool kMass> __device__ __forceinline__ void clear_bins(Shared &sh, int
     }
     __syncthreads();
 }
+// Never falls as l does.
 __device__ __forceinline__ int bin_of(const Scale &sc, float l) {
-    return (int)fminf(distance(sc, l) * kPerOctave, (float)(kBins - 1));
+    return (int)fminf((sc.top - l) * (sc.hi * kPerOctave), (float)(kBins - 1));
+}
+
+// The end of a row whose tokens in question are few: `size` of them, this thread's first kHead places. They are the
+// likeliest of the row, and more than are kept. total: the mass that top_p is of; 0: that of the top_k among these.
+__device__ void finish(Shared &sh, const SampleParams &a, int64_t r, const Settings &st, const Scale &sc, int size, u64 total,
+                       int ahead) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    constexpr int kUsed = kHead / 32;
+    const bool mine = tid < size;
+    const u64 at = mine ? (tid < ahead ? sh.head[tid] : sh.list[tid - ahead]) : 0;
+    u64 w = mine ? weight(sc, logit_at(at), sh.powers) : 0;
+    __syncthreads();
+    if (mine) {
+        sh.list[tid] = at;
+        sh.weight[tid] = w;
+    }
+    __syncthreads();
+    int rank = 0;
+    u64 before = 0;
+    if (mine) {
+#pragma unroll 4
+        for (int j = 0; j < size; ++j)
+            if (sh.list[j] > at) {
+                ++rank;
+                before += sh.weight[j];
+            }
+    }
+    const auto sum_of = [&](u64 v) {
+        v = warp_sum(v);
+        if (lane == 0) sh.warp[warp] = v;
+        __syncthreads();
+        u64 s = 0;
+#pragma unroll
+        for (int i = 0; i < kUsed; ++i) s += sh.warp[i];
+        return s;
+    };
+    bool stays = mine;
+    if (total == 0) {
+        stays = mine && rank < st.k;
+        total = sum_of(stays ? w : 0);
+    }
+    if (st.nucleus) stays = stays && before < nucleus_mass(st.p, total);
+    if (!stays || w < st.least) w = 0;
+    __syncthreads();
+    if (mine) sh.weight[tid] = w;
+    total = sum_of(w);
+    const u64 t = __umul64hi(st.u, total);
+    if (w == 0) return;
+    u64 upto = 0;
+#pragma unroll 4
+    for (int j = 0; j < size; ++j)
+        if ((unsigned)sh.list[j] > (unsigned)at) upto += sh.weight[j];   // lower indexes
+    if (upto <= t && upto + w > t) put(a, r, index_at(at), w, total);
 }
 
 // Narrows the row to the tokens before which the sum of masses (counts) is below the goal: `goal_of` the sum over all that
-// are left by now. Nothing changes where the sum does not reach the goal.
+// are left by now. Nothing changes where the sum does not reach the goal. False: the row is finished.
 template <bool kMass, bool kCluster, typename T, typename G>
-__device__ void cut(Team<kCluster> &team, Row<T> &row, const Scale &sc, G &&goal_of) {
+__device__ bool cut(Team<kCluster> &team, Row<T> &row, const SampleParams &a, int64_t r, const Settings &st, const Scale &sc,
+                    G &&goal_of) {
+    constexpr int kPer = Row<T>::kPer;
     Shared &sh = team.sh;
     clear_bins<kMass>(sh, kBins);
     u64 sum = 0;
-    row.each([&](float l, int) {
-        const int b = bin_of(sc, l);
-        if (kMass) {
-            const u64 w = weight(sc, l, sh.powers);
-            if (w) add_mass(sh, b, w);
-            sum += w;
-        } else {
-            atomicAdd(&sh.low[b], 1u);
-            ++sum;
+    row.each_group([&](const float (&v)[kPer], int i) {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const bool in = row.in(v[j], i + j);
+            if (kMass) {
+                const u64 w = weight(sc, v[j], sh.powers);
+                if (in && w) {
+                    add_mass(sh, bin_of(sc, v[j]), w);
+                    sum += w;
+                }
+            } else if (in) {
+                atomicAdd(&sh.low[bin_of(sc, v[j])], 1u);
+                ++sum;
+            }
         }
     });
     u64 before;
     const u64 total = team.sum(team.block_sum(sum), before), goal = goal_of(total);
-    if (total < goal) return;
+    if (total < goal) return true;
     team.template find_bin<kMass>(kBins, goal);
     const int bin = sh.found;
     before = sh.found_before;
     unsigned prefix = 0, known = 0;   // bits of the key that the tokens looked at share
-    const auto looked_at = [&](float l) { return bin_of(sc, l) == bin && (key_of(l) & known) == prefix; };
     for (;;) {
-        // the tokens in question, to the first CTA
-        if (threadIdx.x == 0) sh.length = 0;
+        // the tokens in question, to the first CTA, and those before them
+        if (threadIdx.x == 0) sh.length = sh.ahead = 0;
         team.sync();
-        row.each([&](float l, int i) {
-            if (!looked_at(l)) return;
-            int at;
-            if (kCluster) {
-                asm volatile("atom.shared::cluster.add.s32 %0, [%1], 1;" : "=r"(at) : "r"(cluster_address(&sh.length, 0)) : "memory");
-                if (at >= kList) return;
-                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_address(&sh.list_logit[at], 0)), "f"(l) : "memory");
-                asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(cluster_address(&sh.list_index[at], 0)), "r"(i) : "memory");
-            } else {
-                at = atomicAdd(&sh.length, 1);
-                if (at >= kList) return;
-                sh.list_logit[at] = l;
-                sh.list_index[at] = i;
+        row.each_group([&](const float (&v)[kPer], int i) {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const int b = bin_of(sc, v[j]);
+                if (b > bin || !row.in(v[j], i + j)) continue;
+                if (b < bin || (key_of(v[j]) & known) > prefix) {
+                    if (known == 0) team.append(&sh.ahead, sh.head, kHead, place(v[j], i + j));
+                } else if ((key_of(v[j]) & known) == prefix) {
+                    team.append(&sh.length, sh.list, kList, place(v[j], i + j));
+                }
             }
         });
         team.sync();
-        const int size = (int)team.peek(reinterpret_cast<const unsigned *>(&sh.length), 0);
+        const int size = team.peek(&sh.length, 0), ahead = team.peek(&sh.ahead, 0);
+        if (known == 0 && ahead + size <= kHead) {
+            team.sync();   // all have seen that
+            if (team.rank == 0) finish(sh, a, r, st, sc, ahead + size, kMass ? total : 0, ahead);
+            return false;
+        }
         if (size <= kList) {
             // each against all others; the last that stays is the one at which the sum reaches the goal
             if (team.rank == 0) {
+                const u64 at = (int)threadIdx.x < size ? sh.list[threadIdx.x] : 0;
                 if (kMass) {
-                    if ((int)threadIdx.x < size) sh.list_weight[threadIdx.x] = weight(sc, sh.list_logit[threadIdx.x], sh.powers);
+                    if (at) sh.weight[threadIdx.x] = weight(sc, logit_at(at), sh.powers);
                     __syncthreads();
                 }
-                if ((int)threadIdx.x < size) {
-                    const float l = sh.list_logit[threadIdx.x];
-                    const int at = sh.list_index[threadIdx.x];
+                if (at) {
                     u64 mine = before;
 #pragma unroll 4
-                    for (int j = 0; j < size; ++j) {
-                        const float o = sh.list_logit[j];
-                        if (o > l || (o == l && sh.list_index[j] < at)) mine += kMass ? sh.list_weight[j] : 1;
-                    }
-                    const u64 w = kMass ? sh.list_weight[threadIdx.x] : 1;
-                    if (mine < goal && mine + w >= goal) {
-                        team.tell(reinterpret_cast<int *>(&sh.last), __float_as_int(l));
-                        team.tell(&sh.last_index, at);
-                    }
+                    for (int j = 0; j < size; ++j)
+                        if (sh.list[j] > at) mine += kMass ? sh.weight[j] : 1;
+                    const u64 w = kMass ? sh.weight[threadIdx.x] : 1;
+                    if (mine < goal && mine + w >= goal) team.tell(&sh.last, at);
                 }
             }
             break;
@@ -544,49 +612,50 @@ __device__ void cut(Team<kCluster> &team, Row<T> &row, const Scale &sc, G &&goal
             const float l = of_key(prefix);
             const u64 w = kMass ? weight(sc, l, sh.powers) : 1;
             const u64 want = (goal - before + w - 1) / w;   // w > 0: the sum reaches the goal among them
-            u64 n = 0, ahead;
-            row.each([&](float o, int) { n += o == l; });
-            n = team.block_sum(n);
-            team.sum(n, ahead);
-            // the group that holds it by its order: a stretch of groups to a thread
-            if (ahead < want && ahead + n >= want) {
-                const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-                const int stretch = (row.g1 - row.g0 + kThreads - 1) / kThreads, a = row.g0 + (int)threadIdx.x * stretch;
-                const int b = min(row.g1, a + stretch);
-                u64 mine = 0;
-                const auto walk = [&](auto &&found) {
-                    for (int g = a; g < b; ++g) {
-                        float v[Row<T>::kPer];
-                        row.load(g, v);
+            // a stretch of groups to a thread; the one that holds it token by token
+            const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+            const int stretch = (row.g1 - row.g0 + kThreads - 1) / kThreads, first = row.g0 + (int)threadIdx.x * stretch;
+            const int end = min(row.g1, first + stretch);
+            const auto walk = [&](auto &&found) {
+                for (int g = first; g < end; ++g) {
+                    float v[kPer];
+                    row.load(g, v);
 #pragma unroll
-                        for (int j = 0; j < Row<T>::kPer; ++j)
-                            if (v[j] == l && row.in(v[j], row.index(g) + j)) found(row.index(g) + j);
-                    }
-                };
-                walk([&](int) { ++mine; });
-                u64 upto = warp_before(mine, lane);
-                if (lane == 31) sh.warp[warp] = upto + mine;
-                __syncthreads();
-                for (int i = 0; i < warp; ++i) upto += sh.warp[i];
-                upto += ahead;
-                if (upto < want && upto + mine >= want)
-                    walk([&](int i) {
-                        if (++upto == want) {
-                            team.tell(reinterpret_cast<int *>(&sh.last), __float_as_int(l));
-                            team.tell(&sh.last_index, i);
-                        }
-                    });
+                    for (int j = 0; j < kPer; ++j)
+                        if (v[j] == l && row.in(v[j], row.index(g) + j)) found(row.index(g) + j);
+                }
+            };
+            u64 mine = 0;
+            walk([&](int) { ++mine; });
+            u64 upto = warp_before(mine, lane), ahead_of;
+            __syncthreads();
+            if (lane == 31) sh.warp[warp] = upto + mine;
+            __syncthreads();
+            u64 all = 0;
+#pragma unroll
+            for (int i = 0; i < kWarps; ++i) {
+                if (i < warp) upto += sh.warp[i];
+                all += sh.warp[i];
             }
+            team.sum(all, ahead_of);
+            upto += ahead_of;
+            if (upto < want && upto + mine >= want)
+                walk([&](int i) {
+                    if (++upto == want) team.tell(&sh.last, place(l, i));
+                });
             break;
         }
         // too many: those that share the next eight bits of the key
         const int shift = known == 0 ? 24 : known == 0xff000000u ? 16 : known == 0xffff0000u ? 8 : 0;
         clear_bins<kMass>(sh, 256);
-        row.each([&](float l, int) {
-            if (!looked_at(l)) return;
-            const int b = (int)(255u - (key_of(l) >> shift & 255u));
-            if (kMass) add_mass(sh, b, weight(sc, l, sh.powers));
-            else atomicAdd(&sh.low[b], 1u);
+        row.each_group([&](const float (&v)[kPer], int i) {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                if (bin_of(sc, v[j]) != bin || (key_of(v[j]) & known) != prefix || !row.in(v[j], i + j)) continue;
+                const int b = (int)(255u - (key_of(v[j]) >> shift & 255u));
+                if (kMass) add_mass(sh, b, weight(sc, v[j], sh.powers));
+                else atomicAdd(&sh.low[b], 1u);
+            }
         });
         team.template find_bin<kMass>(256, goal - before);
         before += sh.found_before;
@@ -594,8 +663,9 @@ __device__ void cut(Team<kCluster> &team, Row<T> &row, const Scale &sc, G &&goal
         known |= 255u << shift;
     }
     team.sync();
-    row.last = sh.last;
-    row.last_index = sh.last_index;
+    row.last = logit_at(sh.last);
+    row.last_index = index_at(sh.last);
+    return true;
 }
 
 template <typename T, bool kCluster>
@@ -656,7 +726,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_long_kernel(const __grid_c
     const Settings st = settings_of(a, r, drop);
     if (st.greedy || st.k == 1) {
         int at = 0x7fffffff;
-        row.each([&](float l, int i) { at = l == top ? min(at, i) : at; });
+        row.each_group([&](const float (&v)[kPer], int i) {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) at = v[j] == top ? min(at, i + j) : at;
+        });
         at = __reduce_min_sync(kFull, at);
         __syncthreads();
         if (lane == 0) sh.warp[warp] = (u64)at;
@@ -670,13 +743,12 @@ __global__ void __launch_bounds__(kThreads, 2) sample_long_kernel(const __grid_c
         return;
     }
     const Scale sc = make_scale(st.temperature, top, drop);
-    if (st.k) cut<false>(team, row, sc, [&](u64) { return (u64)st.k; });
-    if (st.nucleus) cut<true>(team, row, sc, [&](u64 total) { return nucleus_mass(st.p, total); });
+    if (st.k && !cut<false>(team, row, a, r, st, sc, [&](u64) { return (u64)st.k; })) return;
+    if (st.nucleus && !cut<true>(team, row, a, r, st, sc, [&](u64 total) { return nucleus_mass(st.p, total); })) return;
     // the draw: the CTA, then the warp that holds the token (by a stretch of groups each), then by groups of 32 lanes
     const auto left = [&](float l, int i) -> u64 {
-        if (!row.in(l, i)) return 0;
         const u64 w = weight(sc, l, sh.powers);
-        return w >= st.least ? w : 0;
+        return row.in(l, i) && w >= st.least ? w : 0;
     };
     int g0 = row.g0, g1 = row.g1;
     u64 t = 0, total = 0;
@@ -686,6 +758,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_long_kernel(const __grid_c
         for (int g = b0 + lane; g < b1; g += 32) {
             float v[kPer];
             row.load(g, v);
+            float most = v[0];
+#pragma unroll
+            for (int j = 1; j < kPer; ++j) most = fmaxf(most, v[j]);
+            if (most < row.last) continue;
 #pragma unroll
             for (int j = 0; j < kPer; ++j) sum += left(v[j], row.index(g) + j);
         }
