@@ -585,11 +585,12 @@ mb_status mb_matmul_q8(const uint8_t *a, const uint8_t *a_scales, const uint8_t 
  *            largest finite number
  *   u      : [n] fp32 in [0, 1) (1 or more: the last token left; below 0 or NaN: the first)
  *   temperature, top_p, min_p : [n] fp32, top_k : [n] int32, or NULL: 1, 1, 0, 0.
- *            A temperature of 0 (or less, or NaN) takes the largest logit; NaN
- *            in top_p or min_p switches that one off
+ *            A temperature of 0 (or less, or NaN) takes the largest logit, one
+ *            above 1e30 makes all weights 1; NaN in top_p or min_p switches that
+ *            one off
  *   tokens : [n], MB_TOKEN_I32 or MB_TOKEN_I64; -1 where every token is masked
  *   prob   : [n] fp32 or NULL: the probability the token was drawn with (0 with -1)
- * Weights are within 2^-32 of their value and all sums and comparisons exact:
+ * Weights are within 2^-31 of their value and all sums and comparisons exact:
  * the draw is reproducible, and differs from that of exact arithmetic only
  * where a border is as near as that. tokens and prob must not overlap anything else.
  */

@@ -7,7 +7,7 @@
 //
 // Every comparison is of integers. A weight is held as a whole number of units of 2^-shift (shift = 62 - log2 of the
 // vocabulary: sums of a row fit 62 bits), so sums do not depend on their order, atomics included, and products with top_p
-// and u are taken exactly. A weight itself is within 2^-32 of its value (weight()): a draw differs from that of exact
+// and u are taken exactly. A weight itself is within 2^-31 of its value (weight()): a draw differs from that of exact
 // arithmetic where u falls that near to a border.
 //
 // Rows of up to 256 tokens (bytes): one warp, eight tokens a lane, sorted in registers. Longer rows: a CTA, or a
@@ -16,6 +16,7 @@
 #include "../../include/mbscan.h"
 #include "cluster.cuh"
 #include "common.cuh"
+#include "pairs.cuh"
 #include "vec.cuh"
 
 #include <math.h>
@@ -56,31 +57,52 @@ struct Scale {
 };
 __device__ __forceinline__ Scale make_scale(float temperature, float top, int drop) {
     constexpr float kHi = 1.4426950408889634f, kLo = (float)(1.4426950408889634074 - (double)kHi);
+    const bool flat = !(temperature < 1e30f);
     Scale s;
-    s.hi = fminf(__fdiv_rn(kHi, temperature), 3.402823466e38f);
-    s.lo = s.hi < 1e38f && s.hi > 1e-30f ? (fmaf(-s.hi, temperature, kHi) + kLo) / temperature : 0.f;
-    s.top = top;
+    s.hi = flat ? 0.f : fminf(__fdiv_rn(kHi, temperature), 3.402823466e38f);
+    s.lo = flat || !(s.hi < 1e38f) ? 0.f : __fdiv_rn(fmaf(-s.hi, temperature, kHi) + kLo, temperature);
+    s.top = flat ? 0.f : top;
     s.drop = drop;
     return s;
 }
-// 2^-y for y = (top - l) log2(e) / T. y is formed as a sum of two floats (the difference and the product with their
-// rounding errors); it is split at multiples of 1/256 (P. T. P. Tang's table method, 1989), and what is left, |r| < 1/500, goes
-// through the series of exp to the third power: the error is that of r's rounding, 2^-9 2^-24.
-__device__ __forceinline__ u64 weight(const Scale &s, float l, const u64 *powers) {
-    const float d = fminf(s.top - l, 3.402823466e38f);
-    const float b = d - s.top;
-    const float e = (s.top - (d - b)) - (l + b);          // top - l = d + e, where that is finite
-    const float y = d * s.hi;
-    const float ylo = fmaf(d, s.lo, fmaf(e, s.hi, fmaf(d, s.hi, -y)));
-    const float yc = fminf(y, 100.f);                     // nothing is left of it then
-    const int i = __float2int_rn(yc * 256.f);
-    const float r = fmaf((float)i, -1.f / 256.f, yc) + (d < 1e38f ? ylo : 0.f);
-    const float x = r * -0.6931471805599453f;
-    const float em = fmaf(x * x, fmaf(x, 1.f / 6.f, 0.5f), x);
+
+// Two weights, 2^-y for y = (top - l) log2(e) / T. y is formed as a sum of two floats (the difference and the product with
+// their rounding errors); it is split at multiples of 1/256 (P. T. P. Tang's table method, 1989), and what is left, |r| < 1/500,
+// goes through the series of exp to the third power: the error is that of r's rounding, 2^-9 2^-24, and of the units of 2^-32
+// in which the power's correction is taken. Whole numbers are made by adding 1.5 * 2^23, which leaves them in the low bits
+// (conversions have a quarter of the rate), everything in fp32 is done on pairs. Logits that are masked give no number.
+constexpr float kMagic = 12582912.f;
+constexpr int kMagicBits = 0x4b400000;
+
+__device__ __forceinline__ u64 power(float m, float t, int drop, const u64 *powers) {
+    const int i = __float_as_int(m);
     const u64 p = powers[i & 255];
-    const long long c = (long long)(unsigned)(p >> 32) * __float2int_rn(em * 1099511627776.f) >> 8;   // em 2^40, |em| < 2^-9
-    const int drop = s.drop + (i >> 8);
-    return drop < 64 ? (p + (u64)c) >> drop : 0;
+    const u64 w = p + (u64)((long long)(int)(p >> 32) * (2 * (__float_as_int(t) - kMagicBits)));
+    return w >> min(drop + ((i - kMagicBits) >> 8), 63);   // w < 2^63
+}
+__device__ __forceinline__ void weights(const Scale &s, float2 l, const u64 *powers, u64 &w0, u64 &w1) {
+    const float2 minus = splat(-1.f), top = splat(s.top), hi = splat(s.hi);
+    const float2 d = fma2(l, minus, top);
+    const float2 b = add2(d, splat(-s.top));
+    const float2 e = fma2(add2(l, b), minus, fma2(fma2(b, minus, d), minus, top));   // top - l = d + e, where that is finite
+    float2 y = mul2(d, hi);
+    const float2 rest = fma2(d, splat(s.lo), fma2(e, hi, fma2(d, hi, mul2(d, splat(-s.hi)))));
+    y = make_float2(fminf(y.x, 100.f), fminf(y.y, 100.f));   // nothing is left then
+    const float2 m = fma2(y, splat(256.f), splat(kMagic));
+    const float2 x = mul2(add2(fma2(add2(m, splat(-kMagic)), splat(-1.f / 256.f), y), rest), splat(-0.6931471805599453f));
+    const float2 em = fma2(mul2(x, x), fma2(x, splat(1.f / 6.f), splat(0.5f)), x);   // |em| < 2^-9
+    const float2 t = fma2(em, splat(2147483648.f), splat(kMagic));
+    w0 = power(m.x, t.x, s.drop, powers);
+    w1 = power(m.y, t.y, s.drop, powers);
+}
+// One, where few are wanted.
+__device__ __noinline__ u64 weight_of(float hi, float lo, float top, int drop, float l, const u64 *powers) {
+    u64 w, same;
+    weights(Scale{hi, lo, top, drop}, make_float2(l, l), powers, w, same);
+    return w;
+}
+__device__ __forceinline__ u64 weight(const Scale &s, float l, const u64 *powers) {
+    return weight_of(s.hi, s.lo, s.top, s.drop, l, powers);
 }
 
 // ---- logits
@@ -165,27 +187,25 @@ template <typename K> __device__ __forceinline__ void exchange(K &a, K &b, bool 
     b = down ? lo : hi;
 }
 // Falling order over the warp, position 8 * lane + j.
-template <typename K> __device__ __forceinline__ void sort256(K (&v)[kEach], int lane) {
+template <int kSize, int kStep, typename K> __device__ __forceinline__ void merge_step(K (&v)[kEach], int lane) {
+    const bool falls = kSize == kShort || (lane & (kSize / kEach)) == 0;   // stretches of kSize <= 8: by the position in them
+    if constexpr (kStep >= kEach) {
+        const bool larger = falls == ((lane & (kStep / kEach)) == 0);
 #pragma unroll
-    for (int size = 2; size <= kShort; size *= 2) {
-#pragma unroll
-        for (int step = size / 2; step > 0; step /= 2) {
-            if (step >= kEach) {
-                const bool down = (lane & (size / kEach)) == 0 || size == kShort;
-                const bool first = (lane & (step / kEach)) == 0;
-#pragma unroll
-                for (int j = 0; j < kEach; ++j) {
-                    const K o = __shfl_xor_sync(kFull, v[j], step / kEach);
-                    v[j] = (v[j] > o) == (down == first) ? v[j] : o;
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < kEach; ++j)
-                    if ((j & step) == 0)
-                        exchange(v[j], v[j | step], size < kEach ? (j & size) == 0 : (lane & (size / kEach)) == 0 || size == kShort);
-            }
+        for (int j = 0; j < kEach; ++j) {
+            const K o = __shfl_xor_sync(kFull, v[j], kStep / kEach);
+            v[j] = (v[j] > o) == larger ? v[j] : o;
         }
+    } else {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j)
+            if ((j & kStep) == 0) exchange(v[j], v[j | kStep], kSize < kEach ? (j & kSize) == 0 : falls);
     }
+    if constexpr (kStep > 1) merge_step<kSize, kStep / 2>(v, lane);
+}
+template <int kSize = 2, typename K> __device__ __forceinline__ void sort256(K (&v)[kEach], int lane) {
+    merge_step<kSize, kSize / 2>(v, lane);
+    if constexpr (kSize < kShort) sort256<kSize * 2>(v, lane);
 }
 
 // Logit and index in one number, larger for what comes first: 16 + 8 bits of bf16 logits, 32 + 8 of fp32 ones.
@@ -237,10 +257,12 @@ __global__ void __launch_bounds__(256) sample_short_kernel(const __grid_constant
         sort256(c, lane);
         u64 w[kEach], mine = 0;
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-            const unsigned k = unpack(T{}, c[j]);
-            w[j] = k > kMasked && (!st.k || kEach * lane + j < st.k) ? weight(sc, of_key(k), powers) : 0;
-            mine += w[j];
+        for (int j = 0; j < kEach; j += 2) {
+            const unsigned k0 = unpack(T{}, c[j]), k1 = unpack(T{}, c[j + 1]);
+            weights(sc, make_float2(of_key(k0), of_key(k1)), powers, w[j], w[j + 1]);
+            if (k0 <= kMasked || (st.k && kEach * lane + j >= st.k)) w[j] = 0;
+            if (k1 <= kMasked || (st.k && kEach * lane + j + 1 >= st.k)) w[j + 1] = 0;
+            mine += w[j] + w[j + 1];
         }
         u64 before = warp_before(mine, lane);
         const u64 total = __shfl_sync(kFull, before + mine, 31);
@@ -261,9 +283,9 @@ __global__ void __launch_bounds__(256) sample_short_kernel(const __grid_constant
     u64 w[kEach], mine = 0;
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
+        if (j % 2 == 0) weights(sc, make_float2(of_key(key[j]), of_key(key[j + 1])), powers, w[j], w[j + 1]);
         const bool in = key[j] > kMasked && pack(T{}, key[j], kEach * lane + j) >= last;
-        w[j] = in ? weight(sc, of_key(key[j]), powers) : 0;
-        if (w[j] < st.least) w[j] = 0;
+        if (!in || w[j] < st.least) w[j] = 0;
         mine += w[j];
     }
     u64 upto = warp_before(mine, lane);
@@ -289,6 +311,9 @@ constexpr int kBins = 2048;          // of the distance to the maximum, kPerOcta
 constexpr float kPerOctave = 32.f;
 constexpr int kList = kThreads;      // tokens that are ranked one against the other
 constexpr int kHead = 256;           // tokens among which a row is finished at once
+#ifndef MB_SAMPLE_CTAS
+#define MB_SAMPLE_CTAS 2
+#endif
 constexpr int kMaxCtas = 8;          // of a row
 
 struct alignas(16) Shared {
@@ -299,8 +324,11 @@ struct alignas(16) Shared {
     u64 list[kList], head[kHead];       // tokens (place) of the bin that holds the end, and of those before it
     u64 weight[kList];
     u64 found_before, last;
-    int found, length, ahead;
+    int found, length, ahead, length_full, ahead_full;
 };
+
+// The shared memory of the long rows' kernels: Shared, then the CTA's part of the row.
+extern __shared__ __align__(16) unsigned char g_row[];
 
 // Logit and index of a token, larger for what comes first.
 __device__ __forceinline__ u64 place(float l, int i) { return (u64)key_of(l) << 32 | (unsigned)~i; }
@@ -349,6 +377,7 @@ template <bool kCluster> struct Team {
         const u64 *slot = exchange(mine);
         u64 s = 0;
         before = 0;
+#pragma unroll 1
         for (int i = 0; i < size; ++i) {
             if (i == rank) before = s;
             s += slot[i];
@@ -359,40 +388,46 @@ template <bool kCluster> struct Team {
         return kCluster ? (unsigned)cluster_load(reinterpret_cast<const int *>(p), cta) : *p;
     }
     __device__ __forceinline__ int peek(const int *p, int cta) const { return kCluster ? cluster_load(p, cta) : *p; }
-    // A token to a list of the first CTA, as long as that has room.
-    __device__ __forceinline__ void append(int *length, u64 *list, int room, u64 v) const {
+    // A token to a list of the first CTA, as long as that has room; a list that was seen full is left alone (`full`: the
+    // places of one length would be handed out one after the other, to thousands of tokens in vain).
+    __device__ __forceinline__ void append(int *length, u64 *list, int room, u64 v, int *full) const {
+        if (*const_cast<volatile int *>(full)) return;
+        int at;
         if (kCluster) {
-            int at;
             asm volatile("atom.shared::cluster.add.s32 %0, [%1], 1;" : "=r"(at) : "r"(cluster_address(length, 0)) : "memory");
             if (at < room) asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_address(&list[at], 0)), "l"(v) : "memory");
         } else {
-            const int at = atomicAdd(length, 1);
+            at = atomicAdd(length, 1);
             if (at < room) list[at] = v;
         }
+        if (at >= room) *const_cast<volatile int *>(full) = 1;
     }
     __device__ __forceinline__ void tell(u64 *p, u64 v) const {   // the same place of every CTA, by one thread
+#pragma unroll 1
         for (int i = 0; i < size; ++i)
             if (kCluster) asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_address(p, i)), "l"(v) : "memory");
             else *p = v;
     }
     __device__ __forceinline__ void tell(int *p, int v) const {
+#pragma unroll 1
         for (int i = 0; i < size; ++i)
             if (kCluster) asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(cluster_address(p, i)), "r"(v) : "memory");
             else *p = v;
     }
 
     // The bin in which the running sum of the histogram's masses (counts) reaches `goal`, and the sum before it: found,
-    // found_before. Every CTA has filled its own `bins` bins; each adds up an equal share of them over all CTAs.
+    // found_before. Every CTA has filled its own `bins` bins (and all have met since); each adds up an equal share of them
+    // over all CTAs.
     template <bool kMass> __device__ void find_bin(int bins, u64 goal) {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         const int share = bins / size, each = (share + kThreads - 1) / kThreads;   // at most 4
-        sync();
         u64 v[kBins / kThreads], mine = 0;
 #pragma unroll
         for (int j = 0; j < kBins / kThreads; ++j) {
             const int b = threadIdx.x * each + j;
             v[j] = 0;
             if (j < each && b < share)
+#pragma unroll 1
                 for (int i = 0; i < size; ++i) {
                     v[j] += peek(&sh.low[rank * share + b], i);
                     if (kMass) v[j] += (u64)peek(&sh.high[rank * share + b], i) << 32;
@@ -427,9 +462,8 @@ template <bool kCluster> struct Team {
 
 // The logits of this CTA's part of a row, in 16-byte groups as they lie in memory: in shared memory as they count, or
 // where they are (rows that do not fit). What a group holds beyond the row is masked.
-template <typename T> struct Row {
+template <typename T, bool kKept> struct Row {
     static constexpr int kPer = kVec<T>;
-    const uint4 *groups;   // null: read from global memory
     const T *l;
     int vocab, offset;     // the first group starts `offset` elements before the row
     int g0, g1;            // this CTA's groups
@@ -438,21 +472,26 @@ template <typename T> struct Row {
     int last_index = -1;
 
     __device__ __forceinline__ int index(int g) const { return g * kPer - offset; }
+    __device__ __forceinline__ float from_memory(int i) const {
+        return i >= 0 && i < vocab ? clean<T>(to_f32(l[i])) : __uint_as_float(0xff800000u);
+    }
+    __device__ __forceinline__ float at(int g, int j) const {
+        if (kKept) return to_f32(reinterpret_cast<const T *>(g_row + sizeof(Shared))[(g - g0) * kPer + j]);
+        return from_memory(index(g) + j);
+    }
     __device__ __forceinline__ void load(int g, float (&f)[kPer]) const {
-        if (groups) {
-            widen(groups[g - g0], f);
-            return;
-        }
+        if (kKept) {
+            widen(reinterpret_cast<const uint4 *>(g_row + sizeof(Shared))[g - g0], f);
+        } else {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const int i = index(g) + j;
-            f[j] = i >= 0 && i < vocab ? clean<T>(to_f32(l[i])) : __uint_as_float(0xff800000u);
+            for (int j = 0; j < kPer; ++j) f[j] = from_memory(index(g) + j);
         }
     }
     __device__ __forceinline__ bool in(float v, int i) const { return v > last || (v == last && i <= last_index); }
     // f(logits, first index) of this thread's groups that may hold tokens that are left: no other is as large as the last
-    template <typename F> __device__ __forceinline__ void each_group(F &&f) const {
-        for (int g = g0 + threadIdx.x; g < g1; g += kThreads) {
+    template <typename F> __device__ __forceinline__ void groups(F &&f) const {
+#pragma unroll 1
+        for (int g = g0 + (int)threadIdx.x; g < g1; g += kThreads) {
             float v[kPer];
             load(g, v);
             float most = v[0];
@@ -461,6 +500,23 @@ template <typename T> struct Row {
             if (most >= last) f(v, index(g));
         }
     }
+    // f(logit, index), one after the other, of the tokens that are left of groups a, a + step, ... < b
+    template <typename F> __device__ __forceinline__ void each(int a, int b, int step, F &&f) const {
+#pragma unroll 1
+        for (int g = a; g < b; g += step) {
+            float v[kPer];
+            unsigned some = 0;
+            load(g, v);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) some |= in(v[j], index(g) + j) ? 1u << j : 0u;
+#pragma unroll 1
+            for (; some; some &= some - 1) {
+                const int j = __ffs(some) - 1;
+                f(at(g, j), index(g) + j);
+            }
+        }
+    }
+    template <typename F> __device__ __forceinline__ void each(F &&f) const { each(g0 + (int)threadIdx.x, g1, kThreads, f); }
 };
 
 __device__ __forceinline__ void add_mass(Shared &sh, int b, u64 w) {   // 64 bits by two atomics of 32
@@ -478,7 +534,7 @@ template <bool kMass> __device__ __forceinline__ void clear_bins(Shared &sh, int
 }
 // Never falls as l does.
 __device__ __forceinline__ int bin_of(const Scale &sc, float l) {
-    return (int)fminf((sc.top - l) * (sc.hi * kPerOctave), (float)(kBins - 1));
+    return __float_as_int(fmaf(fminf((sc.top - l) * sc.hi, (kBins - 1) / kPerOctave), kPerOctave, kMagic)) - kMagicBits;
 }
 
 // The end of a row whose tokens in question are few: `size` of them, this thread's first kHead places. They are the
@@ -536,26 +592,28 @@ __device__ void finish(Shared &sh, const SampleParams &a, int64_t r, const Setti
 
 // Narrows the row to the tokens before which the sum of masses (counts) is below the goal: `goal_of` the sum over all that
 // are left by now. Nothing changes where the sum does not reach the goal. False: the row is finished.
-template <bool kMass, bool kCluster, typename T, typename G>
-__device__ bool cut(Team<kCluster> &team, Row<T> &row, const SampleParams &a, int64_t r, const Settings &st, const Scale &sc,
+template <bool kMass, bool kCluster, typename T, bool kKept, typename G>
+__device__ bool cut(Team<kCluster> &team, Row<T, kKept> &row, const SampleParams &a, int64_t r, const Settings &st, const Scale &sc,
                     G &&goal_of) {
-    constexpr int kPer = Row<T>::kPer;
+    constexpr int kPer = kVec<T>;
     Shared &sh = team.sh;
+    if (threadIdx.x == 0) sh.length = sh.ahead = sh.length_full = sh.ahead_full = 0;
     clear_bins<kMass>(sh, kBins);
     u64 sum = 0;
-    row.each_group([&](const float (&v)[kPer], int i) {
+    row.groups([&](const float (&v)[kPer], int i) {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const bool in = row.in(v[j], i + j);
+        for (int j = 0; j < kPer; j += 2) {
+            const bool in0 = row.in(v[j], i + j), in1 = row.in(v[j + 1], i + j + 1);
             if (kMass) {
-                const u64 w = weight(sc, v[j], sh.powers);
-                if (in && w) {
-                    add_mass(sh, bin_of(sc, v[j]), w);
-                    sum += w;
-                }
-            } else if (in) {
-                atomicAdd(&sh.low[bin_of(sc, v[j])], 1u);
-                ++sum;
+                u64 w0, w1;
+                weights(sc, make_float2(v[j], v[j + 1]), sh.powers, w0, w1);
+                if (in0) add_mass(sh, bin_of(sc, v[j]), w0);
+                if (in1) add_mass(sh, bin_of(sc, v[j + 1]), w1);
+                sum += (in0 ? w0 : 0) + (in1 ? w1 : 0);
+            } else {
+                if (in0) atomicAdd(&sh.low[bin_of(sc, v[j])], 1u);
+                if (in1) atomicAdd(&sh.low[bin_of(sc, v[j + 1])], 1u);
+                sum += (in0 ? 1 : 0) + (in1 ? 1 : 0);
             }
         }
     });
@@ -565,27 +623,34 @@ __device__ bool cut(Team<kCluster> &team, Row<T> &row, const SampleParams &a, in
     team.template find_bin<kMass>(kBins, goal);
     const int bin = sh.found;
     before = sh.found_before;
+    if (!kMass && before > kHead && threadIdx.x == 0) sh.ahead_full = sh.ahead = kHead + 1;   // not to be finished at once
+    if (!kMass) __syncthreads();
     unsigned prefix = 0, known = 0;   // bits of the key that the tokens looked at share
     for (;;) {
         // the tokens in question, to the first CTA, and those before them
-        if (threadIdx.x == 0) sh.length = sh.ahead = 0;
-        team.sync();
-        row.each_group([&](const float (&v)[kPer], int i) {
+        row.groups([&](const float (&v)[kPer], int i) {
+            unsigned some = 0;
+            const int least = known == 0 && !*const_cast<volatile int *>(&sh.ahead_full) ? 0 : bin;
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
                 const int b = bin_of(sc, v[j]);
-                if (b > bin || !row.in(v[j], i + j)) continue;
-                if (b < bin || (key_of(v[j]) & known) > prefix) {
-                    if (known == 0) team.append(&sh.ahead, sh.head, kHead, place(v[j], i + j));
-                } else if ((key_of(v[j]) & known) == prefix) {
-                    team.append(&sh.length, sh.list, kList, place(v[j], i + j));
+                some |= b >= least && b <= bin && row.in(v[j], i + j) ? 1u << j : 0u;
+            }
+#pragma unroll 1
+            for (; some; some &= some - 1) {
+                const int j = __ffs(some) - 1;
+                const float l = row.at((i + j + row.offset) / kPer, j);
+                if (bin_of(sc, l) < bin) {
+                    team.append(&sh.ahead, sh.head, kHead, place(l, i + j), &sh.ahead_full);
+                } else if ((key_of(l) & known) == prefix) {
+                    team.append(&sh.length, sh.list, kList, place(l, i + j), &sh.length_full);
                 }
             }
         });
         team.sync();
         const int size = team.peek(&sh.length, 0), ahead = team.peek(&sh.ahead, 0);
         if (known == 0 && ahead + size <= kHead) {
-            team.sync();   // all have seen that
+            if (kCluster) team.sync();   // all have seen that
             if (team.rank == 0) finish(sh, a, r, st, sc, ahead + size, kMass ? total : 0, ahead);
             return false;
         }
@@ -616,17 +681,8 @@ __device__ bool cut(Team<kCluster> &team, Row<T> &row, const SampleParams &a, in
             const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
             const int stretch = (row.g1 - row.g0 + kThreads - 1) / kThreads, first = row.g0 + (int)threadIdx.x * stretch;
             const int end = min(row.g1, first + stretch);
-            const auto walk = [&](auto &&found) {
-                for (int g = first; g < end; ++g) {
-                    float v[kPer];
-                    row.load(g, v);
-#pragma unroll
-                    for (int j = 0; j < kPer; ++j)
-                        if (v[j] == l && row.in(v[j], row.index(g) + j)) found(row.index(g) + j);
-                }
-            };
             u64 mine = 0;
-            walk([&](int) { ++mine; });
+            row.each(first, end, 1, [&](float o, int) { mine += o == l; });
             u64 upto = warp_before(mine, lane), ahead_of;
             __syncthreads();
             if (lane == 31) sh.warp[warp] = upto + mine;
@@ -640,23 +696,23 @@ __device__ bool cut(Team<kCluster> &team, Row<T> &row, const SampleParams &a, in
             team.sum(all, ahead_of);
             upto += ahead_of;
             if (upto < want && upto + mine >= want)
-                walk([&](int i) {
-                    if (++upto == want) team.tell(&sh.last, place(l, i));
+                row.each(first, end, 1, [&](float o, int i) {
+                    if (o == l && ++upto == want) team.tell(&sh.last, place(l, i));
                 });
             break;
         }
         // too many: those that share the next eight bits of the key
+        team.sync();   // all have seen the length
         const int shift = known == 0 ? 24 : known == 0xff000000u ? 16 : known == 0xffff0000u ? 8 : 0;
+        if (threadIdx.x == 0) sh.length = sh.ahead = sh.length_full = sh.ahead_full = 0;
         clear_bins<kMass>(sh, 256);
-        row.each_group([&](const float (&v)[kPer], int i) {
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) {
-                if (bin_of(sc, v[j]) != bin || (key_of(v[j]) & known) != prefix || !row.in(v[j], i + j)) continue;
-                const int b = (int)(255u - (key_of(v[j]) >> shift & 255u));
-                if (kMass) add_mass(sh, b, weight(sc, v[j], sh.powers));
-                else atomicAdd(&sh.low[b], 1u);
-            }
+        row.each([&](float l, int) {
+            if (bin_of(sc, l) != bin || (key_of(l) & known) != prefix) return;
+            const int b = (int)(255u - (key_of(l) >> shift & 255u));
+            if (kMass) add_mass(sh, b, weight(sc, l, sh.powers));
+            else atomicAdd(&sh.low[b], 1u);
         });
+        team.sync();
         team.template find_bin<kMass>(256, goal - before);
         before += sh.found_before;
         prefix |= (255u - (unsigned)sh.found) << shift;
@@ -668,11 +724,10 @@ __device__ bool cut(Team<kCluster> &team, Row<T> &row, const SampleParams &a, in
     return true;
 }
 
-template <typename T, bool kCluster>
-__global__ void __launch_bounds__(kThreads, 2) sample_long_kernel(const __grid_constant__ SampleParams a, int drop, bool keep, int ctas,
+template <typename T, bool kCluster, bool kKept>
+__global__ void __launch_bounds__(kThreads, 2) sample_long_kernel(const __grid_constant__ SampleParams a, int drop, int ctas,
                                                                   bool early) {
-    extern __shared__ __align__(16) unsigned char dyn[];
-    Shared &sh = *reinterpret_cast<Shared *>(dyn);
+    Shared &sh = *reinterpret_cast<Shared *>(g_row);
     if (kCluster) cluster_arrive();   // everybody is there before the first exchange
     constexpr int kPer = kVec<T>;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -681,32 +736,39 @@ __global__ void __launch_bounds__(kThreads, 2) sample_long_kernel(const __grid_c
     pdl_wait();
     const int64_t r = blockIdx.x / (unsigned)ctas;
     Team<kCluster> team{sh, (int)(blockIdx.x % (unsigned)ctas), ctas};
-    Row<T> row;
+    Row<T, kKept> row;
     row.l = static_cast<const T *>(a.logits) + r * a.vocab;
     row.vocab = a.vocab;
     row.offset = (int)(reinterpret_cast<uintptr_t>(row.l) & 15) / (int)sizeof(T);
-    row.groups = nullptr;
     const int groups = (row.offset + a.vocab + kPer - 1) / kPer;
     row.g0 = (int)((int64_t)groups * team.rank / ctas);
     row.g1 = (int)((int64_t)groups * (team.rank + 1) / ctas);
-    uint4 *const copy = reinterpret_cast<uint4 *>(dyn + sizeof(Shared));
+    uint4 *const copy = reinterpret_cast<uint4 *>(g_row + sizeof(Shared));
     float top = __uint_as_float(0xff800000u);
-#pragma unroll 4
-    for (int g = row.g0 + threadIdx.x; g < row.g1; g += kThreads) {
-        const int i = row.index(g);
-        float f[kPer];
-        if (i >= 0 && i + kPer <= a.vocab) {
-            widen(ld16(row.l + i), f);
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) f[j] = clean<T>(f[j]);
-        } else {
-            row.load(g, f);
-        }
-        if (keep) copy[g - row.g0] = narrow(f);
+    const auto take = [&](int g, const float (&f)[kPer]) {
+        if (kKept) copy[g - row.g0] = narrow(f);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) top = fmaxf(top, f[j]);
+    };
+    // the whole groups of the row, and the two that may be cut
+    const int whole0 = (row.offset + kPer - 1) / kPer, whole1 = (row.offset + a.vocab) / kPer;
+#pragma unroll 4
+    for (int g = max(row.g0, whole0) + (int)threadIdx.x; g < min(row.g1, whole1); g += kThreads) {
+        float f[kPer];
+        widen(ld16(row.l + row.index(g)), f);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) f[j] = clean<T>(f[j]);
+        take(g, f);
     }
-    if (keep) row.groups = copy;
+    if (threadIdx.x < 2) {
+        const int g = threadIdx.x == 0 ? 0 : groups - 1;
+        if (g >= row.g0 && g < row.g1 && (g < whole0 || g >= whole1)) {
+            float f[kPer];
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) f[j] = row.from_memory(row.index(g) + j);
+            take(g, f);
+        }
+    }
     {
         const unsigned k = __reduce_max_sync(kFull, key_of(top));
         if (lane == 0) sh.warp[warp] = k;
@@ -716,6 +778,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_long_kernel(const __grid_c
         for (int i = 0; i < kWarps; ++i) best = max(best, sh.warp[i]);
         if (kCluster) cluster_wait();
         const u64 *slot = team.exchange(best);
+#pragma unroll 1
         for (int i = 0; i < ctas; ++i) best = max(best, slot[i]);
         top = of_key((unsigned)best);
     }
@@ -726,10 +789,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_long_kernel(const __grid_c
     const Settings st = settings_of(a, r, drop);
     if (st.greedy || st.k == 1) {
         int at = 0x7fffffff;
-        row.each_group([&](const float (&v)[kPer], int i) {
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) at = v[j] == top ? min(at, i + j) : at;
-        });
+        row.each([&](float l, int i) { at = l == top ? min(at, i) : at; });
         at = __reduce_min_sync(kFull, at);
         __syncthreads();
         if (lane == 0) sh.warp[warp] = (u64)at;
@@ -738,6 +798,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_long_kernel(const __grid_c
 #pragma unroll
         for (int i = 0; i < kWarps; ++i) first = min(first, sh.warp[i]);
         const u64 *slot = team.exchange(first);
+#pragma unroll 1
         for (int i = 0; i < ctas; ++i) first = min(first, slot[i]);
         if (team.rank == 0 && threadIdx.x == 0) put(a, r, (int)first, 1, 1);
         return;
@@ -746,24 +807,35 @@ __global__ void __launch_bounds__(kThreads, 2) sample_long_kernel(const __grid_c
     if (st.k && !cut<false>(team, row, a, r, st, sc, [&](u64) { return (u64)st.k; })) return;
     if (st.nucleus && !cut<true>(team, row, a, r, st, sc, [&](u64 total) { return nucleus_mass(st.p, total); })) return;
     // the draw: the CTA, then the warp that holds the token (by a stretch of groups each), then by groups of 32 lanes
-    const auto left = [&](float l, int i) -> u64 {
+    const auto left = [&](float l) -> u64 {
         const u64 w = weight(sc, l, sh.powers);
-        return row.in(l, i) && w >= st.least ? w : 0;
+        return w >= st.least ? w : 0;
     };
     int g0 = row.g0, g1 = row.g1;
     u64 t = 0, total = 0;
+#pragma unroll 1
     for (int level = 0; level < 2; ++level) {
         const int stretch = (g1 - g0 + kThreads - 1) / kThreads * 32, b0 = g0 + warp * stretch, b1 = min(g1, b0 + stretch);
         u64 sum = 0;
-        for (int g = b0 + lane; g < b1; g += 32) {
+#pragma unroll 1
+        for (int c = b0; c < b1; c += 32) {
+            const int g = min(c + lane, b1 - 1);
             float v[kPer];
             row.load(g, v);
-            float most = v[0];
+            unsigned some = 0;
 #pragma unroll
-            for (int j = 1; j < kPer; ++j) most = fmaxf(most, v[j]);
-            if (most < row.last) continue;
+            for (int j = 0; j < kPer; ++j) some |= c + lane < b1 && row.in(v[j], row.index(g) + j) ? 1u << j : 0u;
+            // all of the group, or one after the other where no lane has many (a group of eight costs three of these)
+            if (__any_sync(kFull, __popc(some) * 3 > kPer)) {
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) sum += left(v[j], row.index(g) + j);
+                for (int j = 0; j < kPer; j += 2) {
+                    u64 w0, w1;
+                    weights(sc, make_float2(v[j], v[j + 1]), sh.powers, w0, w1);
+                    sum += (some >> j & 1u && w0 >= st.least ? w0 : 0) + (some >> j & 2u && w1 >= st.least ? w1 : 0);
+                }
+            } else {
+                for (; some; some &= some - 1) sum += left(row.at(g, __ffs(some) - 1));
+            }
         }
         sum = warp_sum(sum);
         __syncthreads();
@@ -784,23 +856,18 @@ __global__ void __launch_bounds__(kThreads, 2) sample_long_kernel(const __grid_c
         g1 = min(g1, g0 + stretch);
     }
     if (warp != 0) return;
+#pragma unroll 1
     for (int c = g0; c < g1; c += 32) {
-        float v[kPer];
-        u64 w[kPer], mine = 0;
-        const int g = min(c + lane, g1 - 1);
-        row.load(g, v);
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            w[j] = c + lane < g1 ? left(v[j], row.index(g) + j) : 0;
-            mine += w[j];
-        }
+        u64 mine = 0;
+        row.each(c + lane, min(g1, c + lane + 1), 1, [&](float l, int) { mine += left(l); });
         u64 upto = warp_before(mine, lane);
         const u64 sum = __shfl_sync(kFull, upto + mine, 31);
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            if (upto <= t && upto + w[j] > t) put(a, r, row.index(g) + j, w[j], total);
-            upto += w[j];
-        }
+        if (upto <= t && upto + mine > t)
+            row.each(c + lane, c + lane + 1, 1, [&](float l, int i) {
+                const u64 w = left(l);
+                if (upto <= t && upto + w > t) put(a, r, i, w, total);
+                upto += w;
+            });
         if (sum > t) break;
         t -= sum;
     }
@@ -821,15 +888,17 @@ template <typename T> cudaError_t launch(const SampleParams &p, cudaStream_t s) 
     const auto bytes = [&](int ctas) { return sizeof(Shared) + ((size_t)p.vocab / kPer / ctas + 3) * 16; };
     int ctas = 1;
     while (ctas < kMaxCtas && (bytes(ctas) > lim->smem_optin ||
-                               (p.n * ctas * 2 <= 2 * (int64_t)lim->sms && p.vocab >= 4096 * ctas)))
+                               (p.n * ctas * 2 <= MB_SAMPLE_CTAS * (int64_t)lim->sms && p.vocab >= 4096 * ctas)))
         ctas *= 2;
     const bool keep = bytes(ctas) <= lim->smem_optin;
-    const auto kern = ctas > 1 ? sample_long_kernel<T, true> : sample_long_kernel<T, false>;
+    const auto kern = !keep      ? sample_long_kernel<T, true, false>
+                      : ctas > 1 ? sample_long_kernel<T, true, true>
+                                 : sample_long_kernel<T, false, true>;
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)lim->smem_optin);
     if (e != cudaSuccess) return e;
     if (p.n > INT32_MAX / ctas) return cudaErrorInvalidValue;
     return launch_cluster(true, kern, dim3((unsigned)(p.n * ctas)), dim3(kThreads), ctas, keep ? bytes(ctas) : sizeof(Shared), s, p,
-                          bits, keep, ctas, p.n * ctas <= lim->sms);
+                          bits, ctas, p.n * ctas <= lim->sms);
 }
 
 }  // namespace

@@ -1,7 +1,7 @@
 """mb_sample against the definition in 64 bits (oracle/serve.py), row by row.
 
-Weights are within 2^-32 of their value, so the token is that of exact arithmetic unless u, top_p or min_p is within a few
-2^-32 (2^-30 here) of a border between two; the probability of a token is a quotient of two such, rounded to fp32 three
+Weights are within 2^-31 of their value, so the token is that of exact arithmetic unless u, top_p or min_p is within two
+such errors (2^-30, relative) of a border between two; the probability of a token is a quotient of two such, rounded to fp32 three
 times: 2^-22."""
 import itertools
 
