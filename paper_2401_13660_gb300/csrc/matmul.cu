@@ -30,6 +30,8 @@ constexpr int kSlots = 4;            // of the ring of scales
 constexpr int kSlotBytes = 512 + 1024;   // a tile's features, then 256 rows
 constexpr int kScaleColumns = 4 + 8;
 constexpr int kMaxSplit = 8;
+constexpr int kChunk = 16;           // rows of a sum that are moved to global memory at a time
+constexpr int kOutBuffers = 4;
 
 struct Tiles {
     int features, rows;       // tiles across
@@ -40,7 +42,7 @@ struct Tiles {
 };
 
 struct Args {
-    CUtensorMap a, w;
+    CUtensorMap a, w, out;
     MatmulParams p;
     Tiles t;
     int stride;               // bytes between rows of scales
@@ -67,6 +69,15 @@ __device__ __forceinline__ float4 cluster_load4(uint32_t address) {
     return v;
 }
 
+__device__ __forceinline__ void store4(float *p, const float4 &v) { *reinterpret_cast<float4 *>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16 *p, const float4 &v) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+    *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const unsigned *>(&a), *reinterpret_cast<const unsigned *>(&b));
+}
+
+// Among the four warps that move sums.
+__device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_constant__ Args g) {
     extern __shared__ unsigned char dyn[];
@@ -75,6 +86,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
     const Tiles &t = g.t;
     const uint32_t a_bytes = (uint32_t)t.height * kK, stage_bytes = kFeatures * kK + a_bytes;
     unsigned char *const scales = smem + (size_t)t.stages * stage_bytes;
+    T *const chunks = reinterpret_cast<T *>(scales + kSlots * kSlotBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)(blockIdx.x % (unsigned)t.split), first = (int)(blockIdx.x / (unsigned)t.split);
     const int step = (int)(gridDim.x / (unsigned)t.split), tiles = t.features * t.rows;
@@ -181,32 +193,43 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
             }
         }
     } else if (warp >= 4) {
-        int count = 0;
+        const int feature = (warp - 4) * 32 + lane;
+        const bool leads = threadIdx.x == 128;
+        int count = 0, moved = 0;
         for (int tile = first; tile < tiles && ok; tile += step, ++count) {
-            const int64_t n = (int64_t)(tile % t.features) * kFeatures + (warp - 4) * 32 + lane;
-            const int64_t m0 = (int64_t)(tile / t.features) * t.height;
+            const int n0 = tile % t.features * kFeatures, m0 = tile / t.features * t.height;
             if (!(ok = __all_sync(kFull, mbar_wait(&bar.sum_full[count & 1], count >> 1 & 1)))) break;
             tmem_fence_after();
             const uint32_t sum = tmem + (count & 1) * t.height + ((uint32_t)(warp - 4) * 32 << 16);
             const int rows = (int)(g.p.rows - m0 < t.height ? g.p.rows - m0 : t.height);
-            for (int c = 0; c < rows; c += 16) {
-                uint32_t v[16];
+            for (int c = 0; c < rows; c += kChunk) {
+                uint32_t v[kChunk];
                 tmem_load16(sum + c, v);
-                tmem_load_wait(v);
                 if (t.split > 1) {   // this CTA's part of the sum, where the ring was
-                    float *part = reinterpret_cast<float *>(smem) + c * kFeatures + (warp - 4) * 32 + lane;
+                    tmem_load_wait(v);
+                    float *part = reinterpret_cast<float *>(smem) + c * kFeatures + feature;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) part[j * kFeatures] = __uint_as_float(v[j]);
-                } else if (n < g.p.n_out) {
-                    T *o = out_at<T>(g.p, m0 + c, n);
+                    for (int j = 0; j < kChunk; ++j) part[j * kFeatures] = __uint_as_float(v[j]);
+                    continue;
+                }
+                T *chunk = chunks + moved++ % kOutBuffers * (kChunk * kFeatures);
+                if (leads) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kOutBuffers - 1) : "memory");
+                tmem_load_wait(v);
+                epilogue_sync();   // the chunk has been read
 #pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (c + j < rows) o[j * g.p.part] = from_f32<T>(__uint_as_float(v[j]));
+                for (int j = 0; j < kChunk; ++j) chunk[j * kFeatures + feature] = from_f32<T>(__uint_as_float(v[j]));
+                fence_proxy_async_smem();
+                epilogue_sync();
+                if (leads) {
+                    const int part = n0 / (int)g.p.part;
+                    tma_store_3d(&g.out, chunk, n0 - part * (int)g.p.part, m0 + c, part);
+                    bulk_commit();
                 }
             }
             tmem_fence_before();
             mbar_arrive(&bar.sum_empty[count & 1]);
         }
+        if (leads) bulk_wait_all();
     }
     if (!ok) report(g.p.status, MB_ERR_TIMEOUT, blockIdx.x);
     __syncthreads();
@@ -228,10 +251,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
                 if (s < t.split) {
                     v[0].x += v[s].x; v[0].y += v[s].y; v[0].z += v[s].z; v[0].w += v[s].w;
                 }
-            T *o = out_at<T>(g.p, m, n);
-            const float f[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] = from_f32<T>(f[j]);
+            store4(out_at<T>(g.p, m, n), v[0]);
         }
         cluster_arrive();   // nobody ends while its part is read
         cluster_wait();
@@ -256,16 +276,22 @@ cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t 
     t.split = 1;
     while (t.split < kMaxSplit && tiles * t.split * 2 <= lim->sms && t.blocks >= 4 * t.split) t.split *= 2;
     const int stage = (kFeatures + t.height) * kK;
-    const size_t room = lim->smem_optin - 1024 - sizeof(Barriers) - 64 - kSlots * kSlotBytes;
+    const int es = out_bf16 ? 2 : 4;
+    const size_t fixed = 1024 + kSlots * kSlotBytes + (size_t)kOutBuffers * kChunk * kFeatures * es;
+    const size_t room = lim->smem_optin - sizeof(Barriers) - 64 - fixed;
     t.stages = (int)(room / stage);
     if (t.stages > kMaxStages) t.stages = kMaxStages;
-    size_t smem = 1024 + (size_t)t.stages * stage + kSlots * kSlotBytes;
+    const size_t smem = fixed + (size_t)t.stages * stage;
     for (t.columns = 32; (int)t.columns < 2 * t.height + kScaleColumns; t.columns *= 2) {}
     const uint64_t wd[2] = {(uint64_t)p.width, (uint64_t)p.n_out}, ad[2] = {(uint64_t)p.width, (uint64_t)p.rows};
     const uint64_t st[1] = {(uint64_t)p.width};
     const uint32_t wb[2] = {kK, kFeatures}, ab[2] = {kK, (uint32_t)t.height};
     if (!encode_tmap(&g.w, p.w, 1, 2, wd, st, wb, 128) || !encode_tmap(&g.a, p.a, 1, 2, ad, st, ab, 128))
         return cudaErrorInvalidValue;
+    const uint64_t od[3] = {(uint64_t)p.part, (uint64_t)p.rows, (uint64_t)(p.n_out / p.part)};
+    const uint64_t os[2] = {(uint64_t)(p.part * es), (uint64_t)(p.rows * p.part * es)};
+    const uint32_t ob[3] = {kFeatures, kChunk, 1};
+    if (!encode_tmap(&g.out, p.out, es, 3, od, os, ob)) return cudaErrorInvalidValue;
     auto kern = out_bf16 ? matmul_q8_kernel<__nv_bfloat16> : matmul_q8_kernel<float>;
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(lim->smem_optin - sizeof(Barriers) - 64));
     if (e != cudaSuccess) return e;
