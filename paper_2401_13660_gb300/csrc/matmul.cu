@@ -23,12 +23,15 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kFeatures = 128;       // output features of a tile: lanes of tensor memory
-constexpr int kMaxRows = 240;        // rows of a tile: two sums and the scales fit 512 columns
+constexpr int kMaxRows = 240;        // rows of a tile: two sums and two sets of scales fit 512 columns
 constexpr int kK = kQuantBlock;      // columns of the sum in a stage
 constexpr int kMaxStages = 12;
 constexpr int kSlots = 4;            // of the ring of scales
 constexpr int kSlotBytes = 512 + 1024;   // a tile's features, then 256 rows
-constexpr int kScaleColumns = 4 + 8;
+constexpr int kScaleColumns = 4 + 8; // of one slot; two sets take turns
+#ifndef MB_PAIR_ROWS
+#define MB_PAIR_ROWS 1024
+#endif
 constexpr int kMaxSplit = 8;
 constexpr int kChunk = 16;           // rows of a sum that are moved to global memory at a time
 constexpr int kOutBuffers = 4;
@@ -55,6 +58,18 @@ struct Barriers {
     uint32_t tmem;
 };
 
+// A place in a ring of `size`, and how often it has been round.
+struct Ring {
+    int at = 0;
+    uint32_t round = 0;
+    __device__ __forceinline__ void next(int size) {
+        if (++at == size) {
+            at = 0;
+            round ^= 1;
+        }
+    }
+};
+
 template <typename T> __device__ __forceinline__ T *out_at(const MatmulParams &p, int64_t row, int64_t n) {
     const int64_t part = n / p.part;
     return static_cast<T *>(p.out) + (part * p.rows + row) * p.part + (n - part * p.part);
@@ -78,19 +93,26 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *p, const float4 &v) {
 // Among the four warps that move sums.
 __device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
-template <typename T>
+// kCtas: 1, or 2: a pair of CTAs shares a tile of 256 features, each with its 128 features and half of the rows.
+template <typename T, int kCtas>
 __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_constant__ Args g) {
     extern __shared__ unsigned char dyn[];
     __shared__ Barriers bar;
     unsigned char *const smem = dyn + ((1024u - (smem_u32(dyn) & 1023u)) & 1023u);
     const Tiles &t = g.t;
-    const uint32_t a_bytes = (uint32_t)t.height * kK, stage_bytes = kFeatures * kK + a_bytes;
+    constexpr int kWide = kCtas * kFeatures;
+    const int mine = t.height / kCtas;   // rows that this CTA loads
+    const uint32_t stage_bytes = (uint32_t)(kFeatures + mine) * kK;
     unsigned char *const scales = smem + (size_t)t.stages * stage_bytes;
     T *const chunks = reinterpret_cast<T *>(scales + kSlots * kSlotBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = (int)(blockIdx.x % (unsigned)t.split), first = (int)(blockIdx.x / (unsigned)t.split);
-    const int step = (int)(gridDim.x / (unsigned)t.split), tiles = t.features * t.rows;
+    const int half = kCtas == 2 ? (int)(blockIdx.x & 1u) : 0;
+    const int rank = kCtas == 2 ? 0 : (int)(blockIdx.x % (unsigned)t.split);
+    const int team = kCtas == 2 ? 2 : t.split;
+    const int first = (int)(blockIdx.x / (unsigned)team), step = (int)(gridDim.x / (unsigned)team), tiles = t.features * t.rows;
     const int k0 = (int)((int64_t)t.blocks * rank / t.split), k1 = (int)((int64_t)t.blocks * (rank + 1) / t.split);
+    // a barrier of the CTA that issues the products
+    const auto lead = [&](uint64_t *b) { return cluster_address(b, 0); };
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < t.stages; ++i) {
@@ -98,98 +120,117 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
             mbar_init(&bar.empty[i], 1);
         }
         for (int i = 0; i < kSlots; ++i) {
-            mbar_init(&bar.scales_full[i], 32);
+            mbar_init(&bar.scales_full[i], 32 * kCtas);
             mbar_init(&bar.scales_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bar.sum_full[i], 1);
-            mbar_init(&bar.sum_empty[i], 128);
+            mbar_init(&bar.sum_empty[i], 128 * kCtas);
         }
         fence_mbar_init();
         // this CTA's first weights are on their way to L2 while the kernel before drains
-        for (int k = k0; k < k1; ++k) tma_prefetch_2d(&g.w, k * kK, first % t.features * kFeatures);
+        for (int k = k0; k < k1; ++k) tma_prefetch_2d(&g.w, k * kK, first % t.features * kWide + half * kFeatures);
     }
-    if (warp == 0) tmem_alloc(&bar.tmem, t.columns);
+    if (warp == 0) tmem_alloc<kCtas>(&bar.tmem, t.columns);
     tmem_fence_before();
     __syncthreads();
+    if (kCtas == 2) {   // the other's barriers are there
+        cluster_arrive();
+        cluster_wait();
+    }
     tmem_fence_after();
-    const uint32_t tmem = bar.tmem, tmem_w = tmem + 2 * t.height, tmem_a = tmem_w + 4;
+    const uint32_t tmem = bar.tmem, tmem_scales = tmem + 2 * t.height;
     pdl_trigger();
     pdl_wait();
 
     bool ok = true;
     if (warp == 0) {
         if (lane == 0) {
+            Ring r;
             int issued = 0;
             for (int tile = first; tile < tiles && ok; tile += step) {
-                const int n0 = tile % t.features * kFeatures, m0 = tile / t.features * t.height;
-                for (int k = k0; k < k1; ++k, ++issued) {
-                    const int s = issued % t.stages;
-                    if (!(ok = mbar_wait(&bar.empty[s], (issued / t.stages & 1) ^ 1))) break;
-                    unsigned char *at = smem + (size_t)s * stage_bytes;
-                    mbar_arrive_expect_tx(&bar.full[s], stage_bytes);
-                    tma_load_2d(at, &g.w, &bar.full[s], k * kK, n0);
-                    tma_load_2d(at + kFeatures * kK, &g.a, &bar.full[s], k * kK, m0);
+                const int n0 = tile % t.features * kWide + half * kFeatures, m0 = tile / t.features * t.height + half * mine;
+                for (int k = k0; k < k1; ++k, ++issued, r.next(t.stages)) {
+                    uint64_t *const full = &bar.full[r.at];
+                    if (!(ok = mbar_wait(&bar.empty[r.at], r.round ^ 1))) break;
+                    unsigned char *at = smem + (uint32_t)r.at * stage_bytes;
+                    if (half == 0) mbar_arrive_expect_tx(full, kCtas * stage_bytes);
+                    if (kCtas == 1) {
+                        tma_load_2d(at, &g.w, full, k * kK, n0);
+                        tma_load_2d(at + kFeatures * kK, &g.a, full, k * kK, m0);
+                    } else {
+                        const uint32_t to = lead(full);
+                        tma_load_2d_pair(at, &g.w, to, k * kK, n0);
+                        tma_load_2d_pair(at + kFeatures * kK, &g.a, to, k * kK, m0);
+                    }
                 }
             }
-            // a failed CTA must not end with copies in flight
-            for (int i = issued > t.stages ? issued - t.stages : 0; !ok && i < issued; ++i)
+            // a failed CTA must not end with copies in flight (those of a pair arrive at the first of them)
+            for (int i = issued > t.stages ? issued - t.stages : 0; !ok && half == 0 && i < issued; ++i)
                 if (!mbar_wait(&bar.full[i % t.stages], i / t.stages & 1)) break;
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            int used = 0, group = 0, count = 0;
-            for (int tile = first; tile < tiles && ok; tile += step, ++count) {
-                const uint32_t sum = tmem + (count & 1) * t.height;
-                if (!(ok = mbar_wait(&bar.sum_empty[count & 1], (count >> 1 & 1) ^ 1))) break;
+        if (lane == 0 && half == 0) {
+            const auto wait = [](uint64_t *b, uint32_t parity) { return kCtas == 1 ? mbar_wait(b, parity) : mbar_wait_cluster(b, parity); };
+            const uint64_t desc = umma_desc_128(smem_u32(smem)), desc_scales = umma_desc_rows16(smem_u32(scales));
+            const uint32_t word0 = umma_word_q8(kWide, t.height, 0);
+            Ring r, slot, sums;   // stages; slots of scales; the two sums
+            uint32_t set = 0;
+            for (int tile = first; tile < tiles && ok; tile += step, sums.next(2)) {
+                const uint32_t sum = tmem + sums.at * t.height;
+                if (!(ok = wait(&bar.sum_empty[sums.at], sums.round ^ 1))) break;
                 tmem_fence_after();
-                for (int k = k0; k < k1; ++k, ++used) {
-                    const int slot = group % kSlots, s = used % t.stages;
+                for (int k = k0; k < k1; ++k, r.next(t.stages)) {
+                    const uint32_t tmem_w = tmem_scales + set * kScaleColumns, tmem_a = tmem_w + 4;
                     if (k == k0 || k % 4 == 0) {
-                        if (!(ok = mbar_wait(&bar.scales_full[slot], group / kSlots & 1))) break;
-                        const uint32_t at = smem_u32(scales) + slot * kSlotBytes;
-                        tmem_copy_scales(tmem_w, umma_desc_rows16(at));
-                        tmem_copy_scales(tmem_a, umma_desc_rows16(at + 512));
-                        if (t.height > 128) tmem_copy_scales(tmem_a + 4, umma_desc_rows16(at + 1024));
+                        if (!(ok = wait(&bar.scales_full[slot.at], slot.round))) break;
+                        const uint64_t d = desc_scales + (uint32_t)slot.at * (kSlotBytes >> 4);
+                        tmem_copy_scales<kCtas>(tmem_w, d);
+                        tmem_copy_scales<kCtas>(tmem_a, d + (512 >> 4));
+                        if (t.height > 128) tmem_copy_scales<kCtas>(tmem_a + 4, d + (1024 >> 4));
                     }
-                    if (!(ok = mbar_wait(&bar.full[s], used / t.stages & 1))) break;
+                    if (!(ok = mbar_wait(&bar.full[r.at], r.round))) break;
                     tmem_fence_after();
-                    const uint32_t at = smem_u32(smem) + s * stage_bytes;
-                    const uint64_t dw = umma_desc_128(at), da = umma_desc_128(at + kFeatures * kK);
-                    const uint32_t word = umma_word_q8(kFeatures, t.height, k % 4);
+                    const uint64_t dw = desc + (uint32_t)r.at * (stage_bytes >> 4), da = dw + (kFeatures * kK >> 4);
+                    const uint32_t word = word0 | (uint32_t)(k & 3) << 4 | (uint32_t)(k & 3) << 29;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) umma_q8(sum, dw + 2 * j, da + 2 * j, word, tmem_w, tmem_a, k > k0 || j > 0);
-                    umma_commit(&bar.empty[s]);
+                    for (int j = 0; j < 4; ++j)
+                        umma_q8<kCtas>(sum, dw + 2 * j, da + 2 * j, word, tmem_w, tmem_a, k > k0 || j > 0);
+                    umma_commit<kCtas>(&bar.empty[r.at]);
                     if (k == k1 - 1 || k % 4 == 3) {
-                        umma_commit(&bar.scales_empty[slot]);
-                        ++group;
+                        umma_commit<kCtas>(&bar.scales_empty[slot.at]);
+                        slot.next(kSlots);
+                        set ^= 1;
                     }
                 }
-                if (ok) umma_commit(&bar.sum_full[count & 1]);
+                if (ok) umma_commit<kCtas>(&bar.sum_full[sums.at]);
             }
         }
     } else if (warp == 2) {
         int group = 0;
+        const int blocks = (int)((g.p.n_out + kFeatures - 1) / kFeatures);
         for (int tile = first; tile < tiles && ok; tile += step) {
-            const int n0 = tile % t.features, m0 = tile / t.features * t.height;
+            const int block = tile % t.features * kCtas + half, m0 = tile / t.features * t.height;
             for (int q = k0 / 4; q <= (k1 - 1) / 4; ++q, ++group) {
                 const int slot = group % kSlots;
                 if (!(ok = __all_sync(kFull, mbar_wait(&bar.scales_empty[slot], (group / kSlots & 1) ^ 1)))) break;
-                const uint32_t w = *reinterpret_cast<const uint32_t *>(g.p.w_scales + (int64_t)n0 * g.stride + 4 * q);
+                const uint32_t w = block < blocks ? *reinterpret_cast<const uint32_t *>(g.p.w_scales + (int64_t)block * g.stride + 4 * q)
+                                                  : 0x7f7f7f7fu;
                 uint4 *at = reinterpret_cast<uint4 *>(scales + slot * kSlotBytes);
                 at[lane] = make_uint4(w, w, w, w);
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
+                for (int part = 0; part < 2; ++part) {
                     uint32_t v[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const int64_t row = m0 + 128 * half + 32 * j + lane;
+                        const int64_t row = m0 + 128 * part + 32 * j + lane;
                         v[j] = row < g.p.rows ? *reinterpret_cast<const uint32_t *>(g.p.a_scales + row * g.stride + 4 * q) : 0x7f7f7f7fu;
                     }
-                    at[32 + 32 * half + lane] = make_uint4(v[0], v[1], v[2], v[3]);
+                    at[32 + 32 * part + lane] = make_uint4(v[0], v[1], v[2], v[3]);
                 }
                 fence_proxy_async_smem();
-                mbar_arrive(&bar.scales_full[slot]);
+                if (kCtas == 1) mbar_arrive(&bar.scales_full[slot]);
+                else mbar_arrive_cluster(lead(&bar.scales_full[slot]));
             }
         }
     } else if (warp >= 4) {
@@ -197,15 +238,15 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
         const bool leads = threadIdx.x == 128;
         int count = 0, moved = 0;
         for (int tile = first; tile < tiles && ok; tile += step, ++count) {
-            const int n0 = tile % t.features * kFeatures, m0 = tile / t.features * t.height;
+            const int n0 = tile % t.features * kWide + half * kFeatures, m0 = tile / t.features * t.height;
             if (!(ok = __all_sync(kFull, mbar_wait(&bar.sum_full[count & 1], count >> 1 & 1)))) break;
             tmem_fence_after();
             const uint32_t sum = tmem + (count & 1) * t.height + ((uint32_t)(warp - 4) * 32 << 16);
-            const int rows = (int)(g.p.rows - m0 < t.height ? g.p.rows - m0 : t.height);
+            const int rows = n0 >= g.p.n_out ? 0 : (int)(g.p.rows - m0 < t.height ? g.p.rows - m0 : t.height);
             for (int c = 0; c < rows; c += kChunk) {
                 uint32_t v[kChunk];
                 tmem_load16(sum + c, v);
-                if (t.split > 1) {   // this CTA's part of the sum, where the ring was
+                if (kCtas == 1 && t.split > 1) {   // this CTA's part of the sum, where the ring was
                     tmem_load_wait(v);
                     float *part = reinterpret_cast<float *>(smem) + c * kFeatures + feature;
 #pragma unroll
@@ -227,13 +268,14 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
                 }
             }
             tmem_fence_before();
-            mbar_arrive(&bar.sum_empty[count & 1]);
+            if (kCtas == 1) mbar_arrive(&bar.sum_empty[count & 1]);
+            else mbar_arrive_cluster(lead(&bar.sum_empty[count & 1]));
         }
         if (leads) bulk_wait_all();
     }
     if (!ok) report(g.p.status, MB_ERR_TIMEOUT, blockIdx.x);
     __syncthreads();
-    if (t.split > 1) {   // the parts in the order of their ranks, every CTA for its share of the rows
+    if (kCtas == 1 && t.split > 1) {   // the parts in the order of their ranks, every CTA for its share of the rows
         cluster_arrive();
         cluster_wait();
         const int64_t m0 = (int64_t)(first / t.features) * t.height, n0 = (int64_t)(first % t.features) * kFeatures;
@@ -256,7 +298,11 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
         cluster_arrive();   // nobody ends while its part is read
         cluster_wait();
     }
-    if (warp == 0) tmem_free(tmem, t.columns);
+    if (kCtas == 2) {   // nobody ends while the other's products and arrivals are under way
+        cluster_arrive();
+        cluster_wait();
+    }
+    if (warp == 0) tmem_free<kCtas>(tmem, t.columns);
 }
 
 }  // namespace
@@ -268,35 +314,40 @@ cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t 
     g.p = p;
     g.stride = (int)quant_stride(p.width);
     Tiles &t = g.t;
-    t.features = (int)((p.n_out + kFeatures - 1) / kFeatures);
-    t.rows = (int)((p.rows + kMaxRows - 1) / kMaxRows);
-    t.height = (int)(((p.rows + t.rows - 1) / t.rows + 15) / 16 * 16);
+    const bool pair = p.rows > MB_PAIR_ROWS && p.n_out > kFeatures;
+    const int ctas = pair ? 2 : 1;
+    t.features = (int)((p.n_out + ctas * kFeatures - 1) / (ctas * kFeatures));
+    const int grain = 16 * ctas, most_rows = kMaxRows / grain * grain;   // a pair takes rows by 32
+    t.rows = (int)((p.rows + most_rows - 1) / most_rows);
+    t.height = (int)(((p.rows + t.rows - 1) / t.rows + grain - 1) / grain * grain);
     t.blocks = (int)((p.width + kK - 1) / kK);
     const int64_t tiles = (int64_t)t.features * t.rows;
     t.split = 1;
-    while (t.split < kMaxSplit && tiles * t.split * 2 <= lim->sms && t.blocks >= 4 * t.split) t.split *= 2;
-    const int stage = (kFeatures + t.height) * kK;
+    while (!pair && t.split < kMaxSplit && tiles * t.split * 2 <= lim->sms && t.blocks >= 4 * t.split) t.split *= 2;
+    const int stage = (kFeatures + t.height / ctas) * kK;
     const int es = out_bf16 ? 2 : 4;
     const size_t fixed = 1024 + kSlots * kSlotBytes + (size_t)kOutBuffers * kChunk * kFeatures * es;
     const size_t room = lim->smem_optin - sizeof(Barriers) - 64 - fixed;
     t.stages = (int)(room / stage);
     if (t.stages > kMaxStages) t.stages = kMaxStages;
     const size_t smem = fixed + (size_t)t.stages * stage;
-    for (t.columns = 32; (int)t.columns < 2 * t.height + kScaleColumns; t.columns *= 2) {}
+    for (t.columns = 32; (int)t.columns < 2 * t.height + 2 * kScaleColumns; t.columns *= 2) {}
     const uint64_t wd[2] = {(uint64_t)p.width, (uint64_t)p.n_out}, ad[2] = {(uint64_t)p.width, (uint64_t)p.rows};
     const uint64_t st[1] = {(uint64_t)p.width};
-    const uint32_t wb[2] = {kK, kFeatures}, ab[2] = {kK, (uint32_t)t.height};
+    const uint32_t wb[2] = {kK, kFeatures}, ab[2] = {kK, (uint32_t)(t.height / ctas)};
     if (!encode_tmap(&g.w, p.w, 1, 2, wd, st, wb, 128) || !encode_tmap(&g.a, p.a, 1, 2, ad, st, ab, 128))
         return cudaErrorInvalidValue;
     const uint64_t od[3] = {(uint64_t)p.part, (uint64_t)p.rows, (uint64_t)(p.n_out / p.part)};
     const uint64_t os[2] = {(uint64_t)(p.part * es), (uint64_t)(p.rows * p.part * es)};
     const uint32_t ob[3] = {kFeatures, kChunk, 1};
     if (!encode_tmap(&g.out, p.out, es, 3, od, os, ob)) return cudaErrorInvalidValue;
-    auto kern = out_bf16 ? matmul_q8_kernel<__nv_bfloat16> : matmul_q8_kernel<float>;
+    const auto kern = pair ? (out_bf16 ? matmul_q8_kernel<__nv_bfloat16, 2> : matmul_q8_kernel<float, 2>)
+                           : (out_bf16 ? matmul_q8_kernel<__nv_bfloat16, 1> : matmul_q8_kernel<float, 1>);
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(lim->smem_optin - sizeof(Barriers) - 64));
     if (e != cudaSuccess) return e;
-    const int64_t grid = t.split > 1 ? tiles * t.split : tiles < lim->sms ? tiles : lim->sms;
-    return launch_cluster(true, kern, dim3((unsigned)grid), dim3(kThreads), t.split, smem, s, g);
+    const int team = pair ? 2 : t.split;
+    const int64_t most = lim->sms / team, teams = t.split > 1 || tiles < most ? tiles : most;
+    return launch_cluster(true, kern, dim3((unsigned)(teams * team)), dim3(kThreads), team, smem, s, g);
 }
 
 }  // namespace mbscan

@@ -9,23 +9,40 @@
 
 namespace mbscan {
 
-// Columns are allocated by one warp, 32 to 512 at a time (a power of two), and freed by it.
-__device__ __forceinline__ void tmem_alloc(uint32_t *address, uint32_t columns) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(address)), "r"(columns)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+// kCtas: 1, or 2 for a pair of CTAs (a cluster of two) that work on one product, each with half of both operands in its
+// shared memory and its half of the lanes of the sum in its tensor memory. Copies and products of a pair are issued by the
+// first of them. A kernel uses one of the two throughout.
+
+// Columns are allocated by one warp (of each CTA), 32 to 512 at a time (a power of two), and freed by it.
+template <int kCtas> __device__ __forceinline__ void tmem_alloc(uint32_t *address, uint32_t columns) {
+    if constexpr (kCtas == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(address)), "r"(columns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(address)), "r"(columns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
 }
-__device__ __forceinline__ void tmem_free(uint32_t address, uint32_t columns) {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(address), "r"(columns));
+template <int kCtas> __device__ __forceinline__ void tmem_free(uint32_t address, uint32_t columns) {
+    if constexpr (kCtas == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(address), "r"(columns));
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(address), "r"(columns));
 }
 
 // Order of this thread's tcgen05 operations against those of threads it synchronises with (before, after that).
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// Arrive on `bar` once every product and copy that this thread has issued is done.
-__device__ __forceinline__ void umma_commit(uint64_t *bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+// Arrive on `bar` (of both CTAs of a pair) once every product and copy that this thread has issued is done.
+template <int kCtas> __device__ __forceinline__ void umma_commit(uint64_t *bar) {
+    if constexpr (kCtas == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                         smem_u32(bar)),
+                     "h"((uint16_t)3)
+                     : "memory");
 }
 
 // Descriptor of an operand in shared memory whose rows are 128 bytes of the sum's dimension, swizzled as a
@@ -39,10 +56,11 @@ __device__ __forceinline__ uint64_t umma_desc_rows16(uint32_t smem) {
     return (uint64_t)((smem & 0x3ffffu) >> 4) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
 }
 
-// Copy 32 rows of 16 bytes to four columns of tensor memory, row l to lane l of each of the four quarters of the lanes.
-// In order with this thread's products.
-__device__ __forceinline__ void tmem_copy_scales(uint32_t column, uint64_t desc) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(column), "l"(desc) : "memory");
+// Copy 32 rows of 16 bytes to four columns of tensor memory, row l to lane l of each of the four quarters of the lanes (in
+// each CTA of a pair, from its own shared memory). In order with this thread's products.
+template <int kCtas> __device__ __forceinline__ void tmem_copy_scales(uint32_t column, uint64_t desc) {
+    if constexpr (kCtas == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(column), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(column), "l"(desc) : "memory");
 }
 
 // Instruction word of a product of e4m3 operands, both with the sum's dimension innermost, m x n, with e8m0 scales. The
@@ -51,16 +69,54 @@ __device__ __forceinline__ uint32_t umma_word_q8(uint32_t m, uint32_t n, uint32_
     return scale << 4 | (n >> 3) << 17 | 1u << 23 | (m >> 4) << 24 | scale << 29;
 }
 
-// d (+)= (A sA)(B sB)^T over 32 columns of the sum: row i of A is lane i, row j of B column j of d. Scales of row r are in
-// lane r % 32 (of every quarter) of column r / 32. Issued by one thread.
+// d (+)= (A sA)(B sB)^T over 32 columns of the sum: row i of A is lane i (of a pair: 128 of 256 rows to a CTA), row j of B
+// column j of d (a pair: half of the rows of B in each CTA, all columns in both). Scales of row r are in lane r % 32 (of every
+// quarter) of column r / 32 (a pair: those of a CTA's own rows of A, of all rows of B). Issued by one thread.
+template <int kCtas>
 __device__ __forceinline__ void umma_q8(uint32_t d, uint64_t a, uint64_t b, uint32_t word, uint32_t a_scales, uint32_t b_scales,
                                         bool add) {
+    if constexpr (kCtas == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(word), "r"(a_scales), "r"(b_scales), "r"((uint32_t)add)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(word), "r"(a_scales), "r"(b_scales), "r"((uint32_t)add)
+            : "memory");
+}
+
+// A 2-D tile to this CTA's shared memory, completing on a barrier of either CTA of a pair (cluster_address).
+__device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *map, uint32_t bar, int x, int y) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(word), "r"(a_scales), "r"(b_scales), "r"((uint32_t)add)
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(
+            smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y)
         : "memory");
+}
+// Arrive on a barrier of another CTA of the cluster, and wait for such arrivals: what was written before is visible after.
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_wait_cluster(uint64_t *bar, uint32_t parity) {
+    const long long t0 = clock64();
+    for (;;) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(smem_u32(bar)), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if (clock64() - t0 > kWaitCycles) return false;
+    }
 }
 
 // 16 columns of this warp's quarter of the lanes (the address's lane: 32 * (warp % 4)); wait before they are used.

@@ -41,7 +41,8 @@ def _check(a, sa, w, sw, out, dtype):
 @pytest.mark.parametrize("rows, n, width", [
     (1, 8, 16), (1, 128, 128), (16, 128, 128), (17, 136, 144), (1, 1024, 1024), (5, 264, 512), (128, 256, 640), (129, 256, 384),
     (240, 128, 256), (241, 128, 256), (255, 1000, 400), (256, 512, 2304), (1003, 520, 1552), (3, 4608, 64), (500, 8, 4608),
-    (2, 2304, 4608), (64, 2304, 4608), (33, 128, 8192)])
+    (2, 2304, 4608), (64, 2304, 4608), (33, 128, 8192),
+    (1025, 264, 272), (1500, 136, 640), (2047, 1032, 1040), (4100, 512, 128), (1200, 2304, 512)])
 def test_product(rows, n, width, dtype):
     a, sa = _matrix(rows, width, 1, 1)
     w, sw = _matrix(n, width, 128, 2)
