@@ -145,15 +145,15 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
 
     bool ok = true;
     if (warp == 0) {
-        if (lane == 0) {
-            Ring r;
-            int issued = 0;
-            for (int tile = first; tile < tiles && ok; tile += step) {
-                const int n0 = tile % t.features * kWide + half * kFeatures, m0 = tile / t.features * t.height + half * mine;
-                for (int k = k0; k < k1; ++k, ++issued, r.next(t.stages)) {
-                    uint64_t *const full = &bar.full[r.at];
-                    if (!(ok = mbar_wait(&bar.empty[r.at], r.round ^ 1))) break;
-                    unsigned char *at = smem + (uint32_t)r.at * stage_bytes;
+        Ring r;
+        int issued = 0;
+        for (int tile = first; tile < tiles && ok; tile += step) {
+            const int n0 = tile % t.features * kWide + half * kFeatures, m0 = tile / t.features * t.height + half * mine;
+            for (int k = k0; k < k1; ++k, ++issued, r.next(t.stages)) {
+                uint64_t *const full = &bar.full[r.at];
+                if (!(ok = __all_sync(kFull, mbar_wait(&bar.empty[r.at], r.round ^ 1)))) break;
+                unsigned char *at = smem + (uint32_t)r.at * stage_bytes;
+                if (elect_one()) {
                     if (half == 0) mbar_arrive_expect_tx(full, kCtas * stage_bytes);
                     if (kCtas == 1) {
                         tma_load_2d(at, &g.w, full, k * kK, n0);
@@ -165,54 +165,58 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
                     }
                 }
             }
-            // a failed CTA must not end with copies in flight (those of a pair arrive at the first of them)
-            for (int i = issued > t.stages ? issued - t.stages : 0; !ok && half == 0 && i < issued; ++i)
-                if (!mbar_wait(&bar.full[i % t.stages], i / t.stages & 1)) break;
         }
-    } else if (warp == 1) {
-        if (lane == 0 && half == 0) {
-            const auto wait = [](uint64_t *b, uint32_t parity) { return kCtas == 1 ? mbar_wait(b, parity) : mbar_wait_cluster(b, parity); };
-            const uint64_t desc = umma_desc_128(smem_u32(smem)), desc_scales = umma_desc_rows16(smem_u32(scales));
-            const uint32_t word0 = umma_word_q8(kWide, t.height, 0);
-            Ring r, slot, sums;   // stages; slots of scales; the two sums
-            uint32_t set = 0;
-            for (int tile = first; tile < tiles && ok; tile += step, sums.next(2)) {
-                const uint32_t sum = tmem + sums.at * t.height;
-                if (!(ok = wait(&bar.sum_empty[sums.at], sums.round ^ 1))) break;
+        // a failed CTA must not end with copies in flight (those of a pair arrive at the first of them)
+        for (int i = issued > t.stages ? issued - t.stages : 0; !ok && half == 0 && i < issued; ++i)
+            if (!mbar_wait(&bar.full[i % t.stages], i / t.stages & 1)) break;
+    } else if (warp == 1 && half == 0) {
+        const auto wait = [](uint64_t *b, uint32_t parity) {
+            return (bool)__all_sync(kFull, kCtas == 1 ? mbar_wait(b, parity) : mbar_wait_cluster(b, parity));
+        };
+        const uint64_t desc = umma_desc_128(smem_u32(smem)), desc_scales = umma_desc_rows16(smem_u32(scales));
+        const uint32_t word0 = umma_word_q8(kWide, t.height, 0);
+        Ring r, slot, sums;   // stages; slots of scales; the two sums
+        uint32_t set = 0;
+        for (int tile = first; tile < tiles && ok; tile += step, sums.next(2)) {
+            const uint32_t sum = tmem + sums.at * t.height;
+            if (!(ok = wait(&bar.sum_empty[sums.at], sums.round ^ 1))) break;
+            tmem_fence_after();
+            for (int k = k0; k < k1; ++k, r.next(t.stages)) {
+                const uint32_t tmem_w = tmem_scales + set * kScaleColumns, tmem_a = tmem_w + 4;
+                const bool begins = k == k0 || k % 4 == 0, ends = k == k1 - 1 || k % 4 == 3;   // with this slot
+                if (begins && !(ok = wait(&bar.scales_full[slot.at], slot.round))) break;
+                if (!(ok = __all_sync(kFull, mbar_wait(&bar.full[r.at], r.round)))) break;
                 tmem_fence_after();
-                for (int k = k0; k < k1; ++k, r.next(t.stages)) {
-                    const uint32_t tmem_w = tmem_scales + set * kScaleColumns, tmem_a = tmem_w + 4;
-                    if (k == k0 || k % 4 == 0) {
-                        if (!(ok = wait(&bar.scales_full[slot.at], slot.round))) break;
-                        const uint64_t d = desc_scales + (uint32_t)slot.at * (kSlotBytes >> 4);
-                        tmem_copy_scales<kCtas>(tmem_w, d);
-                        tmem_copy_scales<kCtas>(tmem_a, d + (512 >> 4));
-                        if (t.height > 128) tmem_copy_scales<kCtas>(tmem_a + 4, d + (1024 >> 4));
+                const uint64_t dw = desc + (uint32_t)r.at * (stage_bytes >> 4), da = dw + (kFeatures * kK >> 4);
+                const uint64_t ds = desc_scales + (uint32_t)slot.at * (kSlotBytes >> 4);
+                const uint32_t word = word0 | (uint32_t)(k & 3) << 4 | (uint32_t)(k & 3) << 29;
+                if (elect_one()) {
+                    if (begins) {
+                        tmem_copy_scales<kCtas>(tmem_w, ds);
+                        tmem_copy_scales<kCtas>(tmem_a, ds + (512 >> 4));
+                        if (t.height > 128) tmem_copy_scales<kCtas>(tmem_a + 4, ds + (1024 >> 4));
                     }
-                    if (!(ok = mbar_wait(&bar.full[r.at], r.round))) break;
-                    tmem_fence_after();
-                    const uint64_t dw = desc + (uint32_t)r.at * (stage_bytes >> 4), da = dw + (kFeatures * kK >> 4);
-                    const uint32_t word = word0 | (uint32_t)(k & 3) << 4 | (uint32_t)(k & 3) << 29;
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         umma_q8<kCtas>(sum, dw + 2 * j, da + 2 * j, word, tmem_w, tmem_a, k > k0 || j > 0);
                     umma_commit<kCtas>(&bar.empty[r.at]);
-                    if (k == k1 - 1 || k % 4 == 3) {
-                        umma_commit<kCtas>(&bar.scales_empty[slot.at]);
-                        slot.next(kSlots);
-                        set ^= 1;
-                    }
+                    if (ends) umma_commit<kCtas>(&bar.scales_empty[slot.at]);
+                    if (k == k1 - 1) umma_commit<kCtas>(&bar.sum_full[sums.at]);
                 }
-                if (ok) umma_commit<kCtas>(&bar.sum_full[sums.at]);
+                if (ends) {
+                    slot.next(kSlots);
+                    set ^= 1;
+                }
             }
         }
-    } else if (warp == 2) {
+    } else if (warp == 2 || warp == 3) {   // words in turn
         int group = 0;
         const int blocks = (int)((g.p.n_out + kFeatures - 1) / kFeatures);
         for (int tile = first; tile < tiles && ok; tile += step) {
             const int block = tile % t.features * kCtas + half, m0 = tile / t.features * t.height;
             for (int q = k0 / 4; q <= (k1 - 1) / 4; ++q, ++group) {
                 const int slot = group % kSlots;
+                if ((group & 1) != warp - 2) continue;
                 if (!(ok = __all_sync(kFull, mbar_wait(&bar.scales_empty[slot], (group / kSlots & 1) ^ 1)))) break;
                 const uint32_t w = block < blocks ? *reinterpret_cast<const uint32_t *>(g.p.w_scales + (int64_t)block * g.stride + 4 * q)
                                                   : 0x7f7f7f7fu;

@@ -30,6 +30,18 @@ template <int kCtas> __device__ __forceinline__ void tmem_free(uint32_t address,
     else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(address), "r"(columns));
 }
 
+// One lane of a whole warp, always the same. What it guards is known to run in one thread: under `lane == 0` the operands of
+// products, which live in registers of the warp, cost several times as much.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(one));
+    return one != 0;
+}
+
 // Order of this thread's tcgen05 operations against those of threads it synchronises with (before, after that).
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
