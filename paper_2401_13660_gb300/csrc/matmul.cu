@@ -8,9 +8,9 @@
 // 240 of them, the columns of the sum in tensor memory): one row costs an eighth of a tile then, not 127 idle lanes, and a
 // decode step streams each weight through one tile.
 //
-// Eight warps: one issues the TMA copies of both operands into a ring of stages (128 columns of the sum each, 128-byte
-// swizzle), one the products, one lays out scales for the tensor core (512 columns' worth at a time: the four scales of a
-// word go to one column of tensor memory), and four move finished sums to global memory while the next tile's products run
+// Twelve warps: one issues the TMA copies of both operands into a ring of stages (128 columns of the sum each, 128-byte
+// swizzle), one the products, two lay out scales for the tensor core (512 columns' worth at a time: the four scales of a
+// word go to one column of tensor memory), and eight move finished sums to global memory while the next tile's products run
 // into the other half of tensor memory. CTAs take tiles in turn. Where tiles are few, a cluster of CTAs shares each tile's
 // sum, every one over part of it, and they add their parts up in order through distributed shared memory.
 #include "../../include/mbscan.h"
@@ -21,7 +21,8 @@
 namespace mbscan {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kGroups = 2;           // of four warps that move sums, chunks in turn
+constexpr int kThreads = 128 + 128 * kGroups;
 constexpr int kFeatures = 128;       // output features of a tile: lanes of tensor memory
 constexpr int kMaxRows = 240;        // rows of a tile: two sums and two sets of scales fit 512 columns
 constexpr int kK = kQuantBlock;      // columns of the sum in a stage
@@ -33,8 +34,8 @@ constexpr int kScaleColumns = 4 + 8; // of one slot; two sets take turns
 #define MB_PAIR_ROWS 1024
 #endif
 constexpr int kMaxSplit = 8;
-constexpr int kChunk = 16;           // rows of a sum that are moved to global memory at a time
-constexpr int kOutBuffers = 4;
+constexpr int kChunk = 32;           // rows of a sum that are moved to global memory at a time, in two stores
+template <typename T> constexpr int kOutBuffers = 4 / (int)sizeof(T);   // of a group
 
 struct Tiles {
     int features, rows;       // tiles across
@@ -90,8 +91,8 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *p, const float4 &v) {
     *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const unsigned *>(&a), *reinterpret_cast<const unsigned *>(&b));
 }
 
-// Among the four warps that move sums.
-__device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+// Among the four warps of a group that moves sums.
+__device__ __forceinline__ void group_sync(int group) { asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory"); }
 
 // kCtas: 1, or 2: a pair of CTAs shares a tile of 256 features, each with its 128 features and half of the rows.
 template <typename T, int kCtas>
@@ -125,9 +126,10 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bar.sum_full[i], 1);
-            mbar_init(&bar.sum_empty[i], 128 * kCtas);
+            mbar_init(&bar.sum_empty[i], 128 * kGroups * kCtas);
         }
         fence_mbar_init();
+        for (const CUtensorMap *m : {&g.a, &g.w, &g.out}) tma_prefetch_map(m);
         // this CTA's first weights are on their way to L2 while the kernel before drains
         for (int k = k0; k < k1; ++k) tma_prefetch_2d(&g.w, k * kK, first % t.features * kWide + half * kFeatures);
     }
@@ -238,42 +240,48 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
             }
         }
     } else if (warp >= 4) {
-        const int feature = (warp - 4) * 32 + lane;
-        const bool leads = threadIdx.x == 128;
-        int count = 0, moved = 0;
-        for (int tile = first; tile < tiles && ok; tile += step, ++count) {
+        const int feature = warp % 4 * 32 + lane, group = warp / 4 - 1;
+        const bool leads = threadIdx.x % 128 == 0;
+        T *const buffers = chunks + group * (kOutBuffers<T> * kChunk * kFeatures);
+        int moved = 0;
+        Ring sums;
+        for (int tile = first; tile < tiles && ok; tile += step, sums.next(2)) {
             const int n0 = tile % t.features * kWide + half * kFeatures, m0 = tile / t.features * t.height;
-            if (!(ok = __all_sync(kFull, mbar_wait(&bar.sum_full[count & 1], count >> 1 & 1)))) break;
+            if (!(ok = __all_sync(kFull, mbar_wait(&bar.sum_full[sums.at], sums.round)))) break;
             tmem_fence_after();
-            const uint32_t sum = tmem + (count & 1) * t.height + ((uint32_t)(warp - 4) * 32 << 16);
+            const uint32_t sum = tmem + sums.at * t.height + ((uint32_t)(warp % 4) * 32 << 16);
             const int rows = n0 >= g.p.n_out ? 0 : (int)(g.p.rows - m0 < t.height ? g.p.rows - m0 : t.height);
-            for (int c = 0; c < rows; c += kChunk) {
+            const int part = n0 / (int)g.p.part, x = n0 - part * (int)g.p.part;
+            for (int c = group * kChunk; c < rows; c += kGroups * kChunk) {
                 uint32_t v[kChunk];
-                tmem_load16(sum + c, v);
+                auto &v0 = *reinterpret_cast<uint32_t(*)[16]>(&v[0]), &v1 = *reinterpret_cast<uint32_t(*)[16]>(&v[16]);
+                tmem_load16(sum + c, v0);
+                tmem_load16(sum + (c + 16 < rows ? c + 16 : c), v1);
+                if (leads) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kOutBuffers<T> - 1) : "memory");
+                tmem_load_wait(v0);
+                tmem_load_wait(v1);
                 if (kCtas == 1 && t.split > 1) {   // this CTA's part of the sum, where the ring was
-                    tmem_load_wait(v);
-                    float *part = reinterpret_cast<float *>(smem) + c * kFeatures + feature;
+                    float *to = reinterpret_cast<float *>(smem) + c * kFeatures + feature;
 #pragma unroll
-                    for (int j = 0; j < kChunk; ++j) part[j * kFeatures] = __uint_as_float(v[j]);
+                    for (int j = 0; j < kChunk; ++j)
+                        if (j < 16 || c + 16 < t.height) to[j * kFeatures] = __uint_as_float(v[j]);
                     continue;
                 }
-                T *chunk = chunks + moved++ % kOutBuffers * (kChunk * kFeatures);
-                if (leads) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kOutBuffers - 1) : "memory");
-                tmem_load_wait(v);
-                epilogue_sync();   // the chunk has been read
+                T *chunk = buffers + moved++ % kOutBuffers<T> * (kChunk * kFeatures);
+                group_sync(group);   // the chunk has been read
 #pragma unroll
                 for (int j = 0; j < kChunk; ++j) chunk[j * kFeatures + feature] = from_f32<T>(__uint_as_float(v[j]));
                 fence_proxy_async_smem();
-                epilogue_sync();
+                group_sync(group);
                 if (leads) {
-                    const int part = n0 / (int)g.p.part;
-                    tma_store_3d(&g.out, chunk, n0 - part * (int)g.p.part, m0 + c, part);
+                    tma_store_3d(&g.out, chunk, x, m0 + c, part);
+                    if (c + 16 < rows) tma_store_3d(&g.out, chunk + 16 * kFeatures, x, m0 + c + 16, part);
                     bulk_commit();
                 }
             }
             tmem_fence_before();
-            if (kCtas == 1) mbar_arrive(&bar.sum_empty[count & 1]);
-            else mbar_arrive_cluster(lead(&bar.sum_empty[count & 1]));
+            if (kCtas == 1) mbar_arrive(&bar.sum_empty[sums.at]);
+            else mbar_arrive_cluster(lead(&bar.sum_empty[sums.at]));
         }
         if (leads) bulk_wait_all();
     }
@@ -330,7 +338,7 @@ cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t 
     while (!pair && t.split < kMaxSplit && tiles * t.split * 2 <= lim->sms && t.blocks >= 4 * t.split) t.split *= 2;
     const int stage = (kFeatures + t.height / ctas) * kK;
     const int es = out_bf16 ? 2 : 4;
-    const size_t fixed = 1024 + kSlots * kSlotBytes + (size_t)kOutBuffers * kChunk * kFeatures * es;
+    const size_t fixed = 1024 + kSlots * kSlotBytes + (size_t)kGroups * 4 * kChunk * kFeatures;
     const size_t room = lim->smem_optin - sizeof(Barriers) - 64 - fixed;
     t.stages = (int)(room / stage);
     if (t.stages > kMaxStages) t.stages = kMaxStages;
@@ -343,7 +351,7 @@ cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t 
         return cudaErrorInvalidValue;
     const uint64_t od[3] = {(uint64_t)p.part, (uint64_t)p.rows, (uint64_t)(p.n_out / p.part)};
     const uint64_t os[2] = {(uint64_t)(p.part * es), (uint64_t)(p.rows * p.part * es)};
-    const uint32_t ob[3] = {kFeatures, kChunk, 1};
+    const uint32_t ob[3] = {kFeatures, 16, 1};
     if (!encode_tmap(&g.out, p.out, es, 3, od, os, ob)) return cudaErrorInvalidValue;
     const auto kern = pair ? (out_bf16 ? matmul_q8_kernel<__nv_bfloat16, 2> : matmul_q8_kernel<float, 2>)
                            : (out_bf16 ? matmul_q8_kernel<__nv_bfloat16, 1> : matmul_q8_kernel<float, 1>);

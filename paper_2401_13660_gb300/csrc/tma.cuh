@@ -101,6 +101,11 @@ __device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, u
         : "memory");
 }
 
+// Fetch a tensor map ahead of its first use.
+__device__ __forceinline__ void tma_prefetch_map(const CUtensorMap *map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+}
+
 // Prefetch the 3-D (2-D) box from global memory into L2 (a hint: no
 // destination, no completion). L2 is where every kernel's writes land, so a
 // prefetch cannot make a later load see an older value.
