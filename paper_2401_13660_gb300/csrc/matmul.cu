@@ -18,30 +18,34 @@
 #include "common.cuh"
 #include "umma.cuh"
 
+#include <algorithm>
+#include <atomic>
+
 namespace mbscan {
 namespace {
 
 constexpr int kGroups = 2;           // of four warps that move sums, chunks in turn
 constexpr int kThreads = 128 + 128 * kGroups;
 constexpr int kFeatures = 128;       // output features of a tile: lanes of tensor memory
-constexpr int kMaxRows = 240;        // rows of a tile: two sums and two sets of scales fit 512 columns
+constexpr int kMaxRows = 224;        // rows of a tile: two sums and two sets of scales fit 512 columns
 constexpr int kK = kQuantBlock;      // columns of the sum in a stage
 constexpr int kMaxStages = 12;
 constexpr int kSlots = 4;            // of the ring of scales
-constexpr int kSlotBytes = 512 + 1024;   // a tile's features, then 256 rows
+constexpr int kSlotBytes = 512 + 1024;
+static_assert(kSlots * kSlotBytes % 1024 == 0, "what follows is swizzled");   // a tile's features, then 256 rows
 constexpr int kScaleColumns = 4 + 8; // of one slot; two sets take turns
-#ifndef MB_PAIR_ROWS
-#define MB_PAIR_ROWS 1024
-#endif
+constexpr int kPairRows = 384;       // more are for pairs of CTAs
 constexpr int kMaxSplit = 8;
-constexpr int kChunk = 32;           // rows of a sum that are moved to global memory at a time, in two stores
-template <typename T> constexpr int kOutBuffers = 4 / (int)sizeof(T);   // of a group
+constexpr int kChunk = 32;           // rows of a sum that are moved at a time
 
 struct Tiles {
     int features, rows;       // tiles across
     int height;               // rows of a tile, a multiple of 16
     int blocks;               // 128-column blocks of the sum
     int split, stages;
+    int held;                 // chunks that a group of warps holds in shared memory at a time
+    int sums;                 // in tensor memory: two, or one where no CTA has more than a tile
+    uint32_t ring;            // bytes of the ring of stages
     uint32_t columns;         // of tensor memory
 };
 
@@ -85,6 +89,10 @@ __device__ __forceinline__ float4 cluster_load4(uint32_t address) {
     return v;
 }
 
+__device__ __forceinline__ uint32_t bf16_pair(uint32_t lo, uint32_t hi) {   // of the bits of two floats
+    const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
 __device__ __forceinline__ void store4(float *p, const float4 &v) { *reinterpret_cast<float4 *>(p) = v; }
 __device__ __forceinline__ void store4(__nv_bfloat16 *p, const float4 &v) {
     const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
@@ -96,16 +104,17 @@ __device__ __forceinline__ void group_sync(int group) { asm volatile("bar.sync %
 
 // kCtas: 1, or 2: a pair of CTAs shares a tile of 256 features, each with its 128 features and half of the rows.
 template <typename T, int kCtas>
-__global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_constant__ Args g) {
+__global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_constant__ Args g) {
     extern __shared__ unsigned char dyn[];
     __shared__ Barriers bar;
     unsigned char *const smem = dyn + ((1024u - (smem_u32(dyn) & 1023u)) & 1023u);
-    const Tiles &t = g.t;
+    const Tiles t = g.t;   // in registers: a wait would have them read again
     constexpr int kWide = kCtas * kFeatures;
     const int mine = t.height / kCtas;   // rows that this CTA loads
     const uint32_t stage_bytes = (uint32_t)(kFeatures + mine) * kK;
-    unsigned char *const scales = smem + (size_t)t.stages * stage_bytes;
-    T *const chunks = reinterpret_cast<T *>(scales + kSlots * kSlotBytes);
+    unsigned char *const scales = smem + t.ring;
+    // 1024-byte aligned (swizzled); of a CTA's only tile, where the ring was
+    T *const chunks = reinterpret_cast<T *>(t.sums == 1 ? smem : scales + kSlots * kSlotBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int half = kCtas == 2 ? (int)(blockIdx.x & 1u) : 0;
     const int rank = kCtas == 2 ? 0 : (int)(blockIdx.x % (unsigned)t.split);
@@ -121,12 +130,12 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
             mbar_init(&bar.empty[i], 1);
         }
         for (int i = 0; i < kSlots; ++i) {
-            mbar_init(&bar.scales_full[i], 32 * kCtas);
+            mbar_init(&bar.scales_full[i], kCtas);
             mbar_init(&bar.scales_empty[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bar.sum_full[i], 1);
-            mbar_init(&bar.sum_empty[i], 128 * kGroups * kCtas);
+            mbar_init(&bar.sum_empty[i], 4 * kGroups * kCtas);
         }
         fence_mbar_init();
         for (const CUtensorMap *m : {&g.a, &g.w, &g.out}) tma_prefetch_map(m);
@@ -141,8 +150,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
         cluster_wait();
     }
     tmem_fence_after();
-    const uint32_t tmem = bar.tmem, tmem_scales = tmem + 2 * t.height;
-    pdl_trigger();
+    const uint32_t tmem = bar.tmem, tmem_scales = tmem + t.sums * t.height;
     pdl_wait();
 
     bool ok = true;
@@ -179,7 +187,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
         const uint32_t word0 = umma_word_q8(kWide, t.height, 0);
         Ring r, slot, sums;   // stages; slots of scales; the two sums
         uint32_t set = 0;
-        for (int tile = first; tile < tiles && ok; tile += step, sums.next(2)) {
+        for (int tile = first; tile < tiles && ok; tile += step, sums.next(t.sums)) {
             const uint32_t sum = tmem + sums.at * t.height;
             if (!(ok = wait(&bar.sum_empty[sums.at], sums.round ^ 1))) break;
             tmem_fence_after();
@@ -235,56 +243,96 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
                     at[32 + 32 * part + lane] = make_uint4(v[0], v[1], v[2], v[3]);
                 }
                 fence_proxy_async_smem();
-                if (kCtas == 1) mbar_arrive(&bar.scales_full[slot]);
-                else mbar_arrive_cluster(lead(&bar.scales_full[slot]));
+                __syncwarp();
+                if (lane == 0) {
+                    if (kCtas == 1) mbar_arrive(&bar.scales_full[slot]);
+                    else mbar_arrive_cluster(lead(&bar.scales_full[slot]));
+                }
             }
         }
     } else if (warp >= 4) {
         const int feature = warp % 4 * 32 + lane, group = warp / 4 - 1;
         const bool leads = threadIdx.x % 128 == 0;
-        T *const buffers = chunks + group * (kOutBuffers<T> * kChunk * kFeatures);
-        int moved = 0;
+        const bool whole = kCtas == 1 && t.split > 1;   // this CTA's part of the sum, where the ring was
+        T *const held = chunks + group * t.held * (kChunk * kFeatures);
+        // bf16: two halves of 64 features, rows of 128 bytes, their 16-byte pieces swizzled by the row
+        const int row = lane % 8;
+        const uint32_t mine_at = warp % 4 / 2 * (kChunk * 128) + row * 128 + ((warp % 2 * 4 + lane / 8) ^ row) * 16;
         Ring sums;
-        for (int tile = first; tile < tiles && ok; tile += step, sums.next(2)) {
+        for (int tile = first; tile < tiles && ok; tile += step, sums.next(t.sums)) {
             const int n0 = tile % t.features * kWide + half * kFeatures, m0 = tile / t.features * t.height;
             if (!(ok = __all_sync(kFull, mbar_wait(&bar.sum_full[sums.at], sums.round)))) break;
             tmem_fence_after();
             const uint32_t sum = tmem + sums.at * t.height + ((uint32_t)(warp % 4) * 32 << 16);
             const int rows = n0 >= g.p.n_out ? 0 : (int)(g.p.rows - m0 < t.height ? g.p.rows - m0 : t.height);
             const int part = n0 / (int)g.p.part, x = n0 - part * (int)g.p.part;
-            for (int c = group * kChunk; c < rows; c += kGroups * kChunk) {
-                uint32_t v[kChunk];
-                auto &v0 = *reinterpret_cast<uint32_t(*)[16]>(&v[0]), &v1 = *reinterpret_cast<uint32_t(*)[16]>(&v[16]);
-                tmem_load16(sum + c, v0);
-                tmem_load16(sum + (c + 16 < rows ? c + 16 : c), v1);
-                if (leads) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kOutBuffers<T> - 1) : "memory");
-                tmem_load_wait(v0);
-                tmem_load_wait(v1);
-                if (kCtas == 1 && t.split > 1) {   // this CTA's part of the sum, where the ring was
-                    float *to = reinterpret_cast<float *>(smem) + c * kFeatures + feature;
-#pragma unroll
-                    for (int j = 0; j < kChunk; ++j)
-                        if (j < 16 || c + 16 < t.height) to[j * kFeatures] = __uint_as_float(v[j]);
-                    continue;
+            // the sum has been read by this warp: before its stores, which take longer than the products may wait
+            const auto sum_read = [&] {
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (kCtas == 1) mbar_arrive(&bar.sum_empty[sums.at]);
+                    else mbar_arrive_cluster_relaxed(lead(&bar.sum_empty[sums.at]));
                 }
-                T *chunk = buffers + moved++ % kOutBuffers<T> * (kChunk * kFeatures);
-                group_sync(group);   // the chunk has been read
+            };
+            for (int c0 = group * kChunk; c0 < rows; c0 += t.held * kGroups * kChunk) {
+                const int c1 = min(rows, c0 + t.held * kGroups * kChunk);
+                if (!whole) {
+                    if (leads) bulk_wait_read_all();
+                    group_sync(group);   // what was held before has been read
+                }
+                T *chunk = held;
+                for (int c = c0; c < c1; c += kGroups * kChunk, chunk += kChunk * kFeatures) {
+                    uint32_t v0[16], v1[16];
+                    if (sizeof(T) == 2 && !whole) {
+                        tmem_load_fragments(sum + c, v0);
+                        tmem_load_fragments(sum + c + (16 << 16), v1);
+                    } else {
+                        tmem_load16(sum + c, v0);
+                        tmem_load16(sum + c + 16, v1);   // a tile of 16 rows: columns that are not used
+                    }
+                    tmem_load_wait(v0);
+                    tmem_load_wait(v1);
+                    if (whole) {
+                        float *to = reinterpret_cast<float *>(smem) + c * kFeatures + feature;
 #pragma unroll
-                for (int j = 0; j < kChunk; ++j) chunk[j * kFeatures + feature] = from_f32<T>(__uint_as_float(v[j]));
+                        for (int j = 0; j < 16; ++j) to[j * kFeatures] = __uint_as_float(v0[j]);
+                        if (c + 16 < t.height)
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) to[(16 + j) * kFeatures] = __uint_as_float(v1[j]);
+                    } else if (sizeof(T) == 2) {
+                        const uint32_t at = smem_u32(chunk) + mine_at;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            stsm_x4_trans(at + q * 1024, bf16_pair(v0[4 * q], v0[4 * q + 1]), bf16_pair(v0[4 * q + 2], v0[4 * q + 3]),
+                                          bf16_pair(v1[4 * q], v1[4 * q + 1]), bf16_pair(v1[4 * q + 2], v1[4 * q + 3]));
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            chunk[j * kFeatures + feature] = from_f32<T>(__uint_as_float(v0[j]));
+                            chunk[(16 + j) * kFeatures + feature] = from_f32<T>(__uint_as_float(v1[j]));
+                        }
+                    }
+                }
+                if (c0 + t.held * kGroups * kChunk >= rows) sum_read();
+                if (whole) continue;
                 fence_proxy_async_smem();
                 group_sync(group);
                 if (leads) {
-                    tma_store_3d(&g.out, chunk, x, m0 + c, part);
-                    if (c + 16 < rows) tma_store_3d(&g.out, chunk + 16 * kFeatures, x, m0 + c + 16, part);
+                    constexpr int kStore = sizeof(T) == 2 ? 64 : 128;   // features
+                    chunk = held;
+                    for (int c = c0; c < c1; c += kGroups * kChunk, chunk += kChunk * kFeatures)
+#pragma unroll
+                        for (int f = 0; f < kFeatures; f += kStore)
+                            if (n0 + f < g.p.n_out) tma_store_3d(&g.out, chunk + f * kChunk, x + f, m0 + c, part);
                     bulk_commit();
                 }
             }
-            tmem_fence_before();
-            if (kCtas == 1) mbar_arrive(&bar.sum_empty[sums.at]);
-            else mbar_arrive_cluster(lead(&bar.sum_empty[sums.at]));
+            if (group * kChunk >= rows) sum_read();   // nothing of it is this group's
         }
         if (leads) bulk_wait_all();
     }
+    pdl_trigger();   // not before: the next kernel's CTAs beside this one cost 1 x 1024 x 4096 0.5 us
     if (!ok) report(g.p.status, MB_ERR_TIMEOUT, blockIdx.x);
     __syncthreads();
     if (kCtas == 1 && t.split > 1) {   // the parts in the order of their ranks, every CTA for its share of the rows
@@ -317,6 +365,33 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_q8_kernel(const __grid_con
     if (warp == 0) tmem_free<kCtas>(tmem, t.columns);
 }
 
+// Clusters of so many CTAs that fit the current device with all the shared memory they can have, looked up once.
+int full_clusters(int size) {
+    constexpr int kDevices = 64;
+    static std::atomic<int> known[kDevices][kMaxSplit + 1];
+    int dev = 0, n = 0;
+    const DeviceLimits *lim = device_limits();
+    if (!lim || cudaGetDevice(&dev) != cudaSuccess || dev >= kDevices) return 0;
+    if ((n = known[dev][size].load(std::memory_order_relaxed)) > 0) return n;
+    const auto kern = matmul_q8_kernel<__nv_bfloat16, 1>;
+    const int smem = (int)(lim->smem_optin - sizeof(Barriers) - 64);
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)size;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)(size * lim->sms));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess)
+        return 0;
+    known[dev][size].store(n, std::memory_order_relaxed);
+    return n;
+}
+
 }  // namespace
 
 cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t s) {
@@ -326,24 +401,44 @@ cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t 
     g.p = p;
     g.stride = (int)quant_stride(p.width);
     Tiles &t = g.t;
-    const bool pair = p.rows > MB_PAIR_ROWS && p.n_out > kFeatures;
+    const bool pair = p.rows > kPairRows && p.n_out > kFeatures;
     const int ctas = pair ? 2 : 1;
     t.features = (int)((p.n_out + ctas * kFeatures - 1) / (ctas * kFeatures));
-    const int grain = 16 * ctas, most_rows = kMaxRows / grain * grain;   // a pair takes rows by 32
-    t.rows = (int)((p.rows + most_rows - 1) / most_rows);
-    t.height = (int)(((p.rows + t.rows - 1) / t.rows + grain - 1) / grain * grain);
+    // rows by 32, so that the stores of a tile end in it, or 16 rows alone
+    t.rows = (int)((p.rows + kMaxRows - 1) / kMaxRows);
+    t.height = p.rows <= 16 ? 16 : (int)(((p.rows + t.rows - 1) / t.rows + kChunk - 1) / kChunk * kChunk);
     t.blocks = (int)((p.width + kK - 1) / kK);
     const int64_t tiles = (int64_t)t.features * t.rows;
+    // Parts of a sum: what they cost is the rows of both operands that a CTA loads (128 bytes each, two cycles), and what a
+    // cluster costs over single CTAs, 1.3 us, and adding up. Microseconds without and with: 1 x 1024 x 4096 5.3, 5.6; 256 x
+    // 1024 x 2304 6.2, 8.7; 1 x 2048 x 1024 6.7, 5.2; 256 x 4608 x 2304 14.9, 10.4.
     t.split = 1;
-    while (!pair && t.split < kMaxSplit && tiles * t.split * 2 <= lim->sms && t.blocks >= 4 * t.split) t.split *= 2;
-    const int stage = (kFeatures + t.height / ctas) * kK;
-    const int es = out_bf16 ? 2 : 4;
-    const size_t fixed = 1024 + kSlots * kSlotBytes + (size_t)kGroups * 4 * kChunk * kFeatures;
-    const size_t room = lim->smem_optin - sizeof(Barriers) - 64 - fixed;
-    t.stages = (int)(room / stage);
-    if (t.stages > kMaxStages) t.stages = kMaxStages;
-    const size_t smem = fixed + (size_t)t.stages * stage;
-    for (t.columns = 32; (int)t.columns < 2 * t.height + 2 * kScaleColumns; t.columns *= 2) {}
+    const auto cost = [&](int split) {
+        return (int64_t)((t.blocks + split - 1) / split) * (kFeatures + t.height) + (split > 1 ? 1250 + 8 * t.height : 0);
+    };
+    for (int split = 2; !pair && split <= kMaxSplit && tiles * split <= lim->sms && split <= t.blocks; split *= 2)
+        if (cost(split) < cost(t.split)) t.split = split;
+    const int team = pair ? 2 : t.split;
+    const bool one = tiles <= lim->sms / team;   // tile to a CTA (or team)
+    const int stage = (kFeatures + t.height / ctas) * kK, share = (t.blocks + t.split - 1) / t.split;
+    const int es = out_bf16 ? 2 : 4, chunk = kChunk * kFeatures * es;
+    const int halves = ((t.height + kChunk - 1) / kChunk + kGroups - 1) / kGroups;   // chunks of a group of warps
+    // Of several tiles to a CTA all that a group moves of a sum in bf16 is held beside the ring, in fp32 half of it.
+    t.sums = one ? 1 : 2;
+    t.held = one || out_bf16 ? halves : (halves + 1) / 2;
+    const size_t fixed = 1024 + kSlots * kSlotBytes + (one ? 0 : (size_t)kGroups * t.held * chunk);
+    const size_t most = lim->smem_optin - sizeof(Barriers) - 64, beside = lim->smem_sm / 2 - lim->smem_reserved - sizeof(Barriers) - 64;
+    // as deep as it may be (256 x 2304 x 9216: 6 stages 10.7 us, 3 stages and room for the next kernel's CTA 12.8), but where
+    // the clusters would not fit the GPU side by side then, two CTAs to an SM (64 x 4608 x 2304: 14.1 -> 8.7 us)
+    const bool tight = t.split > 2 && tiles > full_clusters(t.split);
+    t.stages = std::min((int)(((tight ? beside : most) - fixed) / stage), kMaxStages);
+    if (one) t.stages = std::min(t.stages, share);
+    const size_t parts = one ? std::max((size_t)kGroups * t.held * chunk, t.split > 1 ? (size_t)t.height * kFeatures * 4 : 0) : 0;
+    t.ring = (uint32_t)((std::max((size_t)t.stages * stage, parts) + 1023) / 1024 * 1024);
+    // never three to an SM: half of its tensor memory each, CTAs of one tile never wait for columns while others of their
+    // cluster wait for them
+    const size_t smem = std::max(fixed + t.ring, lim->smem_sm / 3);
+    for (t.columns = 32; (int)t.columns < t.sums * t.height + 2 * kScaleColumns; t.columns *= 2) {}
     const uint64_t wd[2] = {(uint64_t)p.width, (uint64_t)p.n_out}, ad[2] = {(uint64_t)p.width, (uint64_t)p.rows};
     const uint64_t st[1] = {(uint64_t)p.width};
     const uint32_t wb[2] = {kK, kFeatures}, ab[2] = {kK, (uint32_t)(t.height / ctas)};
@@ -351,14 +446,13 @@ cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t 
         return cudaErrorInvalidValue;
     const uint64_t od[3] = {(uint64_t)p.part, (uint64_t)p.rows, (uint64_t)(p.n_out / p.part)};
     const uint64_t os[2] = {(uint64_t)(p.part * es), (uint64_t)(p.rows * p.part * es)};
-    const uint32_t ob[3] = {kFeatures, 16, 1};
-    if (!encode_tmap(&g.out, p.out, es, 3, od, os, ob)) return cudaErrorInvalidValue;
+    const uint32_t ob[3] = {out_bf16 ? 64u : 128u, kChunk, 1};
+    if (!encode_tmap(&g.out, p.out, es, 3, od, os, ob, out_bf16 ? 128 : 0)) return cudaErrorInvalidValue;
     const auto kern = pair ? (out_bf16 ? matmul_q8_kernel<__nv_bfloat16, 2> : matmul_q8_kernel<float, 2>)
                            : (out_bf16 ? matmul_q8_kernel<__nv_bfloat16, 1> : matmul_q8_kernel<float, 1>);
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(lim->smem_optin - sizeof(Barriers) - 64));
     if (e != cudaSuccess) return e;
-    const int team = pair ? 2 : t.split;
-    const int64_t most = lim->sms / team, teams = t.split > 1 || tiles < most ? tiles : most;
+    const int64_t teams = one ? tiles : lim->sms / team;
     return launch_cluster(true, kern, dim3((unsigned)(teams * team)), dim3(kThreads), team, smem, s, g);
 }
 

@@ -115,6 +115,10 @@ __device__ __forceinline__ void tma_load_2d_pair(void *dst, const CUtensorMap *m
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// The same where nothing was written: what this warp has read from tensor memory is in its registers.
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t bar) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 __device__ __forceinline__ bool mbar_wait_cluster(uint64_t *bar, uint32_t parity) {
     const long long t0 = clock64();
     for (;;) {
@@ -139,6 +143,22 @@ __device__ __forceinline__ void tmem_load16(uint32_t address, uint32_t (&v)[16])
           "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
         : "r"(address)
         : "memory");
+}
+// 16 lanes (the address's lane and 15 more, within this warp's quarter) by 32 columns, as fragments of 8 x 8: registers
+// 4 c + 2 u and 4 c + 2 u + 1 are lane 8 u + l / 4, columns 8 c + 2 (l % 4) and the next.
+__device__ __forceinline__ void tmem_load_fragments(uint32_t address, uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(address)
+        : "memory");
+}
+// Four 8 x 8 matrices of 16-bit elements to shared memory, transposed: lane l gives the address of row l % 8 (a column of the
+// fragments) of matrix l / 8 and holds two elements of each, row l / 4, columns 2 (l % 4) and the next.
+__device__ __forceinline__ void stsm_x4_trans(uint32_t address, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(address), "r"(a), "r"(b), "r"(c), "r"(d)
+                 : "memory");
 }
 // Names the registers it waits for, so that no use of them moves in front.
 __device__ __forceinline__ void tmem_load_wait(uint32_t (&v)[16]) {
