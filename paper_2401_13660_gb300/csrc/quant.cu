@@ -17,6 +17,7 @@
 #include <cuda_fp8.h>
 
 #include "common.cuh"
+#include "pairs.cuh"
 #include "vec.cuh"
 
 namespace mbscan {
@@ -26,11 +27,15 @@ constexpr int kBlock = kQuantBlock;
 constexpr int kWord = 4;   // blocks whose scales share a 32-bit word
 
 __device__ __forceinline__ float4 load4(const float *p) { return gld4(p); }
-__device__ __forceinline__ float4 load4(const __nv_bfloat16 *p) {
-    const uint2 u = *reinterpret_cast<const uint2 *>(p);
+// Four elements as they are in memory, and widened.
+__device__ __forceinline__ float4 raw4(const float *p) { return gld4(p); }
+__device__ __forceinline__ uint2 raw4(const __nv_bfloat16 *p) { return *reinterpret_cast<const uint2 *>(p); }
+__device__ __forceinline__ float4 wide(const float4 &v) { return v; }
+__device__ __forceinline__ float4 wide(const uint2 &u) {
     return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
                        __uint_as_float(u.y & 0xffff0000u));
 }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16 *p) { return wide(raw4(p)); }
 
 // The bits of |x|, 0 for what is not finite.
 __device__ __forceinline__ unsigned magnitude(float x) {
@@ -51,11 +56,59 @@ __device__ __forceinline__ int block_exponent(unsigned top) {
 __device__ __forceinline__ float exp2i(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }   // -126 <= e <= 127
 
 // Four values times 2^-E as e4m3, the first in the lowest byte.
+__device__ __forceinline__ unsigned round4(float2 a, float2 b, float inv) {   // no infinities
+    a = mul2(a, splat(inv));
+    b = mul2(b, splat(inv));
+    return __nv_cvt_float2_to_fp8x2(a, __NV_SATFINITE, __NV_E4M3) |
+           (unsigned)__nv_cvt_float2_to_fp8x2(b, __NV_SATFINITE, __NV_E4M3) << 16;
+}
+__device__ __forceinline__ float finite(float x) { return fabsf(x) <= 3.402823466e38f ? x : __uint_as_float(0x7fffffffu); }
 __device__ __forceinline__ unsigned round4(const float4 &v, float inv) {
-    const auto one = [&](float x) { return fabsf(x) <= 3.402823466e38f ? x * inv : __uint_as_float(0x7fffffffu); };
-    const unsigned lo = __nv_cvt_float2_to_fp8x2(make_float2(one(v.x), one(v.y)), __NV_SATFINITE, __NV_E4M3);
-    const unsigned hi = __nv_cvt_float2_to_fp8x2(make_float2(one(v.z), one(v.w)), __NV_SATFINITE, __NV_E4M3);
-    return lo | hi << 16;
+    return round4(make_float2(finite(v.x), finite(v.y)), make_float2(finite(v.z), finite(v.w)), inv);
+}
+
+// ---- the norm's arithmetic: the 8-bit value is the one nearest to the norm itself (with plain fp32 one element in 10^5
+// falls on the other side of a border between two, a step of up to an eighth of its value). The sum of squares carries its
+// rounding errors along; elements are formed in fp32, and only where that is too near to a border, in a block of a thousand,
+// with their errors too.
+
+struct Sum {   // hi + lo
+    float hi, lo;
+};
+__device__ __forceinline__ Sum plus(Sum a, Sum b) {
+    const float t = a.hi + b.hi, bb = t - a.hi;
+    return {t, (a.hi - (t - bb)) + (b.hi - bb) + (a.lo + b.lo)};
+}
+// Adds the squares of two values to two sums.
+__device__ __forceinline__ void add_squares(float2 &hi, float2 &lo, float2 v) {
+    const float2 p = mul2(v, v), minus = splat(-1.f);
+    const float2 e = fma2(v, v, mul2(p, minus));
+    const float2 t = add2(hi, p), b = fma2(hi, minus, t);
+    const float2 err = add2(fma2(fma2(b, minus, t), minus, hi), fma2(b, minus, p));
+    hi = t;
+    lo = add2(lo, add2(err, e));
+}
+// 1 / sqrt(total / width + eps): a step of Newton's iteration gives the lower part.
+__device__ __forceinline__ Sum rstd_of(Sum total, float width, float eps) {
+    const float q = __fdiv_rn(total.hi, width);
+    const float ql = __fdiv_rn(fmaf(-q, width, total.hi) + total.lo, width);
+    const Sum x = plus({q, ql}, {eps, 0.f});
+    const float r = rsqrtf(x.hi), p = r * r, pe = fmaf(r, r, -p);
+    const float t = fmaf(-x.lo, p, fmaf(-x.hi, pe, fmaf(-x.hi, p, 1.f)));
+    return {r, x.hi > 0.f && x.hi <= 3.402823466e38f ? 0.5f * r * t : 0.f};
+}
+// v * rstd * g, with the last bit set where that is not exact (rounding to odd): rounded again, to fewer bits, it gives what
+// the product itself would. What is beyond fp32 is NaN.
+__device__ __forceinline__ float odd(float q, float lo) {
+    const float t = __fadd_rz(q, lo);
+    return t - q != lo ? __uint_as_float(__float_as_uint(t) | 1u) : t;
+}
+__device__ __forceinline__ float2 normalized(float2 v, float2 g, Sum rstd) {
+    const float2 minus = splat(-1.f), p = mul2(v, splat(rstd.hi));
+    const float2 pe = fma2(v, splat(rstd.lo), fma2(v, splat(rstd.hi), mul2(p, minus)));
+    const float2 q = mul2(p, g);
+    const float2 lo = fma2(pe, g, fma2(p, g, mul2(q, minus)));
+    return make_float2(odd(q.x, lo.x), odd(q.y, lo.y));
 }
 
 __device__ __forceinline__ unsigned warp_max(unsigned v) { return __reduce_max_sync(kFull, v); }
@@ -65,16 +118,17 @@ __device__ __forceinline__ unsigned warp_max(unsigned v) { return __reduce_max_s
 // latency counts, and a row spread over four times the warps is there sooner). The first kPer blocks of a warp stay in
 // registers between the sum of squares and the rounding; wider rows are read again.
 template <typename T, int kPer>
-__global__ void __launch_bounds__(1024) rmsnorm_q8_kernel(const T *add, float *residual, const float *w, float eps,
-                                                          uint8_t *q, uint8_t *scales, int width, int stride, bool early) {
-    __shared__ float red[32];
+__global__ void __launch_bounds__(kPer == 1 ? 1024 : 512, 1) rmsnorm_q8_kernel(const T *addend, float *residual, const float *w, float eps,
+                                                                            uint8_t *q, uint8_t *scales, int width, int stride,
+                                                                            bool early) {
+    __shared__ Sum red[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int64_t row = blockIdx.x;
     float *r = residual + row * width;
-    const T *a = add ? add + row * width : nullptr;
+    const T *a = addend ? addend + row * width : nullptr;
     const int step = warps * kPer;
     float4 kept[kPer];
-    float ss = 0.f;
+    float2 hi = make_float2(0.f, 0.f), lo = hi;
     if (early) pdl_trigger();
     pdl_wait();
     for (int b0 = warp * kPer; b0 < stride; b0 += step) {
@@ -92,66 +146,108 @@ __global__ void __launch_bounds__(1024) rmsnorm_q8_kernel(const T *add, float *r
                 v[j].x += d[j].x; v[j].y += d[j].y; v[j].z += d[j].z; v[j].w += d[j].w;
                 *reinterpret_cast<float4 *>(r + c) = v[j];
             }
-            ss = fmaf(v[j].x, v[j].x, fmaf(v[j].y, v[j].y, fmaf(v[j].z, v[j].z, fmaf(v[j].w, v[j].w, ss))));
+            add_squares(hi, lo, make_float2(v[j].x, v[j].y));
+            add_squares(hi, lo, make_float2(v[j].z, v[j].w));
             if (b0 < step) kept[j] = v[j];
         }
     }
+    Sum ss = plus({hi.x, lo.x}, {hi.y, lo.y});
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(kFull, ss, o);
-    if (lane == 0) red[warp] = ss;
-    __syncthreads();
-    float total = 0.f;
-    for (int i = 0; i < warps; ++i) total += red[i];
-    const float rstd = rsqrtf(total / (float)width + eps);
+    for (int o = 16; o > 0; o >>= 1) ss = plus(ss, {__shfl_xor_sync(kFull, ss.hi, o), __shfl_xor_sync(kFull, ss.lo, o)});
+    Sum rstd;
+    if (warps == 1) {
+        rstd = rstd_of(ss, (float)width, eps);
+    } else {   // one warp for all: every one of many would take its turn
+        if (lane == 0) red[warp] = ss;
+        __syncthreads();
+        if (warp == 0) {
+            ss = lane < warps ? red[lane] : Sum{0.f, 0.f};
+            for (int o = warps > 16 ? 16 : warps > 8 ? 8 : warps > 4 ? 4 : warps > 2 ? 2 : 1; o > 0; o >>= 1)
+                ss = plus(ss, {__shfl_xor_sync(kFull, ss.hi, o), __shfl_xor_sync(kFull, ss.lo, o)});
+            __syncwarp();
+            if (lane == 0) red[0] = rstd_of(ss, (float)width, eps);
+        }
+        __syncthreads();
+        rstd = red[0];
+    }
+    const float near = rstd.hi + rstd.lo;
     for (int b0 = warp * kPer; b0 < stride; b0 += step) {
         unsigned word = 0;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             const int c = (b0 + j) * kBlock + 4 * lane;
-            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f), g = v;
             if (c < width) {
-                const float4 v = b0 < step ? kept[j] : load4(r + c), g = load4(w + c);
-                y = make_float4(v.x * rstd * g.x, v.y * rstd * g.y, v.z * rstd * g.z, v.w * rstd * g.w);
+                v = b0 < step ? kept[j] : load4(r + c);
+                g = load4(w + c);
             }
-            const int e = block_exponent(warp_max(magnitude(y)));
-            if (c < width) *reinterpret_cast<unsigned *>(q + row * width + c) = round4(y, exp2i(-e));
+            // within 2^-22 of the norm: times 1 - 2^-21 and 1 + 2^-21 it is rounded to the same value, or it is near a border
+            const float2 v0 = make_float2(v.x, v.y), v1 = make_float2(v.z, v.w), g0 = make_float2(g.x, g.y), g1 = make_float2(g.z, g.w);
+            float2 y0 = mul2(mul2(v0, splat(near)), g0), y1 = mul2(mul2(v1, splat(near)), g1);
+            float top = fmaxf(fmaxf(fabsf(y0.x), fabsf(y0.y)), fmaxf(fabsf(y1.x), fabsf(y1.y)));   // passes NaN over
+            unsigned most = warp_max(__float_as_uint(top));
+            int e = block_exponent(most);
+            const float inv = exp2i(-e);
+            unsigned bytes = round4(y0, y1, inv * (1.f - 0x1p-21f));
+            const bool border = bytes != round4(y0, y1, inv * (1.f + 0x1p-21f)) || most >= 0x7f7ffff0u ||
+                                most < 0x0d000000u ||   // what is subnormal in fp32 is nothing in the block's units above that
+                                ((most + 8u) & 0x7fffffu) - 0x600000u <= 16u;
+            if (__any_sync(kFull, border) && most != 0u) {
+                y0 = normalized(v0, g0, rstd);
+                y1 = normalized(v1, g1, rstd);
+                top = fmaxf(fmaxf(fabsf(y0.x), fabsf(y0.y)), fmaxf(fabsf(y1.x), fabsf(y1.y)));
+                e = block_exponent(warp_max(magnitude(top)));
+                bytes = round4(y0, y1, exp2i(-e));
+            }
+            if (c < width) *reinterpret_cast<unsigned *>(q + row * width + c) = bytes;
             word |= (unsigned)(e + 127) << (8 * j);
         }
         if (lane == 0) {
-            if (kPer == kWord) *reinterpret_cast<unsigned *>(scales + row * stride + b0) = word;
-            else scales[row * stride + b0] = (uint8_t)word;
+            if (kPer == 1) scales[row * stride + b0] = (uint8_t)word;
+            else *reinterpret_cast<unsigned *>(scales + row * stride + b0) = word;
         }
     }
 }
 
 constexpr int kQuantThreads = 256;
 
-// Rows of x, a warp to a word of scales (512 columns).
+// Rows of x, a warp to two words of scales (512 columns each), which may be of different rows.
 template <typename T>
 __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const T *x, int64_t x_stride, uint8_t *q, uint8_t *scales,
-                                                                     int64_t rows, int width, int stride, bool early) {
+                                                                     int64_t rows, int width, int stride, int each, bool early) {
+    using Raw = decltype(raw4(static_cast<const T *>(nullptr)));
+    constexpr int kEach = 2;
     const int lane = threadIdx.x & 31, words = stride / kWord;
-    const int64_t task = (int64_t)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5);
+    const int64_t tasks = rows * words, first = ((int64_t)blockIdx.x * (kQuantThreads / 32) + (threadIdx.x >> 5)) * each;
     if (early) pdl_trigger();
     pdl_wait();
-    if (task >= rows * words) return;
-    const int64_t row = task / words;
-    const int b0 = (int)(task - row * words) * kWord;
-    float4 v[kWord];
+    Raw v[kEach][kWord];
 #pragma unroll
-    for (int j = 0; j < kWord; ++j) {
-        const int c = (b0 + j) * kBlock + 4 * lane;
-        v[j] = c < width ? load4(x + row * x_stride + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-    unsigned word = 0;
+    for (int t = 0; t < kEach; ++t) {
+        const int64_t row = (first + t) / words;
+        const int b0 = (int)(first + t - row * words) * kWord;
 #pragma unroll
-    for (int j = 0; j < kWord; ++j) {
-        const int c = (b0 + j) * kBlock + 4 * lane;
-        const int e = block_exponent(warp_max(magnitude(v[j])));
-        if (c < width) *reinterpret_cast<unsigned *>(q + row * width + c) = round4(v[j], exp2i(-e));
-        word |= (unsigned)(e + 127) << (8 * j);
+        for (int j = 0; j < kWord; ++j) {
+            const int c = (b0 + j) * kBlock + 4 * lane;
+            v[t][j] = t < each && first + t < tasks && c < width ? raw4(x + row * x_stride + c) : Raw{};
+        }
     }
-    if (lane == 0) *reinterpret_cast<unsigned *>(scales + row * stride + b0) = word;
+#pragma unroll
+    for (int t = 0; t < kEach; ++t) {
+        if (t >= each || first + t >= tasks) return;
+        const int64_t row = (first + t) / words;
+        const int b0 = (int)(first + t - row * words) * kWord;
+        unsigned word = 0;
+#pragma unroll
+        for (int j = 0; j < kWord; ++j) {
+            const int c = (b0 + j) * kBlock + 4 * lane;
+            const float4 f = wide(v[t][j]);
+            const int e = block_exponent(warp_max(magnitude(f)));
+            if (c < width) *reinterpret_cast<unsigned *>(q + row * width + c) = round4(f, exp2i(-e));
+            word |= (unsigned)(e + 127) << (8 * j);
+        }
+        if (lane == 0) *reinterpret_cast<unsigned *>(scales + row * stride + b0) = word;
+    }
 }
 
 // 128 x 128 blocks, one CTA each; it keeps its 64 values a thread in registers until the block's maximum is known. There is
@@ -159,21 +255,20 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const T *x
 template <typename T>
 __global__ void __launch_bounds__(kQuantThreads) quantize_blocks_kernel(const T *x, int64_t x_stride, uint8_t *q, uint8_t *scales,
                                                                        int64_t rows, int width, int stride) {
+    using Raw = decltype(raw4(static_cast<const T *>(nullptr)));
     constexpr int kWarps = kQuantThreads / 32, kRows = kBlock / kWarps;
     __shared__ unsigned red[kWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t down = blockIdx.x / stride, row0 = down * kBlock;
+    const int64_t down = blockIdx.x / stride, row0 = down * kBlock + warp;
     const int across = (int)(blockIdx.x - down * stride), c = across * kBlock + 4 * lane;
     pdl_wait();
-    float4 v[kRows];
+    Raw v[kRows];
     unsigned top = 0;
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        const int64_t row = row0 + i * kWarps + warp;
-        v[i] = row < rows && c < width ? load4(x + row * x_stride + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-    }
+    for (int i = 0; i < kRows; ++i)
+        v[i] = row0 + i * kWarps < rows && c < width ? raw4(x + (row0 + i * kWarps) * x_stride + c) : Raw{};
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) top = max(top, magnitude(v[i]));
+    for (int i = 0; i < kRows; ++i) top = max(top, magnitude(wide(v[i])));
     top = warp_max(top);
     if (lane == 0) red[warp] = top;
     __syncthreads();
@@ -182,10 +277,9 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_blocks_kernel(const T 
     const int e = block_exponent(top);
     const float inv = exp2i(-e);
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        const int64_t row = row0 + i * kWarps + warp;
-        if (row < rows && c < width) *reinterpret_cast<unsigned *>(q + row * width + c) = round4(v[i], inv);
-    }
+    for (int i = 0; i < kRows; ++i)
+        if (row0 + i * kWarps < rows && c < width)
+            *reinterpret_cast<unsigned *>(q + (row0 + i * kWarps) * width + c) = round4(wide(v[i]), inv);
     if (threadIdx.x == 0) scales[blockIdx.x] = (uint8_t)(e + 127);
 }
 
@@ -233,11 +327,13 @@ template <typename T>
 cudaError_t norm(const void *add, float *residual, const float *w, float eps, uint8_t *q, uint8_t *scales, int64_t rows,
                  int width, cudaStream_t s) {
     const int stride = (int)quant_stride(width);
+    // few rows: a warp to a block; many: a warp to four (65536 x 1024: 128 us; eight 140, two 134)
     const bool few = rows <= 4 * (int64_t)device_sms();
-    const int warps = few ? (stride < 32 ? stride : 32) : (stride / kWord < 32 ? stride / kWord : 32);
-    return launch_pdl(true, few ? rmsnorm_q8_kernel<T, 1> : rmsnorm_q8_kernel<T, kWord>, dim3((unsigned)rows),
-                      dim3(32 * warps), 0, s, static_cast<const T *>(add), residual, w, eps, q, scales, width, stride,
-                      leaves_room(rows));
+    const int per = few ? 1 : kWord, most = few ? 32 : 16;
+    const int warps = (stride + per - 1) / per < most ? (stride + per - 1) / per : most;
+    const auto kern = few ? rmsnorm_q8_kernel<T, 1> : rmsnorm_q8_kernel<T, kWord>;
+    return launch_pdl(true, kern, dim3((unsigned)rows), dim3(32 * warps), 0, s, static_cast<const T *>(add), residual, w, eps, q,
+                      scales, width, stride, leaves_room(rows));
 }
 
 template <typename T>
@@ -246,9 +342,10 @@ cudaError_t quantize(const void *x, int64_t x_stride, bool blocks, uint8_t *q, u
     const int stride = (int)quant_stride(width);
     if (!blocks) {
         const int64_t tasks = rows * (stride / kWord);
-        return launch_pdl(true, quantize_rows_kernel<T>, dim3(ctas(tasks * 32)), dim3(kQuantThreads), 0, s,
-                          static_cast<const T *>(x), x_stride, q, scales, rows, width, stride,
-                          leaves_room(ctas(tasks * 32)));
+        const int each = tasks * 32 > 2048 * (int64_t)device_sms() ? 2 : 1;   // a warp's, where they fill the GPU
+        const unsigned grid = ctas((tasks + each - 1) / each * 32);
+        return launch_pdl(true, quantize_rows_kernel<T>, dim3(grid), dim3(kQuantThreads), 0, s, static_cast<const T *>(x), x_stride,
+                          q, scales, rows, width, stride, each, leaves_room(grid));
     }
     const int64_t down = (rows + kBlock - 1) / kBlock;
     return launch_pdl(true, quantize_blocks_kernel<T>, dim3((unsigned)(down * stride)), dim3(kQuantThreads), 0, s,
