@@ -113,6 +113,28 @@ __device__ __forceinline__ float2 normalized(float2 v, float2 g, Sum rstd) {
 
 __device__ __forceinline__ unsigned warp_max(unsigned v) { return __reduce_max_sync(kFull, v); }
 
+// rstd of a row from every thread's sums of squares. One warp adds those of many up: every one would take its turn.
+__device__ __forceinline__ Sum row_rstd(Sum *red, float2 hi, float2 lo, float width, float eps) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    Sum ss = plus({hi.x, lo.x}, {hi.y, lo.y});
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ss = plus(ss, {__shfl_xor_sync(kFull, ss.hi, o), __shfl_xor_sync(kFull, ss.lo, o)});
+    if (warps == 1) return rstd_of(ss, width, eps);
+    __syncthreads();
+    if (lane == 0) red[warp] = ss;
+    __syncthreads();
+    if (warp == 0) {
+        ss = lane < warps ? red[lane] : Sum{0.f, 0.f};
+#pragma unroll 1
+        for (int o = warps > 16 ? 16 : warps > 8 ? 8 : warps > 4 ? 4 : warps > 2 ? 2 : 1; o > 0; o >>= 1)
+            ss = plus(ss, {__shfl_xor_sync(kFull, ss.hi, o), __shfl_xor_sync(kFull, ss.lo, o)});
+        __syncwarp();
+        if (lane == 0) red[0] = rstd_of(ss, width, eps);
+    }
+    __syncthreads();
+    return red[0];
+}
+
 // residual[row] += add[row] (when given); q, scales = the 8-bit form of residual[row] * w / sqrt(mean residual[row]^2 + eps).
 // One CTA per row: warp i takes the words (four blocks) i, i + warps, ..., or single blocks with kPer = 1 (few rows:
 // latency counts, and a row spread over four times the warps is there sooner). The first kPer blocks of a warp stay in
@@ -151,24 +173,23 @@ __global__ void __launch_bounds__(kPer == 1 ? 1024 : 512, 1) rmsnorm_q8_kernel(c
             if (b0 < step) kept[j] = v[j];
         }
     }
-    Sum ss = plus({hi.x, lo.x}, {hi.y, lo.y});
+    Sum rstd = row_rstd(red, hi, lo, (float)width, eps);
+    // squares beyond fp32's range, or lost below it: the row again times a power of two
+    const float scale = !(rstd.hi >= 0x1p-62f) ? 0x1p-80f : rstd.hi > 0x1p50f ? 0x1p80f : 1.f;
+    if (scale != 1.f) {
+        hi = lo = make_float2(0.f, 0.f);
+        for (int b0 = warp * kPer; b0 < stride; b0 += step) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) ss = plus(ss, {__shfl_xor_sync(kFull, ss.hi, o), __shfl_xor_sync(kFull, ss.lo, o)});
-    Sum rstd;
-    if (warps == 1) {
-        rstd = rstd_of(ss, (float)width, eps);
-    } else {   // one warp for all: every one of many would take its turn
-        if (lane == 0) red[warp] = ss;
-        __syncthreads();
-        if (warp == 0) {
-            ss = lane < warps ? red[lane] : Sum{0.f, 0.f};
-            for (int o = warps > 16 ? 16 : warps > 8 ? 8 : warps > 4 ? 4 : warps > 2 ? 2 : 1; o > 0; o >>= 1)
-                ss = plus(ss, {__shfl_xor_sync(kFull, ss.hi, o), __shfl_xor_sync(kFull, ss.lo, o)});
-            __syncwarp();
-            if (lane == 0) red[0] = rstd_of(ss, (float)width, eps);
+            for (int j = 0; j < kPer; ++j) {
+                const int c = (b0 + j) * kBlock + 4 * lane;
+                float4 v = b0 < step ? kept[j] : c < width ? load4(r + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+                v = make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
+                add_squares(hi, lo, make_float2(v.x, v.y));
+                add_squares(hi, lo, make_float2(v.z, v.w));
+                if (b0 < step) kept[j] = v;
+            }
         }
-        __syncthreads();
-        rstd = red[0];
+        rstd = row_rstd(red, hi, lo, (float)width, eps * scale * scale);
     }
     const float near = rstd.hi + rstd.lo;
     for (int b0 = warp * kPer; b0 < stride; b0 += step) {
@@ -178,7 +199,11 @@ __global__ void __launch_bounds__(kPer == 1 ? 1024 : 512, 1) rmsnorm_q8_kernel(c
             const int c = (b0 + j) * kBlock + 4 * lane;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f), g = v;
             if (c < width) {
-                v = b0 < step ? kept[j] : load4(r + c);
+                v = kept[j];
+                if (b0 >= step) {
+                    v = load4(r + c);
+                    v = make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
+                }
                 g = load4(w + c);
             }
             // within 2^-22 of the norm: times 1 - 2^-21 and 1 + 2^-21 it is rounded to the same value, or it is near a border

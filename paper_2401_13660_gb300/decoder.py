@@ -17,8 +17,17 @@ the scan rows, "Element-wise gating"):
 and finally rmsnorm and the tied byte head (logits over 256 bytes). The
 input, Delta, output and head projections are plain bf16 GEMMs (fp32
 accumulation) through cuBLAS (torch.bmm / torch.mm); every other step is a
-kernel of libmbscan.so. The whole step can be captured once in a CUDA graph
-(`capture`) and replayed per generated byte.
+kernel of libmbscan.so. With `bits=8` the input and output projections, nearly
+all of the weights, are held and multiplied in 8 bits with block scales:
+
+    h = rmsnorm(residual) * w in 8 bits                              mb_rmsnorm_q8
+    [x; z] = h [W_in_x; W_in_z]^T                                    mb_matmul_q8
+    ...
+    y in 8 bits;  out = y W_out^T                                    mb_quantize_q8, mb_matmul_q8
+
+The whole step can be captured once in a CUDA graph
+(`capture`) and replayed per generated byte. `draw` takes the next bytes from
+the logits (mb_sample), `generate` alternates the two.
 Weights are random (seeded): the kernels and the memory traffic do not depend
 on trained values.
 """
@@ -88,11 +97,44 @@ def init_weights(cfg: DecoderConfig, device, seed: int = 0):
     return layers, emb, torch.ones(D, device=device)
 
 
+class Matrix8:
+    """A weight matrix [rows, width] in 8 bits with a scale for each block of 128 x 128."""
+
+    def __init__(self, W):
+        rows, width = W.shape
+        self.q = torch.empty(rows, width, dtype=torch.float8_e4m3fn, device=W.device)
+        self.scales = torch.empty(-(-rows // mb.Q8_BLOCK), mb.mb_q8_scale_stride(width), dtype=torch.uint8, device=W.device)
+        mb.mb_quantize_q8(W, self.q, self.scales, block_rows=mb.Q8_BLOCK)
+
+    def values(self):
+        return mb.mb_dequantize_q8(self.q, self.scales, torch.empty(self.q.shape, device=self.q.device), block_rows=mb.Q8_BLOCK)
+
+    def nbytes(self):
+        return self.q.numel() + self.scales.numel()
+
+
+class Rows8:
+    """Activations [rows, width] in 8 bits with a scale for 128 columns."""
+
+    def __init__(self, rows, width, device):
+        self.q = torch.empty(rows, width, dtype=torch.float8_e4m3fn, device=device)
+        self.scales = torch.empty(rows, mb.mb_q8_scale_stride(width), dtype=torch.uint8, device=device)
+
+    def values(self):
+        return mb.mb_dequantize_q8(self.q, self.scales, torch.empty(self.q.shape, device=self.q.device))
+
+
 class Decoder:
     """Recurrent byte-level decoder over `batch` streams (bf16 activations,
-    fp32 residual stream and SSM states, bf16 convolution windows)."""
+    fp32 residual stream and SSM states, bf16 convolution windows). bits: 16
+    (bf16 projections) or 8 (input and output projections in 8 bits; needs
+    d_inner % 128 == 0, and the decoder keeps no bf16 copy of them)."""
 
-    def __init__(self, cfg: DecoderConfig, batch: int, device, seed: int = 0, weights=None):
+    def __init__(self, cfg: DecoderConfig, batch: int, device, seed: int = 0, weights=None, bits: int = 16):
+        if bits not in (8, 16):
+            raise ValueError(f"bits {bits}, expected 8 or 16")
+        if bits == 8 and (cfg.d_inner % mb.Q8_BLOCK or cfg.d_model % 16):
+            raise ValueError(f"no 8-bit projections for d_model {cfg.d_model}, d_inner {cfg.d_inner}")
         # fp32 accumulation all the way in the bf16 GEMMs
         torch.backends.cuda.matmul.allow_bf16_reduced_precision_reduction = False
         self.cfg, self.batch, self.device = cfg, batch, torch.device(device)
@@ -109,6 +151,14 @@ class Decoder:
         self.xc, self.dt, self.y = (torch.empty(B, E, device=dev, dtype=bf) for _ in range(3))
         self.xdbl = torch.empty(B, R + 2 * N, device=dev, dtype=bf)   # [dt_low | B | C]
         self.logits = torch.empty(B, cfg.vocab, device=dev, dtype=bf)
+        self.drawn = torch.zeros(B, dtype=torch.int64, device=dev)
+        self.bits = bits
+        if bits == 8:
+            # the layers' own dicts stay as they were given
+            self.layers = [dict(L, W_in=Matrix8(L["W_in"].view(2 * E, D)), W_out=Matrix8(L["W_out"])) for L in self.layers]
+            for L in self.layers:
+                del L["W_in_x"], L["W_in_z"]
+            self.h8, self.y8 = Rows8(B, D, dev), Rows8(B, E, dev)
         # status block of the scan steps and of the fused convolution +
         # x-projection (a wait that times out is recorded there), then the
         # projection's fp32 partial sums
@@ -134,20 +184,32 @@ class Decoder:
             if trace is not None:   # copies of the block's inputs (host memory)
                 trace.append({"residual": self.residual.cpu(), "add": None if add is None else add.cpu(),
                               "ssm": self.ssm[l].cpu(), "conv": self.conv[l].cpu()})
-            mb.mb_rmsnorm(self.residual, L["norm_w"], self.h, add=add, eps=cfg.eps)
-            torch.bmm(hb, L["W_in"].transpose(1, 2), out=self.xz)
+            if self.bits == 8:
+                h8, y8, W_in, W_out = self.h8, self.y8, L["W_in"], L["W_out"]
+                mb.mb_rmsnorm_q8(self.residual, L["norm_w"], h8.q, h8.scales, add=add, eps=cfg.eps)
+                mb.mb_matmul_q8(h8.q, h8.scales, W_in.q, W_in.scales, self.xz, ws=self.ws)
+            else:
+                mb.mb_rmsnorm(self.residual, L["norm_w"], self.h, add=add, eps=cfg.eps)
+                torch.bmm(hb, L["W_in"].transpose(1, 2), out=self.xz)
             mb.mb_conv_xproj(self.xz[0], self.conv[l], L["conv_w"], L["W_xproj"], self.xc, self.xdbl, self.ws,
                              bias=L["conv_b"])
             torch.mm(self.xdbl[:, :R], L["W_dt"].t(), out=self.dt)
             mb.mb_step(self.xc[:, None], self.dt[:, None], Bv, Cv, L["A"], self.y[:, None], self.ssm[l],
                        z=self.xz[1][:, None], D=L["D"], dt_bias=L["dt_bias"], ws=self.ws)
-            torch.mm(self.y, L["W_out"].t(), out=self.out)
+            if self.bits == 8:
+                mb.mb_quantize_q8(self.y, y8.q, y8.scales)
+                mb.mb_matmul_q8(y8.q, y8.scales, W_out.q, W_out.scales, self.out, ws=self.ws)
+            else:
+                torch.mm(self.y, L["W_out"].t(), out=self.out)
             add = self.out
             if trace is not None:   # its intermediates and outputs
-                trace[-1].update(residual_out=self.residual.cpu(), h=self.h.cpu(), x=self.xz[0].cpu(),
+                trace[-1].update(residual_out=self.residual.cpu(), h=(h8.values() if self.bits == 8 else self.h).cpu(),
+                                 x=self.xz[0].cpu(),
                                  z=self.xz[1].cpu(), xc=self.xc.cpu(), xdbl=self.xdbl.cpu(), dt=self.dt.cpu(),
                                  y=self.y.cpu(), out=self.out.cpu(), ssm_out=self.ssm[l].cpu(),
                                  conv_out=self.conv[l].cpu())
+                if self.bits == 8:
+                    trace[-1].update(y8=y8.values().cpu())
         mb.mb_rmsnorm(self.residual, self.norm_f, self.h, add=add, eps=cfg.eps)
         torch.mm(self.h, self.emb.t(), out=self.logits)
 
@@ -183,6 +245,27 @@ class Decoder:
             self._forward(trace)
         return self.logits
 
+    def draw(self, u, *, temperature=None, top_k=None, top_p=None, min_p=None, prob=None):
+        """Draw every stream's next byte from the logits of the last step, by the
+        random numbers u [batch] (fp32 in [0, 1)). The settings are those of
+        mb_sample: a number for all streams, or a tensor [batch]. Returns the
+        bytes, int64 [batch] (overwritten by the next draw)."""
+        def each(v, dtype):
+            return v if v is None or isinstance(v, torch.Tensor) else torch.full((self.batch,), v, dtype=dtype, device=self.device)
+        return mb.mb_sample(self.logits, u, self.drawn, temperature=each(temperature, torch.float32),
+                            top_k=each(top_k, torch.int32), top_p=each(top_p, torch.float32),
+                            min_p=each(min_p, torch.float32), prob=prob)
+
+    def generate(self, tokens, u, **settings):
+        """Feed one byte per stream (int64 [batch]), then generate u.shape[0]
+        more of each, drawn by u [bytes, batch]: int64 [bytes, batch]."""
+        out = torch.empty(u.shape[0], self.batch, dtype=torch.int64, device=self.device)
+        for i in range(u.shape[0]):
+            self.step(tokens)
+            tokens = self.draw(u[i], **settings)
+            out[i] = tokens
+        return out
+
     def check(self):
         """Raise if a scan step recorded a device-side error (blocking)."""
         st, detail = mb.mb_check(self.ws)
@@ -192,7 +275,8 @@ class Decoder:
     def bytes_per_step(self) -> int:
         """Bytes one step must move: every weight once, the SSM states and
         convolution windows read and written, the embedding rows and head."""
-        w = sum(L[k].numel() * L[k].element_size() for L in self.layers for k in STORED_KEYS)
+        w = sum(L[k].nbytes() if isinstance(L[k], Matrix8) else L[k].numel() * L[k].element_size()
+                for L in self.layers for k in STORED_KEYS)
         w += self.emb.numel() * self.emb.element_size() + self.norm_f.numel() * 4
         st = sum(t.numel() * t.element_size() for t in self.ssm + self.conv)
         return w + 2 * st

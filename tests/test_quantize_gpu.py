@@ -155,3 +155,56 @@ def test_nothing_to_do():
         mb.mb_quantize_q8(torch.empty(rows, width, device=DEV), q, s)
         mb.mb_dequantize_q8(q, s, torch.empty(rows, width, device=DEV))
         mb.mb_rmsnorm_q8(torch.empty(rows, width, device=DEV), torch.empty(width, device=DEV), q, s)
+
+
+def test_offsets_beyond_32_bits():
+    rows, width = 131072, 16384   # 2^31 elements
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn(1024, width, device=DEV, generator=g, dtype=torch.bfloat16).repeat(rows // 1024, 1)
+    x[-1] *= 3
+    some = [0, 1, 65535, 65536, rows - 1]
+    q = torch.empty(rows, width, dtype=torch.uint8, device=DEV)
+    for block_rows in (1, 128):
+        s = torch.empty(-(-rows // block_rows), serve.stride(width), dtype=torch.uint8, device=DEV)
+        mb.mb_quantize_q8(x, q, s, block_rows=block_rows)
+        last = slice(rows - 128, rows)
+        if block_rows == 1:
+            _check(x[some], q[some], s[some], 1)
+        _check(x[last], q[last], s[-(128 // block_rows):], block_rows)
+    out = torch.empty(rows, width, dtype=torch.bfloat16, device=DEV)
+    mb.mb_dequantize_q8(q, s, out, block_rows=128)
+    want = serve.dequantize(q[last].cpu().numpy(), s[-1:].cpu().numpy(), 128)
+    assert np.array_equal(to_np(out[last]), want)
+    del out, x
+    residual = torch.randn(1024, width, device=DEV, generator=g).repeat(rows // 1024, 1)
+    w = torch.rand(width, device=DEV, generator=g) + 0.5
+    s = torch.empty(rows, serve.stride(width), dtype=torch.uint8, device=DEV)
+    mb.mb_rmsnorm_q8(residual, w, q, s)
+    rq, rs = serve.quantize(serve.rmsnorm(to_np(residual[some]), to_np(w), float(np.float32(1e-5))), 1)
+    assert np.array_equal(serve.e4m3_values(q[some].cpu().numpy()), rq) and np.array_equal(s[some].cpu().numpy(), rs)
+
+
+@pytest.mark.parametrize("scale", [1e-38, 1e-30, 1e-16, 1e15, 1e18, 1e37])
+def test_norm_of_small_and_large_rows(scale):
+    residual = torch.randn(7, 640, device=DEV) * scale
+    w = torch.randn(640, device=DEV)
+    w[3] = 1e30
+    w[200:] *= 1e-20
+    q, s = _empty(7, 640, 1)
+    mb.mb_rmsnorm_q8(residual, w, q, s, eps=1e-5)
+    rq, rs = serve.quantize(serve.rmsnorm(to_np(residual), to_np(w), float(np.float32(1e-5))), 1)
+    got = serve.e4m3_values(q.cpu().numpy())
+    # what is subnormal in fp32 on the way has fewer bits
+    tiny = np.abs(serve.rmsnorm(to_np(residual), to_np(w), 1e-5)) < 2.0 ** -100
+    assert np.array_equal(np.where(tiny, 0, got), np.where(tiny, 0, rq))
+
+
+@pytest.mark.parametrize("width", [640, 20496])
+@pytest.mark.parametrize("scale", [1e-37, 1e-25, 1.0])
+def test_norm_without_eps(scale, width):
+    residual = torch.randn(5, width, device=DEV) * scale
+    w = torch.rand(width, device=DEV) + 0.5
+    q, s = _empty(5, width, 1)
+    mb.mb_rmsnorm_q8(residual, w, q, s, eps=0.0)
+    rq, rs = serve.quantize(serve.rmsnorm(to_np(residual), to_np(w), 0.0), 1)
+    assert np.array_equal(serve.e4m3_values(q.cpu().numpy()), rq) and np.array_equal(s.cpu().numpy(), rs)

@@ -82,7 +82,7 @@ def test_draw(n, vocab, which, dtype):
     _check(logits, u, tokens, prob, dtype, **settings)
 
 
-@pytest.mark.parametrize("vocab, dtype", [(32001, "bf16"), (50257, "f32"), (130000, "bf16"), (200003, "f32")])
+@pytest.mark.parametrize("vocab, dtype", [(32001, "bf16"), (50257, "f32"), (130000, "bf16"), (200003, "f32"), (600007, "f32")])
 def test_large_vocabularies(vocab, dtype):
     g = torch.Generator(device=DEV).manual_seed(vocab)
     n = 5
@@ -177,6 +177,29 @@ def test_frequencies():
     p = torch.softmax(logits.double(), 0).cpu().numpy()
     assert np.abs(np.bincount(tokens, minlength=vocab) - n * p).max() <= 2
     assert np.abs(prob - p[tokens]).max() <= 2.0 ** -22
+
+
+def test_ties_in_a_row_that_does_not_fit():
+    """Read from memory in every pass, equals across the parts of a cluster."""
+    n, vocab = 3, 600001
+    logits = torch.full((n, vocab), 1.5, device=DEV)
+    logits[0, ::2] = 1.0
+    u = torch.full((n,), 0.75, device=DEV)
+    for top_k, top_p in ((0, 0.5), (400000, 1.0), (450001, 0.25), (7, 1.0)):
+        settings = dict(top_k=torch.full((n,), top_k, dtype=torch.int32, device=DEV), top_p=torch.full((n,), top_p, device=DEV))
+        tokens, prob = _sample(logits, u, **settings)
+        _check(logits, u, tokens, prob, "f32", **settings)
+
+
+def test_offsets_beyond_32_bits():
+    n, vocab = 2047, 1048573
+    logits = torch.zeros(n, vocab, dtype=torch.bfloat16, device=DEV)
+    at = torch.randint(0, vocab, (n,), device=DEV)
+    logits.scatter_(1, at[:, None], 30.0)
+    u = torch.rand(n, device=DEV)
+    for settings in ({}, dict(top_p=torch.full((n,), 0.5, device=DEV)), dict(temperature=torch.zeros(n, device=DEV))):
+        tokens = mb.mb_sample(logits, u, **settings)
+        assert torch.equal(tokens, at)
 
 
 def test_no_rows():
