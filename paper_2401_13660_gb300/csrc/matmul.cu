@@ -40,14 +40,27 @@ constexpr int kChunk = 32;           // rows of a sum that are moved at a time
 
 struct Tiles {
     int features, rows;       // tiles across
+    int band;                 // rows of tiles that are taken together, all of them for one column of tiles before the next
     int height;               // rows of a tile, a multiple of 16
     int blocks;               // 128-column blocks of the sum
+    int deep;                 // blocks of a stage: 1, 2 or 4
     int split, stages;
     int held;                 // chunks that a group of warps holds in shared memory at a time
     int sums;                 // in tensor memory: two, or one where no CTA has more than a tile
     uint32_t ring;            // bytes of the ring of stages
     uint32_t columns;         // of tensor memory
 };
+
+// Column and row of a tile.
+struct Place {
+    int feature, row;
+};
+__device__ __forceinline__ Place place_of(const Tiles &t, int tile) {
+    if (t.band == 1) return {tile % t.features, tile / t.features};
+    const int many = t.band * t.features, b = tile / many, in = tile - b * many;
+    const int height = min(t.band, t.rows - b * t.band);
+    return {in / height, b * t.band + in % height};
+}
 
 struct Args {
     CUtensorMap a, w, out;
@@ -111,7 +124,8 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
     const Tiles t = g.t;   // in registers: a wait would have them read again
     constexpr int kWide = kCtas * kFeatures;
     const int mine = t.height / kCtas;   // rows that this CTA loads
-    const uint32_t stage_bytes = (uint32_t)(kFeatures + mine) * kK;
+    const int deep = kCtas == 2 ? 1 : t.deep;
+    const uint32_t unit_bytes = (uint32_t)(kFeatures + mine) * kK, stage_bytes = deep * unit_bytes;
     unsigned char *const scales = smem + t.ring;
     // 1024-byte aligned (swizzled); of a CTA's only tile, where the ring was
     T *const chunks = reinterpret_cast<T *>(t.sums == 1 ? smem : scales + kSlots * kSlotBytes);
@@ -120,7 +134,9 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
     const int rank = kCtas == 2 ? 0 : (int)(blockIdx.x % (unsigned)t.split);
     const int team = kCtas == 2 ? 2 : t.split;
     const int first = (int)(blockIdx.x / (unsigned)team), step = (int)(gridDim.x / (unsigned)team), tiles = t.features * t.rows;
-    const int k0 = (int)((int64_t)t.blocks * rank / t.split), k1 = (int)((int64_t)t.blocks * (rank + 1) / t.split);
+    // this CTA's blocks of the sum: whole stages but for the last
+    const int units = (t.blocks + deep - 1) / deep;
+    const int k0 = units * rank / t.split * deep, k1 = min(t.blocks, units * (rank + 1) / t.split * deep);
     // a barrier of the CTA that issues the products
     const auto lead = [&](uint64_t *b) { return cluster_address(b, 0); };
 
@@ -139,8 +155,6 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
         }
         fence_mbar_init();
         for (const CUtensorMap *m : {&g.a, &g.w, &g.out}) tma_prefetch_map(m);
-        // this CTA's first weights are on their way to L2 while the kernel before drains
-        for (int k = k0; k < k1; ++k) tma_prefetch_2d(&g.w, k * kK, first % t.features * kWide + half * kFeatures);
     }
     if (warp == 0) tmem_alloc<kCtas>(&bar.tmem, t.columns);
     tmem_fence_before();
@@ -158,21 +172,25 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
         Ring r;
         int issued = 0;
         for (int tile = first; tile < tiles && ok; tile += step) {
-            const int n0 = tile % t.features * kWide + half * kFeatures, m0 = tile / t.features * t.height + half * mine;
-            for (int k = k0; k < k1; ++k, ++issued, r.next(t.stages)) {
+            const Place at_tile = place_of(t, tile);
+            const int n0 = at_tile.feature * kWide + half * kFeatures, m0 = at_tile.row * t.height + half * mine;
+            for (int k = k0; k < k1; k += deep, ++issued, r.next(t.stages)) {
                 uint64_t *const full = &bar.full[r.at];
                 if (!(ok = __all_sync(kFull, mbar_wait(&bar.empty[r.at], r.round ^ 1)))) break;
                 unsigned char *at = smem + (uint32_t)r.at * stage_bytes;
+                const int end = min(k1, k + deep);
                 if (elect_one()) {
-                    if (half == 0) mbar_arrive_expect_tx(full, kCtas * stage_bytes);
-                    if (kCtas == 1) {
-                        tma_load_2d(at, &g.w, full, k * kK, n0);
-                        tma_load_2d(at + kFeatures * kK, &g.a, full, k * kK, m0);
-                    } else {
-                        const uint32_t to = lead(full);
-                        tma_load_2d_pair(at, &g.w, to, k * kK, n0);
-                        tma_load_2d_pair(at + kFeatures * kK, &g.a, to, k * kK, m0);
-                    }
+                    if (half == 0) mbar_arrive_expect_tx(full, (uint32_t)(end - k) * kCtas * unit_bytes);
+                    const uint32_t to = kCtas == 2 ? lead(full) : 0u;
+#pragma unroll 1
+                    for (int u = k; u < end; ++u, at += unit_bytes)
+                        if (kCtas == 1) {
+                            tma_load_2d(at, &g.w, full, u * kK, n0);
+                            tma_load_2d(at + kFeatures * kK, &g.a, full, u * kK, m0);
+                        } else {
+                            tma_load_2d_pair(at, &g.w, to, u * kK, n0);
+                            tma_load_2d_pair(at + kFeatures * kK, &g.a, to, u * kK, m0);
+                        }
                 }
             }
         }
@@ -191,27 +209,33 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
             const uint32_t sum = tmem + sums.at * t.height;
             if (!(ok = wait(&bar.sum_empty[sums.at], sums.round ^ 1))) break;
             tmem_fence_after();
-            for (int k = k0; k < k1; ++k, r.next(t.stages)) {
+            for (int k = k0; k < k1; k += deep, r.next(t.stages)) {
                 const uint32_t tmem_w = tmem_scales + set * kScaleColumns, tmem_a = tmem_w + 4;
-                const bool begins = k == k0 || k % 4 == 0, ends = k == k1 - 1 || k % 4 == 3;   // with this slot
+                // a stage's blocks are of one word of scales; whether it begins, or ends, with this slot
+                const int end = min(k1, k + deep);
+                const bool begins = k == k0 || k % 4 == 0, ends = end == k1 || end % 4 == 0;
                 if (begins && !(ok = wait(&bar.scales_full[slot.at], slot.round))) break;
                 if (!(ok = __all_sync(kFull, mbar_wait(&bar.full[r.at], r.round)))) break;
                 tmem_fence_after();
-                const uint64_t dw = desc + (uint32_t)r.at * (stage_bytes >> 4), da = dw + (kFeatures * kK >> 4);
+                uint64_t dw = desc + (uint32_t)r.at * (stage_bytes >> 4);
                 const uint64_t ds = desc_scales + (uint32_t)slot.at * (kSlotBytes >> 4);
-                const uint32_t word = word0 | (uint32_t)(k & 3) << 4 | (uint32_t)(k & 3) << 29;
                 if (elect_one()) {
                     if (begins) {
                         tmem_copy_scales<kCtas>(tmem_w, ds);
                         tmem_copy_scales<kCtas>(tmem_a, ds + (512 >> 4));
                         if (t.height > 128) tmem_copy_scales<kCtas>(tmem_a + 4, ds + (1024 >> 4));
                     }
+#pragma unroll 1
+                    for (int u = k; u < end; ++u, dw += unit_bytes >> 4) {
+                        const uint64_t da = dw + (kFeatures * kK >> 4);
+                        const uint32_t word = word0 | (uint32_t)(u & 3) << 4 | (uint32_t)(u & 3) << 29;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        umma_q8<kCtas>(sum, dw + 2 * j, da + 2 * j, word, tmem_w, tmem_a, k > k0 || j > 0);
+                        for (int j = 0; j < 4; ++j)
+                            umma_q8<kCtas>(sum, dw + 2 * j, da + 2 * j, word, tmem_w, tmem_a, u > k0 || j > 0);
+                    }
                     umma_commit<kCtas>(&bar.empty[r.at]);
                     if (ends) umma_commit<kCtas>(&bar.scales_empty[slot.at]);
-                    if (k == k1 - 1) umma_commit<kCtas>(&bar.sum_full[sums.at]);
+                    if (end == k1) umma_commit<kCtas>(&bar.sum_full[sums.at]);
                 }
                 if (ends) {
                     slot.next(kSlots);
@@ -223,7 +247,8 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
         int group = 0;
         const int blocks = (int)((g.p.n_out + kFeatures - 1) / kFeatures);
         for (int tile = first; tile < tiles && ok; tile += step) {
-            const int block = tile % t.features * kCtas + half, m0 = tile / t.features * t.height;
+            const Place at_tile = place_of(t, tile);
+            const int block = at_tile.feature * kCtas + half, m0 = at_tile.row * t.height;
             for (int q = k0 / 4; q <= (k1 - 1) / 4; ++q, ++group) {
                 const int slot = group % kSlots;
                 if ((group & 1) != warp - 2) continue;
@@ -260,7 +285,8 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
         const uint32_t mine_at = warp % 4 / 2 * (kChunk * 128) + row * 128 + ((warp % 2 * 4 + lane / 8) ^ row) * 16;
         Ring sums;
         for (int tile = first; tile < tiles && ok; tile += step, sums.next(t.sums)) {
-            const int n0 = tile % t.features * kWide + half * kFeatures, m0 = tile / t.features * t.height;
+            const Place at_tile = place_of(t, tile);
+            const int n0 = at_tile.feature * kWide + half * kFeatures, m0 = at_tile.row * t.height;
             if (!(ok = __all_sync(kFull, mbar_wait(&bar.sum_full[sums.at], sums.round)))) break;
             tmem_fence_after();
             const uint32_t sum = tmem + sums.at * t.height + ((uint32_t)(warp % 4) * 32 << 16);
@@ -330,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
             }
             if (group * kChunk >= rows) sum_read();   // nothing of it is this group's
         }
-        if (leads) bulk_wait_all();
+        if (leads) bulk_wait_read_all();   // shared memory stays until its stores have read it
     }
     pdl_trigger();   // not before: the next kernel's CTAs beside this one cost 1 x 1024 x 4096 0.5 us
     if (!ok) report(g.p.status, MB_ERR_TIMEOUT, blockIdx.x);
@@ -407,6 +433,7 @@ cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t 
     // rows by 32, so that the stores of a tile end in it, or 16 rows alone
     t.rows = (int)((p.rows + kMaxRows - 1) / kMaxRows);
     t.height = p.rows <= 16 ? 16 : (int)(((p.rows + t.rows - 1) / t.rows + kChunk - 1) / kChunk * kChunk);
+    t.band = t.rows > 16 ? 4 : 1;   // 65536 x 1024 x 4096: 190 us, with 1 202; 256 x 2304 x 9216: 11.9 and 11.1
     t.blocks = (int)((p.width + kK - 1) / kK);
     const int64_t tiles = (int64_t)t.features * t.rows;
     // Parts of a sum: what they cost is the rows of both operands that a CTA loads (128 bytes each, two cycles), and what a
@@ -416,11 +443,16 @@ cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t 
     const auto cost = [&](int split) {
         return (int64_t)((t.blocks + split - 1) / split) * (kFeatures + t.height) + (split > 1 ? 1250 + 8 * t.height : 0);
     };
-    for (int split = 2; !pair && split <= kMaxSplit && tiles * split <= lim->sms && split <= t.blocks; split *= 2)
+    for (int split = 2; !pair && split <= kMaxSplit && tiles * split <= lim->sms && 4 * split <= t.blocks; split *= 2)
         if (cost(split) < cost(t.split)) t.split = split;
     const int team = pair ? 2 : t.split;
     const bool one = tiles <= lim->sms / team;   // tile to a CTA (or team)
-    const int stage = (kFeatures + t.height / ctas) * kK, share = (t.blocks + t.split - 1) / t.split;
+    const int unit = (kFeatures + t.height / ctas) * kK;
+    const bool tight = t.split > 2 && tiles > full_clusters(t.split);
+    // What a stage costs the warp that issues its products, some 250 cycles beside them, is little next to 4 x 128 columns of
+    // few rows (1 x 2304 x 9216: 8.4 -> 6.1 us, 256 x 2304 x 9216: 11.5 -> 9.7); a pair's products hide it.
+    t.deep = pair || tight ? 1 : unit <= 20 * 1024 ? 4 : unit <= 32 * 1024 ? 2 : 1;
+    const int stage = t.deep * unit, share = ((t.blocks + t.deep - 1) / t.deep + t.split - 1) / t.split;   // stages of a tile
     const int es = out_bf16 ? 2 : 4, chunk = kChunk * kFeatures * es;
     const int halves = ((t.height + kChunk - 1) / kChunk + kGroups - 1) / kGroups;   // chunks of a group of warps
     // Of several tiles to a CTA all that a group moves of a sum in bf16 is held beside the ring, in fp32 half of it.
@@ -430,7 +462,6 @@ cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t 
     const size_t most = lim->smem_optin - sizeof(Barriers) - 64, beside = lim->smem_sm / 2 - lim->smem_reserved - sizeof(Barriers) - 64;
     // as deep as it may be (256 x 2304 x 9216: 6 stages 10.7 us, 3 stages and room for the next kernel's CTA 12.8), but where
     // the clusters would not fit the GPU side by side then, two CTAs to an SM (64 x 4608 x 2304: 14.1 -> 8.7 us)
-    const bool tight = t.split > 2 && tiles > full_clusters(t.split);
     t.stages = std::min((int)(((tight ? beside : most) - fixed) / stage), kMaxStages);
     if (one) t.stages = std::min(t.stages, share);
     const size_t parts = one ? std::max((size_t)kGroups * t.held * chunk, t.split > 1 ? (size_t)t.height * kFeatures * 4 : 0) : 0;
