@@ -208,15 +208,8 @@ template <int kSize = 2, typename K> __device__ __forceinline__ void sort256(K (
     if constexpr (kSize < kShort) sort256<kSize * 2>(v, lane);
 }
 
-// Logit and index in one number, larger for what comes first: 16 + 8 bits of bf16 logits, 32 + 8 of fp32 ones.
-__device__ __forceinline__ unsigned pack(__nv_bfloat16, unsigned key, int i) { return key >> 16 << 8 | (unsigned)(255 - i); }
-__device__ __forceinline__ unsigned unpack(__nv_bfloat16, unsigned c) { return c >> 8 << 16 | (c & 0x800000u ? 0u : 0xffffu); }
-__device__ __forceinline__ u64 pack(float, unsigned key, int i) { return (u64)key << 8 | (unsigned)(255 - i); }
-__device__ __forceinline__ unsigned unpack(float, u64 c) { return (unsigned)(c >> 8); }
-
 template <typename T>
 __global__ void __launch_bounds__(256) sample_short_kernel(const __grid_constant__ SampleParams a, int drop, bool early) {
-    using K = decltype(pack(T{}, 0u, 0));
     __shared__ u64 powers[256];
     const int lane = threadIdx.x & 31;
     for (int i = threadIdx.x; i < 256; i += blockDim.x) powers[i] = kPowers.v[i];
@@ -249,19 +242,20 @@ __global__ void __launch_bounds__(256) sample_short_kernel(const __grid_constant
         return;
     }
     const Scale sc = make_scale(st.temperature, of_key(top), drop);
-    K last = 0;   // of the tokens that stay
+    // the tokens that stay: of larger keys than the last one's, and the first `equals` of those that have it
+    unsigned last = kMasked;
+    int equals = 0;
     if (st.k || st.nucleus) {
-        K c[kEach];
+        unsigned c[kEach];
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) c[j] = pack(T{}, key[j], kEach * lane + j);
+        for (int j = 0; j < kEach; ++j) c[j] = key[j];
         sort256(c, lane);
         u64 w[kEach], mine = 0;
 #pragma unroll
         for (int j = 0; j < kEach; j += 2) {
-            const unsigned k0 = unpack(T{}, c[j]), k1 = unpack(T{}, c[j + 1]);
-            weights(sc, make_float2(of_key(k0), of_key(k1)), powers, w[j], w[j + 1]);
-            if (k0 <= kMasked || (st.k && kEach * lane + j >= st.k)) w[j] = 0;
-            if (k1 <= kMasked || (st.k && kEach * lane + j + 1 >= st.k)) w[j + 1] = 0;
+            weights(sc, make_float2(of_key(c[j]), of_key(c[j + 1])), powers, w[j], w[j + 1]);
+            if (c[j] <= kMasked || (st.k && kEach * lane + j >= st.k)) w[j] = 0;
+            if (c[j + 1] <= kMasked || (st.k && kEach * lane + j + 1 >= st.k)) w[j + 1] = 0;
             mine += w[j] + w[j + 1];
         }
         u64 before = warp_before(mine, lane);
@@ -270,21 +264,37 @@ __global__ void __launch_bounds__(256) sample_short_kernel(const __grid_constant
         int kept = 0;   // a prefix of the sorted tokens
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            const unsigned k = unpack(T{}, c[j]);
-            kept += k > kMasked && (!st.k || kEach * lane + j < st.k) && before < reach;
+            kept += c[j] > kMasked && (!st.k || kEach * lane + j < st.k) && before < reach;
             before += w[j];
         }
         kept = __reduce_add_sync(kFull, kept);
-        K mine_last = 0;
+        unsigned mine_last = 0;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) mine_last = ((kept - 1) & (kEach - 1)) == j ? c[j] : mine_last;
         last = __shfl_sync(kFull, mine_last, (kept - 1) / kEach);
+        int above = 0;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) above += c[j] > last;
+        equals = kept - __reduce_add_sync(kFull, above);
+    }
+    int alike = 0;   // of the equal ones, those of lower lanes
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) alike += key[j] == last;
+    {
+        const int own = alike;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int v = __shfl_up_sync(kFull, alike, o);
+            if (lane >= o) alike += v;
+        }
+        alike -= own;
     }
     u64 w[kEach], mine = 0;
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
         if (j % 2 == 0) weights(sc, make_float2(of_key(key[j]), of_key(key[j + 1])), powers, w[j], w[j + 1]);
-        const bool in = key[j] > kMasked && pack(T{}, key[j], kEach * lane + j) >= last;
+        const bool in = key[j] > last || (key[j] == last && alike < equals);
+        alike += key[j] == last;
         if (!in || w[j] < st.least) w[j] = 0;
         mine += w[j];
     }
@@ -426,12 +436,18 @@ template <bool kCluster> struct Team {
         for (int j = 0; j < kBins / kThreads; ++j) {
             const int b = threadIdx.x * each + j;
             v[j] = 0;
-            if (j < each && b < share)
-#pragma unroll 1
-                for (int i = 0; i < size; ++i) {
-                    v[j] += peek(&sh.low[rank * share + b], i);
-                    if (kMass) v[j] += (u64)peek(&sh.high[rank * share + b], i) << 32;
-                }
+            if (j < each && b < share) {
+                unsigned low[kMaxCtas], high[kMaxCtas];   // all on their way at once
+#pragma unroll
+                for (int i = 0; i < (kCluster ? kMaxCtas : 1); ++i)
+                    if (i < size) {
+                        low[i] = peek(&sh.low[rank * share + b], i);
+                        high[i] = kMass ? peek(&sh.high[rank * share + b], i) : 0u;
+                    }
+#pragma unroll
+                for (int i = 0; i < (kCluster ? kMaxCtas : 1); ++i)
+                    if (i < size) v[j] += ((u64)high[i] << 32) + low[i];
+            }
             mine += v[j];
         }
         u64 before = warp_before(mine, lane);
