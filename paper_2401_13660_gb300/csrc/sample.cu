@@ -262,16 +262,16 @@ __global__ void __launch_bounds__(256) sample_short_kernel(const __grid_constant
         const u64 total = __shfl_sync(kFull, before + mine, 31);
         const u64 reach = st.nucleus ? nucleus_mass(st.p, total) : ~0ull;
         int kept = 0;   // a prefix of the sorted tokens
+        last = ~0u;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            kept += c[j] > kMasked && (!st.k || kEach * lane + j < st.k) && before < reach;
+            const bool stays = c[j] > kMasked && (!st.k || kEach * lane + j < st.k) && before < reach;
+            kept += stays;
+            last = stays ? min(last, c[j]) : last;
             before += w[j];
         }
         kept = __reduce_add_sync(kFull, kept);
-        unsigned mine_last = 0;
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) mine_last = ((kept - 1) & (kEach - 1)) == j ? c[j] : mine_last;
-        last = __shfl_sync(kFull, mine_last, (kept - 1) / kEach);
+        last = __reduce_min_sync(kFull, last);
         int above = 0;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) above += c[j] > last;
