@@ -932,7 +932,7 @@ def mb_quantize_q8(x, q, scales, *, block_rows=1, stream=None):
     if tuple(x.shape) != (rows, width) or x.device != dev:
         raise ValueError(f"x: {tuple(x.shape)} on {x.device}, expected {(rows, width)} on {dev}")
     S = width if x.is_contiguous() or rows == 1 and x.stride(1) == 1 else x.stride(0)
-    if S != width and (x.stride(1) != 1 or S < width):
+    if not x.is_contiguous() and x.stride(1) != 1 or S < width:
         raise ValueError("x must be contiguous or a column block of wider rows")
     _here(dev)
     rc = load_library().mb_quantize_q8(_ptr(x), _DTYPES[x.dtype], S, block_rows, _ptr(q), _ptr(scales), rows, width,

@@ -92,6 +92,10 @@ def test_the_binding_refuses_what_does_not_fit():
         a = dict(x=x, q=q, scales=s, block_rows=1) | bad
         with pytest.raises((TypeError, ValueError)):
             mb.mb_quantize_q8(a["x"], a["q"], a["scales"], block_rows=a["block_rows"])
+    wide = torch.zeros(4096)
+    for strides in ((256, 2), (512, 2), (1, 4), (0, 1), (255, 1)):
+        with pytest.raises(ValueError, match="column block"):
+            mb.mb_quantize_q8(torch.as_strided(wide, (4, 256), strides), q, s)
     for bad in (dict(out=x.half()), dict(out=x[:3]), dict(block_rows=128), dict()):
         a = dict(out=x, block_rows=1) | bad
         with pytest.raises((TypeError, ValueError)):
