@@ -590,9 +590,10 @@ mb_status mb_matmul_q8(const uint8_t *a, const uint8_t *a_scales, const uint8_t 
  *            one off
  *   tokens : [n], MB_TOKEN_I32 or MB_TOKEN_I64; -1 where every token is masked
  *   prob   : [n] fp32 or NULL: the probability the token was drawn with (0 with -1)
- * Weights are within 2^-31 of their value and all sums and comparisons exact:
- * the draw is reproducible, and differs from that of exact arithmetic only
- * where a border is as near as that. tokens and prob must not overlap anything else.
+ * Weights are within 2^-31 of their value and one unit of 2^-(62 - ceil(log2
+ * vocab)) of the largest one, and all sums and comparisons exact: the draw is
+ * reproducible, and differs from that of exact arithmetic only where a border is
+ * as near as that (of vocab weights, 2^-31 and vocab^2 2^-62 of the largest). tokens and prob must not overlap anything else.
  */
 mb_status mb_sample(const void *logits, int32_t dtype, const float *u, const float *temperature, const int32_t *top_k,
                     const float *top_p, const float *min_p, void *tokens, int32_t token_type, float *prob, int64_t n,

@@ -7,8 +7,8 @@
 //
 // Every comparison is of integers. A weight is held as a whole number of units of 2^-shift (shift = 62 - log2 of the
 // vocabulary: sums of a row fit 62 bits), so sums do not depend on their order, atomics included, and products with top_p
-// and u are taken exactly. A weight itself is within 2^-31 of its value (weight()): a draw differs from that of exact
-// arithmetic where u falls that near to a border.
+// and u are taken exactly. A weight itself is within 2^-31 of its value and one unit (weight()): a draw differs from
+// that of exact arithmetic where u falls that near to a border.
 //
 // Rows of up to 256 tokens (bytes): one warp, eight tokens a lane, sorted in registers. Longer rows: a CTA, or a
 // cluster of them where rows are few, which keeps the row in shared memory, finds where top_k and top_p end by histograms of
