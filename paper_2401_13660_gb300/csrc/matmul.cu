@@ -5,14 +5,15 @@
 // fp32 in tensor memory: no pass over partial sums.
 //
 // The weights are the instruction's A operand (128 output features in the 128 lanes), the rows of a its B operand (16 to
-// 240 of them, the columns of the sum in tensor memory): one row costs an eighth of a tile then, not 127 idle lanes, and a
+// 224 of them, the columns of the sum in tensor memory): one row costs an eighth of a tile then, not 127 idle lanes, and a
 // decode step streams each weight through one tile.
 //
-// Twelve warps: one issues the TMA copies of both operands into a ring of stages (128 columns of the sum each, 128-byte
-// swizzle), one the products, two lay out scales for the tensor core (512 columns' worth at a time: the four scales of a
+// Twelve warps: one issues the TMA copies of both operands into a ring of stages (128 to 512 columns of the sum each,
+// 128-byte swizzle), one the products, two lay out scales for the tensor core (512 columns' worth at a time: the four scales of a
 // word go to one column of tensor memory), and eight move finished sums to global memory while the next tile's products run
 // into the other half of tensor memory. CTAs take tiles in turn. Where tiles are few, a cluster of CTAs shares each tile's
-// sum, every one over part of it, and they add their parts up in order through distributed shared memory.
+// sum, every one over part of it; each gets the others' parts of its share of the rows into its shared memory and adds them up
+// in the order of the ranks, so that a result is the same in every run.
 #include "../../include/mbscan.h"
 #include "cluster.cuh"
 #include "common.cuh"
@@ -93,15 +94,20 @@ template <typename T> __device__ __forceinline__ T *out_at(const MatmulParams &p
     return static_cast<T *>(p.out) + (part * p.rows + row) * p.part + (n - part * p.part);
 }
 
-__device__ __forceinline__ float4 cluster_load4(uint32_t address) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                 : "r"(address)
-                 : "memory");
-    return v;
+// Four lanes' four words turned: word j of lane i is lane j's word i.
+__device__ __forceinline__ void transpose4(uint32_t *v, int lane) {
+#pragma unroll
+    for (int d = 1; d <= 2; d *= 2) {
+        const bool odd = lane & d;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (j & d) continue;
+            const uint32_t got = __shfl_xor_sync(~0u, odd ? v[j] : v[j + d], d);
+            v[j] = odd ? got : v[j];
+            v[j + d] = odd ? v[j + d] : got;
+        }
+    }
 }
-
 __device__ __forceinline__ uint32_t bf16_pair(uint32_t lo, uint32_t hi) {   // of the bits of two floats
     const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(lo), __uint_as_float(hi));
     return *reinterpret_cast<const uint32_t *>(&h);
@@ -278,7 +284,6 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
     } else if (warp >= 4) {
         const int feature = warp % 4 * 32 + lane, group = warp / 4 - 1;
         const bool leads = threadIdx.x % 128 == 0;
-        const bool whole = kCtas == 1 && t.split > 1;   // this CTA's part of the sum, where the ring was
         T *const held = chunks + group * t.held * (kChunk * kFeatures);
         // bf16: two halves of 64 features, rows of 128 bytes, their 16-byte pieces swizzled by the row
         const int row = lane % 8;
@@ -288,6 +293,7 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
             const Place at_tile = place_of(t, tile);
             const int n0 = at_tile.feature * kWide + half * kFeatures, m0 = at_tile.row * t.height;
             if (!(ok = __all_sync(kFull, mbar_wait(&bar.sum_full[sums.at], sums.round)))) break;
+            if (kCtas == 1 && t.split > 1) break;   // a part of a sum: below
             tmem_fence_after();
             const uint32_t sum = tmem + sums.at * t.height + ((uint32_t)(warp % 4) * 32 << 16);
             const int rows = n0 >= g.p.n_out ? 0 : (int)(g.p.rows - m0 < t.height ? g.p.rows - m0 : t.height);
@@ -303,14 +309,12 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
             };
             for (int c0 = group * kChunk; c0 < rows; c0 += t.held * kGroups * kChunk) {
                 const int c1 = min(rows, c0 + t.held * kGroups * kChunk);
-                if (!whole) {
-                    if (leads) bulk_wait_read_all();
-                    group_sync(group);   // what was held before has been read
-                }
+                if (leads) bulk_wait_read_all();
+                group_sync(group);   // what was held before has been read
                 T *chunk = held;
                 for (int c = c0; c < c1; c += kGroups * kChunk, chunk += kChunk * kFeatures) {
                     uint32_t v0[16], v1[16];
-                    if (sizeof(T) == 2 && !whole) {
+                    if (sizeof(T) == 2) {
                         tmem_load_fragments(sum + c, v0);
                         tmem_load_fragments(sum + c + (16 << 16), v1);
                     } else {
@@ -319,14 +323,7 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
                     }
                     tmem_load_wait(v0);
                     tmem_load_wait(v1);
-                    if (whole) {
-                        float *to = reinterpret_cast<float *>(smem) + c * kFeatures + feature;
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) to[j * kFeatures] = __uint_as_float(v0[j]);
-                        if (c + 16 < t.height)
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) to[(16 + j) * kFeatures] = __uint_as_float(v1[j]);
-                    } else if (sizeof(T) == 2) {
+                    if (sizeof(T) == 2) {
                         const uint32_t at = smem_u32(chunk) + mine_at;
 #pragma unroll
                         for (int q = 0; q < 4; ++q)
@@ -341,7 +338,6 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
                     }
                 }
                 if (c0 + t.held * kGroups * kChunk >= rows) sum_read();
-                if (whole) continue;
                 fence_proxy_async_smem();
                 group_sync(group);
                 if (leads) {
@@ -361,28 +357,51 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
     pdl_trigger();   // not before: the next kernel's CTAs beside this one cost 1 x 1024 x 4096 0.5 us
     if (!ok) report(g.p.status, MB_ERR_TIMEOUT, blockIdx.x);
     __syncthreads();
-    if (kCtas == 1 && t.split > 1) {   // the parts in the order of their ranks, every CTA for its share of the rows
+    if (kCtas == 1 && t.split > 1) {
+        // Every CTA has an equal share of the rows, gets all parts of them where its ring was, once all are done with their
+        // rings, and adds them up in the order of the ranks. Sent, 16 bytes to a lane, 64 x 4608 x 2304 takes 7.4 us and
+        // 1 x 2048 x 1024 4.7; fetched from where each CTA had put its parts down, 8.0 and 5.0 (128 rows of a tile: 10.5,
+        // 10.4).
+        cluster_arrive();
+        const Place at_tile = place_of(t, first);
+        const int64_t m0 = (int64_t)at_tile.row * t.height;
+        const int each = t.height / t.split, n0 = at_tile.feature * kFeatures;
+        const int feature = warp % 4 * 32 + lane / 4 * 4, rows = (int)(g.p.rows - m0 < t.height ? g.p.rows - m0 : t.height);
+        const uint32_t sum = tmem + ((uint32_t)(warp % 4) * 32 << 16);
+        const int part = (65535 + each) / each;   // of a row below 224, row * part >> 16 is row / each
+        cluster_wait();
+        if (warp >= 4) {
+            tmem_fence_after();
+            for (int c = (warp / 4 - 1) * 16; c < rows; c += kGroups * 16) {
+                uint32_t v[16];
+                tmem_load16(sum + c, v);
+                tmem_load_wait(v);
+#pragma unroll
+                for (int q = 0; q < 16; q += 4) {
+                    transpose4(v + q, lane);
+                    const int row = c + q + lane % 4, to = row * part >> 16;
+                    const uint32_t at = cluster_address(smem, to) + ((rank * each + row - to * each) * kFeatures + feature) * 4;
+                    if (row < rows)
+                        asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[q]), "r"(v[q + 1]),
+                                     "r"(v[q + 2]), "r"(v[q + 3])
+                                     : "memory");
+                }
+            }
+        }
         cluster_arrive();
         cluster_wait();
-        const int64_t m0 = (int64_t)(first / t.features) * t.height, n0 = (int64_t)(first % t.features) * kFeatures;
-        const int r0 = t.height * rank / t.split, r1 = t.height * (rank + 1) / t.split;
-        for (int i = r0 * 32 + threadIdx.x; i < r1 * 32; i += kThreads) {
-            const int64_t m = m0 + i / 32, n = n0 + i % 32 * 4;
+        const float4 *parts = reinterpret_cast<const float4 *>(smem);
+        for (int i = threadIdx.x; i < each * 32; i += kThreads) {
+            const int64_t m = m0 + rank * each + i / 32, n = n0 + i % 32 * 4;
             if (m >= g.p.rows || n >= g.p.n_out) continue;
-            const float *part = reinterpret_cast<const float *>(smem) + 4 * i;
-            float4 v[kMaxSplit];
-#pragma unroll
-            for (int s = 0; s < kMaxSplit; ++s)
-                if (s < t.split) v[s] = cluster_load4(cluster_address(part, s));
-#pragma unroll
-            for (int s = 1; s < kMaxSplit; ++s)
-                if (s < t.split) {
-                    v[0].x += v[s].x; v[0].y += v[s].y; v[0].z += v[s].z; v[0].w += v[s].w;
-                }
-            store4(out_at<T>(g.p, m, n), v[0]);
+            float4 v = parts[i];
+#pragma unroll 1
+            for (int s = 1; s < t.split; ++s) {
+                const float4 o = parts[s * each * 32 + i];
+                v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+            }
+            store4(out_at<T>(g.p, m, n), v);
         }
-        cluster_arrive();   // nobody ends while its part is read
-        cluster_wait();
     }
     if (kCtas == 2) {   // nobody ends while the other's products and arrivals are under way
         cluster_arrive();
@@ -430,21 +449,28 @@ cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t 
     const bool pair = p.rows > kPairRows && p.n_out > kFeatures;
     const int ctas = pair ? 2 : 1;
     t.features = (int)((p.n_out + ctas * kFeatures - 1) / (ctas * kFeatures));
-    // rows by 32, so that the stores of a tile end in it, or 16 rows alone
-    t.rows = (int)((p.rows + kMaxRows - 1) / kMaxRows);
-    t.height = p.rows <= 16 ? 16 : (int)(((p.rows + t.rows - 1) / t.rows + kChunk - 1) / kChunk * kChunk);
-    t.band = t.rows > 16 ? 4 : 1;   // 65536 x 1024 x 4096: 190 us, with 1 202; 256 x 2304 x 9216: 11.9 and 11.1
     t.blocks = (int)((p.width + kK - 1) / kK);
-    const int64_t tiles = (int64_t)t.features * t.rows;
-    // Parts of a sum: what they cost is the rows of both operands that a CTA loads (128 bytes each, two cycles), and what a
-    // cluster costs over single CTAs, 1.3 us, and adding up. Microseconds without and with: 1 x 1024 x 4096 5.3, 5.6; 256 x
-    // 1024 x 2304 6.2, 8.7; 1 x 2048 x 1024 6.7, 5.2; 256 x 4608 x 2304 14.9, 10.4.
+    // rows by 32, so that the stores of a tile end in it, or 16 rows alone
+    const int fewest = (int)((p.rows + kMaxRows - 1) / kMaxRows);
+    const auto height = [&](int rows) { return p.rows <= 16 ? 16 : (int)((((p.rows + rows - 1) / rows) + kChunk - 1) / kChunk * kChunk); };
+    // Rows of a tile and parts of a sum, where there are fewer tiles than SMs. What they cost is the rows of both operands
+    // that a CTA loads (128 bytes each, two cycles a row), what a cluster costs over single CTAs, some 0.5 us, with adding up,
+    // 10 ns to a row, and 1 us more where the clusters do not fit the GPU side by side. Microseconds with the fewest tiles
+    // and no parts, with parts, with what this rule takes: 1 x 2048 x 1024 6.7, 5.0, 4.7; 256 x 1024 x 2304 5.7, 8.7, 4.8;
+    // 200 x 4608 x 2304 21, -, 9.8; 384 x 4608 x 2304 -, 12.1, 11.1; 128 x 2304 x 4608 8.7, -, 6.9.
+    t.rows = fewest;
     t.split = 1;
-    const auto cost = [&](int split) {
-        return (int64_t)((t.blocks + split - 1) / split) * (kFeatures + t.height) + (split > 1 ? 1250 + 8 * t.height : 0);
+    const auto cost = [&](int rows, int split) {
+        return (int64_t)((t.blocks + split - 1) / split) * (kFeatures + height(rows)) + (split > 1 ? 1000 + 19 * height(rows) : 0) +
+               (split > 2 && t.features * rows > full_clusters(split) ? 2000 : 0);
     };
-    for (int split = 2; !pair && split <= kMaxSplit && tiles * split <= lim->sms && 4 * split <= t.blocks; split *= 2)
-        if (cost(split) < cost(t.split)) t.split = split;
+    for (int rows = fewest; !pair && rows <= (p.rows + kChunk - 1) / kChunk && (int64_t)t.features * rows <= lim->sms; ++rows)
+        for (int split = 1; split <= kMaxSplit && t.features * rows * split <= lim->sms && 4 * split <= std::max(t.blocks, 4); split *= 2)
+            if (cost(rows, split) < cost(t.rows, t.split)) t.rows = rows, t.split = split;
+    t.height = height(t.rows);
+    t.rows = (int)((p.rows + t.height - 1) / t.height);
+    t.band = t.rows > 16 ? 4 : 1;   // 65536 x 1024 x 4096: 190 us, with 1 202; 256 x 2304 x 9216: 11.9 and 11.1
+    const int64_t tiles = (int64_t)t.features * t.rows;
     const int team = pair ? 2 : t.split;
     const bool one = tiles <= lim->sms / team;   // tile to a CTA (or team)
     const int unit = (kFeatures + t.height / ctas) * kK;
@@ -461,7 +487,7 @@ cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t 
     const size_t fixed = 1024 + kSlots * kSlotBytes + (one ? 0 : (size_t)kGroups * t.held * chunk);
     const size_t most = lim->smem_optin - sizeof(Barriers) - 64, beside = lim->smem_sm / 2 - lim->smem_reserved - sizeof(Barriers) - 64;
     // as deep as it may be (256 x 2304 x 9216: 6 stages 10.7 us, 3 stages and room for the next kernel's CTA 12.8), but where
-    // the clusters would not fit the GPU side by side then, two CTAs to an SM (64 x 4608 x 2304: 14.1 -> 8.7 us)
+    // the clusters would not fit the GPU side by side then, two CTAs to an SM
     t.stages = std::min((int)(((tight ? beside : most) - fixed) / stage), kMaxStages);
     if (one) t.stages = std::min(t.stages, share);
     const size_t parts = one ? std::max((size_t)kGroups * t.held * chunk, t.split > 1 ? (size_t)t.height * kFeatures * 4 : 0) : 0;

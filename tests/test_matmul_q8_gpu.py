@@ -56,6 +56,21 @@ def test_product(rows, n, width, dtype):
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [2, 31, 64, 100, 200, 250, 320, 384])
+@pytest.mark.parametrize("n, width", [(128, 8192), (264, 2304), (1024, 4608), (2304, 4608)])
+def test_sums_in_parts(rows, n, width, dtype):
+    """Few tiles: two, four or eight parts of a sum, of tiles of every height, with rows missing in the last."""
+    a, sa = _matrix(rows, width, 1, 11)
+    w, sw = _matrix(n, width, 128, 12)
+    out = torch.full((rows, n), float("nan"), dtype=TYPES[dtype], device=DEV)
+    mb.mb_matmul_q8(a, sa, w, sw, out)
+    _check(a, sa, w, sw, out, dtype)
+    again = torch.empty_like(out)
+    mb.mb_matmul_q8(a, sa, w, sw, again)
+    assert torch.equal(out, again)
+
+
 @pytest.mark.parametrize("rows, parts", [(1, 2), (37, 3), (300, 2), (1100, 2)])
 def test_groups_of_columns_come_apart(rows, parts):
     a, sa = _matrix(rows, 1040, 1, 3)
