@@ -35,7 +35,7 @@ constexpr int kSlots = 4;            // of the ring of scales
 constexpr int kSlotBytes = 512 + 1024;
 static_assert(kSlots * kSlotBytes % 1024 == 0, "what follows is swizzled");   // a tile's features, then 256 rows
 constexpr int kScaleColumns = 4 + 8; // of one slot; two sets take turns
-constexpr int kPairRows = 384;       // more are for pairs of CTAs
+constexpr int kPairRows = 64;        // more may be for pairs of CTAs
 constexpr int kMaxSplit = 8;
 constexpr int kChunk = 32;           // rows of a sum that are moved at a time
 
@@ -446,12 +446,10 @@ cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t 
     g.p = p;
     g.stride = (int)quant_stride(p.width);
     Tiles &t = g.t;
-    const bool pair = p.rows > kPairRows && p.n_out > kFeatures;
-    const int ctas = pair ? 2 : 1;
-    t.features = (int)((p.n_out + ctas * kFeatures - 1) / (ctas * kFeatures));
+    t.features = (int)((p.n_out + kFeatures - 1) / kFeatures);
     t.blocks = (int)((p.width + kK - 1) / kK);
     // rows by 32, so that the stores of a tile end in it, or 16 rows alone
-    const int fewest = (int)((p.rows + kMaxRows - 1) / kMaxRows);
+    const int fewest = (int)((p.rows + kMaxRows - 1) / kMaxRows), most_rows = (int)((p.rows + kChunk - 1) / kChunk);
     const auto height = [&](int rows) { return p.rows <= 16 ? 16 : (int)((((p.rows + rows - 1) / rows) + kChunk - 1) / kChunk * kChunk); };
     // Rows of a tile and parts of a sum, where there are fewer tiles than SMs. What they cost is the rows of both operands
     // that a CTA loads (128 bytes each, two cycles a row), what a cluster costs over single CTAs, some 0.5 us, with adding up,
@@ -464,9 +462,22 @@ cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t 
         return (int64_t)((t.blocks + split - 1) / split) * (kFeatures + height(rows)) + (split > 1 ? 1000 + 19 * height(rows) : 0) +
                (split > 2 && t.features * rows > full_clusters(split) ? 2000 : 0);
     };
-    for (int rows = fewest; !pair && rows <= (p.rows + kChunk - 1) / kChunk && (int64_t)t.features * rows <= lim->sms; ++rows)
+    const bool round = (int64_t)t.features * fewest <= lim->sms;   // all tiles at once
+    for (int rows = fewest; round && rows <= most_rows && t.features * rows <= lim->sms; ++rows)
         for (int split = 1; split <= kMaxSplit && t.features * rows * split <= lim->sms && 4 * split <= std::max(t.blocks, 4); split *= 2)
             if (cost(rows, split) < cost(t.rows, t.split)) t.rows = rows, t.split = split;
+    // Pairs of CTAs load half of a tile's rows each, but wait for one another, some 1.4 us. Microseconds of single CTAs and
+    // pairs: 1024 x 2304 x 2304 8.7, 10.7; 2048 x 4608 x 1024 13.0, 15.1; 4096 x 4608 x 768 17.7, 16.4. Tiles in several
+    // rounds: 200 x 2304 x 32000 24.9, 21.7; 64 x 1024 x 32000 9.2, 11.5.
+    const int pairs = (t.features + 1) / 2, pair_rows = std::max(fewest, std::min(most_rows, lim->sms / 2 / pairs));
+    const bool pair = p.n_out > kFeatures && p.rows > kPairRows &&
+                      (!round || cost(t.rows, t.split) > (int64_t)t.blocks * (kFeatures + height(pair_rows) / 2) + 2800);
+    if (pair) {
+        t.features = pairs;
+        t.rows = pair_rows;
+        t.split = 1;
+    }
+    const int ctas = pair ? 2 : 1;
     t.height = height(t.rows);
     t.rows = (int)((p.rows + t.height - 1) / t.height);
     t.band = t.rows > 16 ? 4 : 1;   // 65536 x 1024 x 4096: 190 us, with 1 202; 256 x 2304 x 9216: 11.9 and 11.1

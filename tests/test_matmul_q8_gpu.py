@@ -71,6 +71,18 @@ def test_sums_in_parts(rows, n, width, dtype):
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows, n, width", [(65, 19720, 144), (100, 19592, 640), (225, 10008, 272), (385, 6664, 400),
+                                            (4096, 776, 4608), (3001, 520, 4112), (64, 19720, 144), (500, 2304, 16384)])
+def test_wide_products(rows, n, width, dtype):
+    """Pairs of CTAs, of tiles low and high, the last ones ragged both ways."""
+    a, sa = _matrix(rows, width, 1, 13)
+    w, sw = _matrix(n, width, 128, 14)
+    out = torch.full((rows, n), float("nan"), dtype=TYPES[dtype], device=DEV)
+    mb.mb_matmul_q8(a, sa, w, sw, out)
+    _check(a, sa, w, sw, out, dtype)
+
+
 @pytest.mark.parametrize("rows, parts", [(1, 2), (37, 3), (300, 2), (1100, 2)])
 def test_groups_of_columns_come_apart(rows, parts):
     a, sa = _matrix(rows, 1040, 1, 3)
