@@ -614,9 +614,11 @@ mb_status mb_check(void *ws, void *stream, int64_t *detail);
  * the kernels (for a TMA stage, a ring slot) gives up after about 2 s of SM
  * clocks, records MB_ERR_TIMEOUT in the workspace status block and returns,
  * so that a stalled copy cannot hang the GPU. This call runs that path on
- * purpose: one warp waits on a barrier nothing arrives on, for wait_cycles SM
- * clocks (1 .. 4e9), then records MB_ERR_TIMEOUT with detail = the clocks it
- * waited. Read it with mb_check; the context stays usable.
+ * purpose: one of four warps that work together waits on a barrier nothing
+ * arrives on, for wait_cycles SM clocks (1 .. 4e9), then completes it for the
+ * other three. All four give up, and MB_ERR_TIMEOUT is recorded with detail =
+ * the clocks that the first one waited (MB_ERR_CUDA if one of them went on).
+ * Read it with mb_check; the context stays usable.
  *   ws, ws_bytes : a workspace as for mb_scan_prefill (>= 256 bytes, 256-byte aligned)
  * Returns MB_ERR_INVALID_ARG for a bad workspace or wait_cycles.
  */

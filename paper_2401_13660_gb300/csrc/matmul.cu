@@ -74,6 +74,7 @@ struct Barriers {
     uint64_t full[kMaxStages], empty[kMaxStages];
     uint64_t scales_full[kSlots], scales_empty[kSlots];
     uint64_t sum_full[2], sum_empty[2];
+    uint64_t drained;         // of a CTA whose waits gave up: the products it had issued
     uint32_t tmem;
 };
 
@@ -118,7 +119,7 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *p, const float4 &v) {
     *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const unsigned *>(&a), *reinterpret_cast<const unsigned *>(&b));
 }
 
-// Among the four warps of a group that moves sums.
+// Among the four warps of a group that moves sums (after mbar_wait_group: all of them are there, or none).
 __device__ __forceinline__ void group_sync(int group) { asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory"); }
 
 // kCtas: 1, or 2: a pair of CTAs shares a tile of 256 features, each with its 128 features and half of the rows.
@@ -159,6 +160,7 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
             mbar_init(&bar.sum_full[i], 1);
             mbar_init(&bar.sum_empty[i], 4 * kGroups * kCtas);
         }
+        mbar_init(&bar.drained, 1);
         fence_mbar_init();
         for (const CUtensorMap *m : {&g.a, &g.w, &g.out}) tma_prefetch_map(m);
     }
@@ -249,6 +251,10 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
                 }
             }
         }
+        if (!ok) {   // tensor memory and the ring stay until what was issued is done
+            if (elect_one()) umma_commit<kCtas>(&bar.drained);
+            wait(&bar.drained, 0);
+        }
     } else if (warp == 2 || warp == 3) {   // words in turn
         int group = 0;
         const int blocks = (int)((g.p.n_out + kFeatures - 1) / kFeatures);
@@ -292,8 +298,12 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
         for (int tile = first; tile < tiles && ok; tile += step, sums.next(t.sums)) {
             const Place at_tile = place_of(t, tile);
             const int n0 = at_tile.feature * kWide + half * kFeatures, m0 = at_tile.row * t.height;
-            if (!(ok = __all_sync(kFull, mbar_wait(&bar.sum_full[sums.at], sums.round)))) break;
-            if (kCtas == 1 && t.split > 1) break;   // a part of a sum: below
+            if (kCtas == 1 && t.split > 1) {   // a part of a sum: below
+                ok = __all_sync(kFull, mbar_wait(&bar.sum_full[sums.at], sums.round));
+                break;
+            }
+            if (leads) bulk_wait_read_all();   // what was held before has been read
+            if (!(ok = mbar_wait_group(&bar.sum_full[sums.at], sums.round, 1 + group))) break;
             tmem_fence_after();
             const uint32_t sum = tmem + sums.at * t.height + ((uint32_t)(warp % 4) * 32 << 16);
             const int rows = n0 >= g.p.n_out ? 0 : (int)(g.p.rows - m0 < t.height ? g.p.rows - m0 : t.height);
@@ -309,8 +319,10 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
             };
             for (int c0 = group * kChunk; c0 < rows; c0 += t.held * kGroups * kChunk) {
                 const int c1 = min(rows, c0 + t.held * kGroups * kChunk);
-                if (leads) bulk_wait_read_all();
-                group_sync(group);   // what was held before has been read
+                if (c0 != group * kChunk) {   // as above
+                    if (leads) bulk_wait_read_all();
+                    group_sync(group);
+                }
                 T *chunk = held;
                 for (int c = c0; c < c1; c += kGroups * kChunk, chunk += kChunk * kFeatures) {
                     uint32_t v0[16], v1[16];

@@ -79,6 +79,25 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity) {
     return mbar_wait_for(bar, parity, kWaitCycles);
 }
 
+// A group of four whole warps that goes on to meet at the named barrier `id`, where nothing limits a wait, goes on together
+// or not at all: each warp's own limit runs out by itself. group_all: whether ok holds in all of the group's threads (they
+// meet at the barrier); mbar_wait_group: whether all of them saw the phase complete.
+__device__ __forceinline__ bool group_all(int id, bool ok) {
+    uint32_t all;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 q, %2, 0;\n\t"
+        "bar.red.and.pred p, %1, 128, q;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(all)
+        : "r"(id), "r"((uint32_t)ok)
+        : "memory");
+    return all != 0;
+}
+__device__ __forceinline__ bool mbar_wait_group(uint64_t *bar, uint32_t parity, int id) {
+    return group_all(id, __all_sync(0xffffffffu, mbar_wait(bar, parity)));
+}
+
 // 3-D tiled TMA load of box (x, y, z) into shared memory, completing on `bar`.
 // x is the innermost coordinate; x * element size must be a multiple of 16.
 __device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, uint64_t *bar, int x,

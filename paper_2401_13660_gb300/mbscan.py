@@ -1026,9 +1026,9 @@ def mb_sample(logits, u, tokens=None, *, temperature=None, top_k=None, top_p=Non
 
 
 def mb_selftest_timeout(ws, wait_cycles, stream=None):
-    """Run the bounded-wait diagnostic: a kernel waits wait_cycles SM clocks on
-    a barrier nothing arrives on and records MB_ERR_TIMEOUT in ws (read it with
-    mb_check)."""
+    """Run the bounded-wait diagnostic: one of four warps waits wait_cycles SM
+    clocks on a barrier nothing arrives on, all four give up, and
+    MB_ERR_TIMEOUT is recorded in ws (read it with mb_check)."""
     _need(ws, "ws", torch.uint8)
     rc = load_library().mb_selftest_timeout(_ptr(ws), ws.numel(), int(wait_cycles), _stream(stream, ws.device))
     _check(rc, "mb_selftest_timeout")
