@@ -554,7 +554,9 @@ mb_status mb_dequantize_q8(const uint8_t *q, const uint8_t *scales, int32_t bloc
  *   out[m, n] = sum_k A[m, k] W[n, k]
  * with A [rows, width] (a, a_scales: block_rows 1) and W [n_out, width] (w,
  * w_scales: block_rows 128) the values that stand in 8 bits; products are
- * exact, sums fp32 in an order that depends on the sizes only, out rounded once.
+ * exact, sums fp32, out rounded once. The order of a sum depends on the sizes and
+ * the device: it is the same in every call there, but a row beside more rows or
+ * fewer may be added up in another one.
  *   out  : [n_out / part, rows, part], out_dtype: columns n of the product in
  *          groups of `part` (0: n_out, one group), each a matrix of its own:
  *          [x | z] of one projection come apart. part % 128 == 0 and n_out % part
@@ -569,6 +571,16 @@ mb_status mb_dequantize_q8(const uint8_t *q, const uint8_t *scales, int32_t bloc
 mb_status mb_matmul_q8(const uint8_t *a, const uint8_t *a_scales, const uint8_t *w, const uint8_t *w_scales, void *out,
                        int32_t out_dtype, int64_t rows, int64_t n_out, int64_t width, int64_t part, void *ws,
                        size_t ws_bytes, void *stream);
+
+/*
+ * How mb_matmul_q8 takes a product of these sizes on the current device; what the
+ * order of its sums depends on. form[0]: 2 where pairs of CTAs share tiles, else 1;
+ * form[1]: parts of each sum, 128-column blocks of it to a CTA each; form[2]: rows of
+ * a tile (of 128 columns of out, 256 of a pair); form[3]: blocks fetched at a time;
+ * form[4]: tiles that a CTA (or pair, or the CTAs of a sum) takes at most. All 0 where
+ * there is nothing to multiply. Errors as of mb_matmul_q8.
+ */
+mb_status mb_matmul_q8_form(int64_t rows, int64_t n_out, int64_t width, int32_t out_dtype, int64_t form[5]);
 
 /*
  * Draw the next token of every stream from its logits and a given random

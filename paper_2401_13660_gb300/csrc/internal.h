@@ -199,6 +199,9 @@ struct MatmulParams {
     StatusBlock *status;           // may be null
 };
 cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t s);
+// How it takes a product on the current device; false where there is none.
+struct MatmulPlan;             // matmul_plan.h
+bool plan_matmul_here(int64_t rows, int64_t n_out, int64_t width, bool out_bf16, MatmulPlan *plan);
 // Draws from next-token distributions (sample.cu). n, vocab > 0.
 struct SampleParams {
     const void *logits;

@@ -17,40 +17,15 @@
 #include "../../include/mbscan.h"
 #include "cluster.cuh"
 #include "common.cuh"
+#include "matmul_plan.h"
 #include "umma.cuh"
 
-#include <algorithm>
 #include <atomic>
 
 namespace mbscan {
 namespace {
 
-constexpr int kGroups = 2;           // of four warps that move sums, chunks in turn
 constexpr int kThreads = 128 + 128 * kGroups;
-constexpr int kFeatures = 128;       // output features of a tile: lanes of tensor memory
-constexpr int kMaxRows = 224;        // rows of a tile: two sums and two sets of scales fit 512 columns
-constexpr int kK = kQuantBlock;      // columns of the sum in a stage
-constexpr int kMaxStages = 12;
-constexpr int kSlots = 4;            // of the ring of scales
-constexpr int kSlotBytes = 512 + 1024;
-static_assert(kSlots * kSlotBytes % 1024 == 0, "what follows is swizzled");   // a tile's features, then 256 rows
-constexpr int kScaleColumns = 4 + 8; // of one slot; two sets take turns
-constexpr int kPairRows = 64;        // more may be for pairs of CTAs
-constexpr int kMaxSplit = 8;
-constexpr int kChunk = 32;           // rows of a sum that are moved at a time
-
-struct Tiles {
-    int features, rows;       // tiles across
-    int band;                 // rows of tiles that are taken together, all of them for one column of tiles before the next
-    int height;               // rows of a tile, a multiple of 16
-    int blocks;               // 128-column blocks of the sum
-    int deep;                 // blocks of a stage: 1, 2 or 4
-    int split, stages;
-    int held;                 // chunks that a group of warps holds in shared memory at a time
-    int sums;                 // in tensor memory: two, or one where no CTA has more than a tile
-    uint32_t ring;            // bytes of the ring of stages
-    uint32_t columns;         // of tensor memory
-};
 
 // Column and row of a tile.
 struct Place {
@@ -74,7 +49,7 @@ struct Barriers {
     uint64_t full[kMaxStages], empty[kMaxStages];
     uint64_t scales_full[kSlots], scales_empty[kSlots];
     uint64_t sum_full[2], sum_empty[2];
-    uint64_t drained;         // of a CTA whose waits gave up: the products it had issued
+    uint64_t drained;   // of a CTA whose waits gave up: the products it had issued
     uint32_t tmem;
 };
 
@@ -422,16 +397,20 @@ __global__ void __launch_bounds__(kThreads, 2) matmul_q8_kernel(const __grid_con
     if (warp == 0) tmem_free<kCtas>(tmem, t.columns);
 }
 
-// Clusters of so many CTAs that fit the current device with all the shared memory they can have, looked up once.
+static_assert(sizeof(Barriers) <= kBarrierBytes, "beside the dynamic shared memory");
+static_assert(kK == kQuantBlock, "a block of the sum has one scale");
+
+// Clusters of so many CTAs that fit the current device with all the shared memory they can have; 0 where they cannot be
+// launched or the device does not say. Asked once: a product takes the same form in every call.
 int full_clusters(int size) {
     constexpr int kDevices = 64;
-    static std::atomic<int> known[kDevices][kMaxSplit + 1];
+    static std::atomic<int> known[kDevices][kMaxSplit + 1];   // the answer and one, 0: not asked yet
     int dev = 0, n = 0;
     const DeviceLimits *lim = device_limits();
     if (!lim || cudaGetDevice(&dev) != cudaSuccess || dev >= kDevices) return 0;
-    if ((n = known[dev][size].load(std::memory_order_relaxed)) > 0) return n;
+    if ((n = known[dev][size].load(std::memory_order_relaxed)) > 0) return n - 1;
     const auto kern = matmul_q8_kernel<__nv_bfloat16, 1>;
-    const int smem = (int)(lim->smem_optin - sizeof(Barriers) - 64);
+    const int smem = (int)(lim->smem_optin - kBarrierBytes);
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -443,97 +422,48 @@ int full_clusters(int size) {
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess ||
-        cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess)
-        return 0;
-    known[dev][size].store(n, std::memory_order_relaxed);
+        cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 0) {
+        cudaGetLastError();   // not a later call's
+        n = 0;
+    }
+    known[dev][size].store(n + 1, std::memory_order_relaxed);
     return n;
 }
 
 }  // namespace
 
-cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t s) {
+bool plan_matmul_here(int64_t rows, int64_t n_out, int64_t width, bool out_bf16, MatmulPlan *plan) {
     const DeviceLimits *lim = device_limits();
-    if (!lim) return cudaErrorInvalidDevice;
+    if (!lim) return false;
+    *plan = plan_matmul(rows, n_out, width, out_bf16, {lim->sms, lim->smem_sm, lim->smem_reserved, lim->smem_optin}, full_clusters);
+    return true;
+}
+
+cudaError_t launch_matmul_q8(const MatmulParams &p, bool out_bf16, cudaStream_t s) {
+    MatmulPlan plan;
+    if (!plan_matmul_here(p.rows, p.n_out, p.width, out_bf16, &plan)) return cudaErrorInvalidDevice;
     Args g;
     g.p = p;
     g.stride = (int)quant_stride(p.width);
-    Tiles &t = g.t;
-    t.features = (int)((p.n_out + kFeatures - 1) / kFeatures);
-    t.blocks = (int)((p.width + kK - 1) / kK);
-    // rows by 32, so that the stores of a tile end in it, or 16 rows alone
-    const int fewest = (int)((p.rows + kMaxRows - 1) / kMaxRows), most_rows = (int)((p.rows + kChunk - 1) / kChunk);
-    const auto height = [&](int rows) { return p.rows <= 16 ? 16 : (int)((((p.rows + rows - 1) / rows) + kChunk - 1) / kChunk * kChunk); };
-    // Rows of a tile and parts of a sum, where there are fewer tiles than SMs. What they cost is the rows of both operands
-    // that a CTA loads (128 bytes each, two cycles a row), what a cluster costs over single CTAs, some 0.5 us, with adding up,
-    // 10 ns to a row, and 1 us more where the clusters do not fit the GPU side by side. Microseconds with the fewest tiles
-    // and no parts, with parts, with what this rule takes: 1 x 2048 x 1024 6.7, 5.0, 4.7; 256 x 1024 x 2304 5.7, 8.7, 4.8;
-    // 200 x 4608 x 2304 21, -, 9.8; 384 x 4608 x 2304 -, 12.1, 11.1; 128 x 2304 x 4608 8.7, -, 6.9.
-    t.rows = fewest;
-    t.split = 1;
-    const auto cost = [&](int rows, int split) {
-        return (int64_t)((t.blocks + split - 1) / split) * (kFeatures + height(rows)) + (split > 1 ? 1000 + 19 * height(rows) : 0) +
-               (split > 2 && t.features * rows > full_clusters(split) ? 2000 : 0);
-    };
-    const bool round = (int64_t)t.features * fewest <= lim->sms;   // all tiles at once
-    for (int rows = fewest; round && rows <= most_rows && t.features * rows <= lim->sms; ++rows)
-        for (int split = 1; split <= kMaxSplit && t.features * rows * split <= lim->sms && 4 * split <= std::max(t.blocks, 4); split *= 2)
-            if (cost(rows, split) < cost(t.rows, t.split)) t.rows = rows, t.split = split;
-    // Pairs of CTAs load half of a tile's rows each, but wait for one another, some 1.4 us. Microseconds of single CTAs and
-    // pairs: 1024 x 2304 x 2304 8.7, 10.7; 2048 x 4608 x 1024 13.0, 15.1; 4096 x 4608 x 768 17.7, 16.4. Tiles in several
-    // rounds: 200 x 2304 x 32000 24.9, 21.7; 64 x 1024 x 32000 9.2, 11.5.
-    const int pairs = (t.features + 1) / 2, pair_rows = std::max(fewest, std::min(most_rows, lim->sms / 2 / pairs));
-    const bool pair = p.n_out > kFeatures && p.rows > kPairRows &&
-                      (!round || cost(t.rows, t.split) > (int64_t)t.blocks * (kFeatures + height(pair_rows) / 2) + 2800);
-    if (pair) {
-        t.features = pairs;
-        t.rows = pair_rows;
-        t.split = 1;
-    }
-    const int ctas = pair ? 2 : 1;
-    t.height = height(t.rows);
-    t.rows = (int)((p.rows + t.height - 1) / t.height);
-    t.band = t.rows > 16 ? 4 : 1;   // 65536 x 1024 x 4096: 190 us, with 1 202; 256 x 2304 x 9216: 11.9 and 11.1
-    const int64_t tiles = (int64_t)t.features * t.rows;
-    const int team = pair ? 2 : t.split;
-    const bool one = tiles <= lim->sms / team;   // tile to a CTA (or team)
-    const int unit = (kFeatures + t.height / ctas) * kK;
-    const bool tight = t.split > 2 && tiles > full_clusters(t.split);
-    // What a stage costs the warp that issues its products, some 250 cycles beside them, is little next to 4 x 128 columns of
-    // few rows (1 x 2304 x 9216: 8.4 -> 6.1 us, 256 x 2304 x 9216: 11.5 -> 9.7); a pair's products hide it.
-    t.deep = pair || tight ? 1 : unit <= 20 * 1024 ? 4 : unit <= 32 * 1024 ? 2 : 1;
-    const int stage = t.deep * unit, share = ((t.blocks + t.deep - 1) / t.deep + t.split - 1) / t.split;   // stages of a tile
-    const int es = out_bf16 ? 2 : 4, chunk = kChunk * kFeatures * es;
-    const int halves = ((t.height + kChunk - 1) / kChunk + kGroups - 1) / kGroups;   // chunks of a group of warps
-    // Of several tiles to a CTA all that a group moves of a sum in bf16 is held beside the ring, in fp32 half of it.
-    t.sums = one ? 1 : 2;
-    t.held = one || out_bf16 ? halves : (halves + 1) / 2;
-    const size_t fixed = 1024 + kSlots * kSlotBytes + (one ? 0 : (size_t)kGroups * t.held * chunk);
-    const size_t most = lim->smem_optin - sizeof(Barriers) - 64, beside = lim->smem_sm / 2 - lim->smem_reserved - sizeof(Barriers) - 64;
-    // as deep as it may be (256 x 2304 x 9216: 6 stages 10.7 us, 3 stages and room for the next kernel's CTA 12.8), but where
-    // the clusters would not fit the GPU side by side then, two CTAs to an SM
-    t.stages = std::min((int)(((tight ? beside : most) - fixed) / stage), kMaxStages);
-    if (one) t.stages = std::min(t.stages, share);
-    const size_t parts = one ? std::max((size_t)kGroups * t.held * chunk, t.split > 1 ? (size_t)t.height * kFeatures * 4 : 0) : 0;
-    t.ring = (uint32_t)((std::max((size_t)t.stages * stage, parts) + 1023) / 1024 * 1024);
-    // never three to an SM: half of its tensor memory each, CTAs of one tile never wait for columns while others of their
-    // cluster wait for them
-    const size_t smem = std::max(fixed + t.ring, lim->smem_sm / 3);
-    for (t.columns = 32; (int)t.columns < t.sums * t.height + 2 * kScaleColumns; t.columns *= 2) {}
+    g.t = plan.t;
+    const Tiles &t = g.t;
     const uint64_t wd[2] = {(uint64_t)p.width, (uint64_t)p.n_out}, ad[2] = {(uint64_t)p.width, (uint64_t)p.rows};
     const uint64_t st[1] = {(uint64_t)p.width};
-    const uint32_t wb[2] = {kK, kFeatures}, ab[2] = {kK, (uint32_t)(t.height / ctas)};
+    const uint32_t wb[2] = {kK, kFeatures}, ab[2] = {kK, (uint32_t)(t.height / plan.ctas)};
     if (!encode_tmap(&g.w, p.w, 1, 2, wd, st, wb, 128) || !encode_tmap(&g.a, p.a, 1, 2, ad, st, ab, 128))
         return cudaErrorInvalidValue;
+    const int es = out_bf16 ? 2 : 4;
     const uint64_t od[3] = {(uint64_t)p.part, (uint64_t)p.rows, (uint64_t)(p.n_out / p.part)};
     const uint64_t os[2] = {(uint64_t)(p.part * es), (uint64_t)(p.rows * p.part * es)};
     const uint32_t ob[3] = {out_bf16 ? 64u : 128u, kChunk, 1};
     if (!encode_tmap(&g.out, p.out, es, 3, od, os, ob, out_bf16 ? 128 : 0)) return cudaErrorInvalidValue;
+    const bool pair = plan.ctas == 2;
     const auto kern = pair ? (out_bf16 ? matmul_q8_kernel<__nv_bfloat16, 2> : matmul_q8_kernel<float, 2>)
                            : (out_bf16 ? matmul_q8_kernel<__nv_bfloat16, 1> : matmul_q8_kernel<float, 1>);
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(lim->smem_optin - sizeof(Barriers) - 64));
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               (int)(device_limits()->smem_optin - kBarrierBytes));
     if (e != cudaSuccess) return e;
-    const int64_t teams = one ? tiles : lim->sms / team;
-    return launch_cluster(true, kern, dim3((unsigned)(teams * team)), dim3(kThreads), team, smem, s, g);
+    return launch_cluster(true, kern, dim3((unsigned)(plan.teams * plan.team)), dim3(kThreads), plan.team, plan.smem, s, g);
 }
 
 }  // namespace mbscan

@@ -7,6 +7,7 @@
 #include "../../include/mbscan.h"
 #include "checks.h"
 #include "internal.h"
+#include "matmul_plan.h"
 
 using mbscan::aligned16;
 using mbscan::from_cuda;
@@ -31,6 +32,16 @@ mb_status check_size(int64_t rows, int64_t width) {
 }
 int64_t scale_rows(int64_t rows, int32_t block_rows) { return (rows + block_rows - 1) / block_rows; }
 bool block_rows_ok(int32_t block_rows) { return block_rows == 1 || block_rows == kQuantBlock; }
+
+// Sizes of a product of two of them, and its type.
+mb_status check_product(int64_t rows, int64_t n_out, int64_t width, int32_t out_dtype) {
+    for (const int64_t n : {rows, n_out})
+        if (const mb_status st = check_size(n, width); st != MB_OK) return st;
+    if (!dtype_ok(out_dtype)) return MB_ERR_INVALID_ARG;
+    if (n_out % 8 != 0) return MB_ERR_UNSUPPORTED;
+    if (n_out > 0 && rows > kMaxTokens / n_out) return MB_ERR_INVALID_ARG;
+    return MB_OK;
+}
 
 Range scales_range(const void *scales, int64_t rows, int32_t block_rows, int64_t width) {
     return range_of(scales, scale_rows(rows, block_rows) * mbscan::quant_stride(width));
@@ -98,11 +109,7 @@ mb_status mb_dequantize_q8(const uint8_t *q, const uint8_t *scales, int32_t bloc
 mb_status mb_matmul_q8(const uint8_t *a, const uint8_t *a_scales, const uint8_t *w, const uint8_t *w_scales, void *out,
                        int32_t out_dtype, int64_t rows, int64_t n_out, int64_t width, int64_t part, void *ws, size_t ws_bytes,
                        void *stream) {
-    for (const int64_t n : {rows, n_out})
-        if (const mb_status st = check_size(n, width); st != MB_OK) return st;
-    if (!dtype_ok(out_dtype)) return MB_ERR_INVALID_ARG;
-    if (n_out % 8 != 0) return MB_ERR_UNSUPPORTED;
-    if (n_out > 0 && rows > kMaxTokens / n_out) return MB_ERR_INVALID_ARG;
+    if (const mb_status st = check_product(rows, n_out, width, out_dtype); st != MB_OK) return st;
     if (part == 0) part = n_out;
     if (part != n_out && (part < 0 || part % kQuantBlock != 0 || n_out % part != 0)) return MB_ERR_INVALID_ARG;
     if (ws && (ws_bytes < mbscan::kStatusBytes || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0)) return MB_ERR_INVALID_ARG;
@@ -118,6 +125,19 @@ mb_status mb_matmul_q8(const uint8_t *a, const uint8_t *a_scales, const uint8_t 
     if (!apart(outs, ins)) return MB_ERR_INVALID_ARG;
     mbscan::MatmulParams p{a, a_scales, w, w_scales, out, rows, n_out, width, part, static_cast<mbscan::StatusBlock *>(ws)};
     return from_cuda(mbscan::launch_matmul_q8(p, out_dtype == MB_BF16, (cudaStream_t)stream));
+}
+
+mb_status mb_matmul_q8_form(int64_t rows, int64_t n_out, int64_t width, int32_t out_dtype, int64_t form[5]) {
+    if (!form) return MB_ERR_INVALID_ARG;
+    if (const mb_status st = check_product(rows, n_out, width, out_dtype); st != MB_OK) return st;
+    for (int i = 0; i < 5; ++i) form[i] = 0;
+    if (rows * n_out == 0 || width == 0) return MB_OK;   // no product runs
+    mbscan::MatmulPlan p;
+    if (!mbscan::plan_matmul_here(rows, n_out, width, out_dtype == MB_BF16, &p)) return MB_ERR_CUDA;
+    const int64_t tiles = (int64_t)p.t.features * p.t.rows;
+    const int64_t v[5] = {p.ctas, p.t.split, p.t.height, p.t.deep, (tiles + p.teams - 1) / p.teams};
+    for (int i = 0; i < 5; ++i) form[i] = v[i];
+    return MB_OK;
 }
 
 mb_status mb_sample(const void *logits, int32_t dtype, const float *u, const float *temperature, const int32_t *top_k,

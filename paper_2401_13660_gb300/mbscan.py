@@ -164,13 +164,14 @@ def load_library(build_if_needed: bool = True) -> ctypes.CDLL:
             lib.mb_quantize_q8.argtypes = [vp, i32, i64, i32, vp, vp, i64, i64, vp]
             lib.mb_dequantize_q8.argtypes = [vp, vp, i32, vp, i32, i64, i64, vp]
             lib.mb_matmul_q8.argtypes = [vp, vp, vp, vp, vp, i32, i64, i64, i64, i64, vp, sz, vp]
+            lib.mb_matmul_q8_form.argtypes = [i64, i64, i64, i32, ctypes.POINTER(i64)]
             lib.mb_sample.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, i32, vp, i64, i64, vp]
             for f in ("mb_scan_prefill", "mb_scan_verify", "mb_rollback", "mb_step", "mb_check",
                       "mb_accept_topk", "mb_step_resume", "mb_scan_prefill_ckpt", "mb_scan_backward",
                       "mb_rmsnorm", "mb_conv1d_step", "mb_selftest_timeout", "mb_scan_verify_resume",
                       "mb_conv_xproj", "mb_conv1d", "mb_conv1d_backward", "mb_embed", "mb_embed_backward",
                       "mb_cross_entropy", "mb_grad_norm", "mb_grad_clip", "mb_rmsnorm_q8", "mb_quantize_q8",
-                      "mb_dequantize_q8", "mb_matmul_q8", "mb_sample"):
+                      "mb_dequantize_q8", "mb_matmul_q8", "mb_matmul_q8_form", "mb_sample"):
                 getattr(lib, f).restype = ctypes.c_int
             lib.mb_status_string.argtypes = [ctypes.c_int]
             lib.mb_status_string.restype = ctypes.c_char_p
@@ -989,6 +990,18 @@ def mb_matmul_q8(a, a_scales, w, w_scales, out, *, ws=None, stream=None):
                                      n_out, width, part, _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream, dev))
     _check(rc, "mb_matmul_q8")
     return out
+
+
+def mb_matmul_q8_form(rows, n_out, width, dtype=torch.bfloat16):
+    """How mb_matmul_q8 takes a product of these sizes on the current device:
+    {"pair", "parts", "height", "deep", "tiles"} (2 where pairs of CTAs share
+    tiles; parts of each sum; rows of a tile; 128-column blocks fetched at a
+    time; tiles to a CTA)."""
+    if dtype not in _DTYPES:
+        raise TypeError(f"unsupported dtype {dtype}")
+    form = (ctypes.c_int64 * 5)()
+    _check(load_library().mb_matmul_q8_form(int(rows), int(n_out), int(width), _DTYPES[dtype], form), "mb_matmul_q8_form")
+    return dict(zip(("pair", "parts", "height", "deep", "tiles"), form))
 
 
 def mb_sample(logits, u, tokens=None, *, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, stream=None):
