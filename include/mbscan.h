@@ -531,6 +531,8 @@ int64_t mb_q8_scale_stride(int64_t width);
  * mb_rmsnorm with its output in 8 bits (block_rows 1):
  *   residual[b] += add[b]            (skipped when add == NULL)
  *   q, scales[b] = residual[b] * w / sqrt(mean_j residual[b, j]^2 + eps), rounded once
+ * Norms beyond fp32's range become NaN, a block of norms below 2^-200 counts as
+ * all zeros.
  * residual: fp32 [rows, width], read and written; add: dtype [rows, width];
  * w: fp32 [width]. No argument may overlap another.
  */

@@ -47,12 +47,13 @@ __device__ __forceinline__ unsigned magnitude(const float4 &v) {
 }
 
 // E of a block from the bits of its largest magnitude m * 2^k, 1 <= m < 2: k - 8 for m <= 1.75, else k - 7
-// (fp32's own subnormals end at the lower limit).
-__device__ __forceinline__ int block_exponent(unsigned top) {
-    if (top == 0u) return 0;
+// (fp32's own subnormals end at the lower limit). Of elements times 2^lift: E + lift.
+__device__ __forceinline__ int block_exponent(unsigned top, int lift = 0) {
+    if (top == 0u) return lift;
     const int k = (int)(top >> 23) - 127;
-    return max((top & 0x7fffffu) > 0x600000u ? k - 7 : k - 8, -126);
+    return max((top & 0x7fffffu) > 0x600000u ? k - 7 : k - 8, lift - 126);
 }
+__device__ __forceinline__ int ilog(float x) { return (int)(__float_as_uint(x) >> 23 & 255u) - 127; }   // of a normal number
 __device__ __forceinline__ float exp2i(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }   // -126 <= e <= 127
 
 // Four values times 2^-E as e4m3, the first in the lowest byte.
@@ -70,7 +71,7 @@ __device__ __forceinline__ unsigned round4(const float4 &v, float inv) {
 // ---- the norm's arithmetic: the 8-bit value is the one nearest to the norm itself (with plain fp32 one element in 10^5
 // falls on the other side of a border between two, a step of up to an eighth of its value). The sum of squares carries its
 // rounding errors along; elements are formed in fp32, and only where that is too near to a border, in a block of a thousand,
-// with their errors too.
+// with their errors too, and where fp32's range may not hold what that takes, with their exponents apart.
 
 struct Sum {   // hi + lo
     float hi, lo;
@@ -88,14 +89,18 @@ __device__ __forceinline__ void add_squares(float2 &hi, float2 &lo, float2 v) {
     hi = t;
     lo = add2(lo, add2(err, e));
 }
-// 1 / sqrt(total / width + eps): a step of Newton's iteration gives the lower part.
-__device__ __forceinline__ Sum rstd_of(Sum total, float width, float eps) {
+// What is formed is the norm times 2^kLift: v * rstd is 2^15.5 at the most (the root of the width), and 2^-165 is no subnormal
+// then, nor is its rounding error. No more than a constant, so that nothing waits for it.
+constexpr int kLift = 64;
+
+// 2^lift / sqrt(total / width + eps): a step of Newton's iteration gives the lower part.
+__device__ __forceinline__ Sum rstd_of(Sum total, float width, float eps, int lift) {
     const float q = __fdiv_rn(total.hi, width);
     const float ql = __fdiv_rn(fmaf(-q, width, total.hi) + total.lo, width);
     const Sum x = plus({q, ql}, {eps, 0.f});
     const float r = rsqrtf(x.hi), p = r * r, pe = fmaf(r, r, -p);
     const float t = fmaf(-x.lo, p, fmaf(-x.hi, pe, fmaf(-x.hi, p, 1.f)));
-    return {r, x.hi > 0.f && x.hi <= 3.402823466e38f ? 0.5f * r * t : 0.f};
+    return {r * exp2i(lift), x.hi > 0.f && x.hi <= 3.402823466e38f ? exp2i(lift - 1) * r * t : 0.f};
 }
 // v * rstd * g, with the last bit set where that is not exact (rounding to odd): rounded again, to fewer bits, it gives what
 // the product itself would. What is beyond fp32 is NaN.
@@ -113,13 +118,50 @@ __device__ __forceinline__ float2 normalized(float2 v, float2 g, Sum rstd) {
 
 __device__ __forceinline__ unsigned warp_max(unsigned v) { return __reduce_max_sync(kFull, v); }
 
-// rstd of a row from every thread's sums of squares. One warp adds those of many up: every one would take its turn.
-__device__ __forceinline__ Sum row_rstd(Sum *red, float2 hi, float2 lo, float width, float eps) {
+// The same with exponents apart, where fp32's range does not hold all of it: t 2^n, 1 <= |t| < 8 (or t is zero, or NaN).
+struct Apart {
+    float t;
+    int n;
+};
+__device__ __forceinline__ Apart apart(float x) {   // 1 <= |t| < 2, but of zero and what is no number
+    const bool low = fabsf(x) < 0x1p-126f;
+    const unsigned b = __float_as_uint(low ? x * 0x1p64f : x), e = b >> 23 & 255u;
+    if (e == 0u || e == 255u) return {x, 0};
+    return {__uint_as_float((b & 0x807fffffu) | 0x3f800000u), (int)e - (low ? 127 + 64 : 127)};
+}
+__device__ __forceinline__ Apart normalized(float v, float g, Sum rstd, int n) {   // rstd times 2^n, 1 <= rstd.hi < 2
+    const Apart a = apart(v), b = apart(g);
+    const float p = a.t * rstd.hi, pe = fmaf(a.t, rstd.lo, fmaf(a.t, rstd.hi, -p));
+    const float q = p * b.t;
+    const Apart y = {odd(q, fmaf(pe, b.t, fmaf(p, b.t, -q))), a.n + b.n + n};
+    return y.n + ilog(y.t) > 127 ? Apart{__uint_as_float(0x7fffffffu), 0} : y;   // beyond fp32
+}
+// The order of magnitudes as that of whole numbers: exponent + kLowest, 23 bits of the mantissa; what is below is 1, what is
+// no number 0.
+constexpr int kLowest = 161;
+__device__ __forceinline__ unsigned magnitude(const Apart &y) {
+    const unsigned b = magnitude(y.t);
+    const int e = y.n + ilog(y.t) + kLowest;
+    return b == 0u ? 0u : e > 0 ? (unsigned)e << 23 | (b & 0x7fffffu) : 1u;
+}
+// Bytes and E of a block of such values.
+__device__ __forceinline__ uint2 round_apart(const Apart (&y)[4]) {
+    const unsigned most = warp_max(max(max(magnitude(y[0]), magnitude(y[1])), max(magnitude(y[2]), magnitude(y[3]))));
+    const int k = (int)(most >> 23) - kLowest;
+    const int e = most == 0u ? 0 : max((most & 0x7fffffu) > 0x600000u ? k - 7 : k - 8, -126);
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = y[i].t * exp2i(min(max(y[i].n - e, -126), 127));
+    return make_uint2(round4(make_float2(f[0], f[1]), make_float2(f[2], f[3]), 1.f), (unsigned)e);
+}
+
+// rstd of a row, times 2^lift, from every thread's sums of squares. One warp adds those of many up: every one would take its turn.
+__device__ __forceinline__ Sum row_rstd(Sum *red, float2 hi, float2 lo, float width, float eps, int lift) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     Sum ss = plus({hi.x, lo.x}, {hi.y, lo.y});
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) ss = plus(ss, {__shfl_xor_sync(kFull, ss.hi, o), __shfl_xor_sync(kFull, ss.lo, o)});
-    if (warps == 1) return rstd_of(ss, width, eps);
+    if (warps == 1) return rstd_of(ss, width, eps, lift);
     __syncthreads();
     if (lane == 0) red[warp] = ss;
     __syncthreads();
@@ -129,7 +171,7 @@ __device__ __forceinline__ Sum row_rstd(Sum *red, float2 hi, float2 lo, float wi
         for (int o = warps > 16 ? 16 : warps > 8 ? 8 : warps > 4 ? 4 : warps > 2 ? 2 : 1; o > 0; o >>= 1)
             ss = plus(ss, {__shfl_xor_sync(kFull, ss.hi, o), __shfl_xor_sync(kFull, ss.lo, o)});
         __syncwarp();
-        if (lane == 0) red[0] = rstd_of(ss, width, eps);
+        if (lane == 0) red[0] = rstd_of(ss, width, eps, lift);
     }
     __syncthreads();
     return red[0];
@@ -173,25 +215,26 @@ __global__ void __launch_bounds__(kPer == 1 ? 1024 : 512, 1) rmsnorm_q8_kernel(c
             if (b0 < step) kept[j] = v[j];
         }
     }
-    Sum rstd = row_rstd(red, hi, lo, (float)width, eps);
+    Sum rstd = row_rstd(red, hi, lo, (float)width, eps, kLift);
     // squares beyond fp32's range, or lost below it: the row again times a power of two
-    const float scale = !(rstd.hi >= 0x1p-62f) ? 0x1p-80f : rstd.hi > 0x1p50f ? 0x1p80f : 1.f;
-    if (scale != 1.f) {
+    const int up = !(rstd.hi >= exp2i(kLift - 62)) ? -80 : rstd.hi > exp2i(kLift + 50) ? 96 : 0;
+    if (up != 0) {
+        const float scale = exp2i(up);
         hi = lo = make_float2(0.f, 0.f);
         for (int b0 = warp * kPer; b0 < stride; b0 += step) {
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
                 const int c = (b0 + j) * kBlock + 4 * lane;
-                float4 v = b0 < step ? kept[j] : c < width ? load4(r + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-                v = make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
-                add_squares(hi, lo, make_float2(v.x, v.y));
-                add_squares(hi, lo, make_float2(v.z, v.w));
-                if (b0 < step) kept[j] = v;
+                const float4 v = b0 < step ? kept[j] : c < width ? load4(r + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+                add_squares(hi, lo, make_float2(v.x * scale, v.y * scale));
+                add_squares(hi, lo, make_float2(v.z * scale, v.w * scale));
             }
         }
-        rstd = row_rstd(red, hi, lo, (float)width, eps * scale * scale);
+        rstd = row_rstd(red, hi, lo, (float)width, eps * scale * scale, 0);
     }
     const float near = rstd.hi + rstd.lo;
+    constexpr unsigned kLeast = (unsigned)(127 + kLift - 17) << 23;
+    bool again = up != 0;   // what fp32 may not hold all of, nor in a row that was taken times a power of two
     for (int b0 = warp * kPer; b0 < stride; b0 += step) {
         unsigned word = 0;
 #pragma unroll
@@ -199,37 +242,58 @@ __global__ void __launch_bounds__(kPer == 1 ? 1024 : 512, 1) rmsnorm_q8_kernel(c
             const int c = (b0 + j) * kBlock + 4 * lane;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f), g = v;
             if (c < width) {
-                v = kept[j];
-                if (b0 >= step) {
-                    v = load4(r + c);
-                    v = make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
-                }
+                v = b0 < step ? kept[j] : load4(r + c);
                 g = load4(w + c);
             }
             // within 2^-22 of the norm: times 1 - 2^-21 and 1 + 2^-21 it is rounded to the same value, or it is near a border
             const float2 v0 = make_float2(v.x, v.y), v1 = make_float2(v.z, v.w), g0 = make_float2(g.x, g.y), g1 = make_float2(g.z, g.w);
             float2 y0 = mul2(mul2(v0, splat(near)), g0), y1 = mul2(mul2(v1, splat(near)), g1);
             float top = fmaxf(fmaxf(fabsf(y0.x), fabsf(y0.y)), fmaxf(fabsf(y1.x), fabsf(y1.y)));   // passes NaN over
-            unsigned most = warp_max(__float_as_uint(top));
-            int e = block_exponent(most);
+            const unsigned most = warp_max(__float_as_uint(top));
+            int e = block_exponent(most, kLift);
             const float inv = exp2i(-e);
             unsigned bytes = round4(y0, y1, inv * (1.f - 0x1p-21f));
-            const bool border = bytes != round4(y0, y1, inv * (1.f + 0x1p-21f)) || most >= 0x7f7ffff0u ||
-                                most < 0x0d000000u ||   // what is subnormal in fp32 is nothing in the block's units above that
-                                ((most + 8u) & 0x7fffffu) - 0x600000u <= 16u;
+            const bool border = bytes != round4(y0, y1, inv * (1.f + 0x1p-21f)) || ((most + 8u) & 0x7fffffu) - 0x600000u <= 16u;
+            // Where the largest value is 2^-17 or more, what is not rounded to zero is above 2^-37, so v * rstd above 2^-165
+            // whatever the weights are. Below that, and beyond 2^64, fp32 may not hold what it takes. (Zeros are zeros, or
+            // below 2^-213.)
+            again = again || (most != 0u && (most < kLeast || most >= 0x7f7ffff0u));
             if (__any_sync(kFull, border) && most != 0u) {
                 y0 = normalized(v0, g0, rstd);
                 y1 = normalized(v1, g1, rstd);
                 top = fmaxf(fmaxf(fabsf(y0.x), fabsf(y0.y)), fmaxf(fabsf(y1.x), fabsf(y1.y)));
-                e = block_exponent(warp_max(magnitude(top)));
+                e = block_exponent(warp_max(magnitude(top)), kLift);
                 bytes = round4(y0, y1, exp2i(-e));
             }
             if (c < width) *reinterpret_cast<unsigned *>(q + row * width + c) = bytes;
-            word |= (unsigned)(e + 127) << (8 * j);
+            word |= (unsigned)(e - kLift + 127) << (8 * j);
         }
         if (lane == 0) {
             if (kPer == 1) scales[row * stride + b0] = (uint8_t)word;
             else *reinterpret_cast<unsigned *>(scales + row * stride + b0) = word;
+        }
+    }
+    if (!again) return;
+    // This warp's blocks once more (down here: in the loop, never run, this costs 256 x 2304 0.1 us). rstd.hi is normal, or
+    // the row has an infinity, or NaN.
+    const int n = rstd.hi >= 0x1p-126f && rstd.hi <= 0x1p126f ? ilog(rstd.hi) : 0;
+    const Sum r1 = {rstd.hi * exp2i(-n), rstd.lo * exp2i(-n)};
+    const int to = n + (up != 0 ? up : -kLift);
+#pragma unroll 1
+    for (int b0 = warp * kPer; b0 < stride; b0 += step) {
+#pragma unroll 1
+        for (int j = 0; j < kPer; ++j) {
+            const int c = (b0 + j) * kBlock + 4 * lane;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f), g = v;
+            if (c < width) {
+                v = load4(r + c);
+                g = load4(w + c);
+            }
+            const Apart y[4] = {normalized(v.x, g.x, r1, to), normalized(v.y, g.y, r1, to), normalized(v.z, g.z, r1, to),
+                                normalized(v.w, g.w, r1, to)};
+            const uint2 u = round_apart(y);
+            if (c < width) *reinterpret_cast<unsigned *>(q + row * width + c) = u.x;
+            if (lane == 0) scales[row * stride + b0 + j] = (uint8_t)(u.y + 127u);
         }
     }
 }
