@@ -600,8 +600,8 @@ mb_status mb_matmul_q8_form(int64_t rows, int64_t n_out, int64_t width, int32_t 
  *   u      : [n] fp32 in [0, 1) (1 or more: the last token left; below 0 or NaN: the first)
  *   temperature, top_p, min_p : [n] fp32, top_k : [n] int32, or NULL: 1, 1, 0, 0.
  *            A temperature of 0 (or less, or NaN) takes the largest logit, one
- *            above 1e30 makes all weights 1; NaN in top_p or min_p switches that
- *            one off
+ *            above 1e30 makes all weights 1, one below 2^-127 counts as 2^-127;
+ *            NaN in top_p or min_p switches that one off
  *   tokens : [n], MB_TOKEN_I32 or MB_TOKEN_I64; -1 where every token is masked
  *   prob   : [n] fp32 or NULL: the probability the token was drawn with (0 with -1)
  * Weights are within 2^-31 of their value and one unit of 2^-(62 - ceil(log2

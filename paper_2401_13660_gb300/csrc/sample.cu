@@ -59,8 +59,9 @@ __device__ __forceinline__ Scale make_scale(float temperature, float top, int dr
     constexpr float kHi = 1.4426950408889634f, kLo = (float)(1.4426950408889634074 - (double)kHi);
     const bool flat = !(temperature < 1e30f);
     Scale s;
-    s.hi = flat ? 0.f : fminf(__fdiv_rn(kHi, temperature), 3.402823466e38f);
-    s.lo = flat || !(s.hi < 1e38f) ? 0.f : __fdiv_rn(fmaf(-s.hi, temperature, kHi) + kLo, temperature);
+    const float t = fmaxf(temperature, 0x1p-127f);   // log2(e) / T within fp32
+    s.hi = flat ? 0.f : __fdiv_rn(kHi, t);
+    s.lo = flat ? 0.f : __fdiv_rn(fmaf(-s.hi, t, kHi) + kLo, t);
     s.top = flat ? 0.f : top;
     s.drop = drop;
     return s;
