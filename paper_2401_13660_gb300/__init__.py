@@ -10,6 +10,8 @@ _BINDING = ("mb_scan_prefill", "mb_scan_verify", "mb_rollback", "mb_step", "mb_s
             "mb_selftest_timeout", "mb_scan_verify_resume", "mb_conv1d", "mb_conv1d_backward",
             "mb_conv1d_backward_workspace_size", "mb_embed", "mb_embed_backward", "mb_embed_backward_workspace_size",
             "mb_cross_entropy", "mb_tensor_list", "mb_grad_norm", "mb_grad_norm_workspace_size", "mb_grad_clip",
+            "mb_conv_xproj", "mb_conv_xproj_workspace_size", "mb_q8_scale_stride", "mb_rmsnorm_q8", "mb_quantize_q8",
+            "mb_dequantize_q8", "mb_matmul_q8", "mb_matmul_q8_form", "mb_sample",
             "mb_workspace_size", "mb_status_string", "mb_version", "load_library", "MbError",
             "make_args", "new_workspace")
 
