@@ -322,9 +322,6 @@ constexpr int kBins = 2048;          // of the distance to the maximum, kPerOcta
 constexpr float kPerOctave = 32.f;
 constexpr int kList = kThreads;      // tokens that are ranked one against the other
 constexpr int kHead = 256;           // tokens among which a row is finished at once
-#ifndef MB_SAMPLE_CTAS
-#define MB_SAMPLE_CTAS 2
-#endif
 constexpr int kMaxCtas = 8;          // of a row
 
 struct alignas(16) Shared {
@@ -905,7 +902,7 @@ template <typename T> cudaError_t launch(const SampleParams &p, cudaStream_t s) 
     const auto bytes = [&](int ctas) { return sizeof(Shared) + ((size_t)p.vocab / kPer / ctas + 3) * 16; };
     int ctas = 1;
     while (ctas < kMaxCtas && (bytes(ctas) > lim->smem_optin ||
-                               (p.n * ctas * 2 <= MB_SAMPLE_CTAS * (int64_t)lim->sms && p.vocab >= 4096 * ctas)))
+                               (p.n * ctas <= (int64_t)lim->sms && p.vocab >= 4096 * ctas)))
         ctas *= 2;
     const bool keep = bytes(ctas) <= lim->smem_optin;
     const auto kern = !keep      ? sample_long_kernel<T, true, false>
