@@ -547,7 +547,7 @@ mb_status mb_rmsnorm_q8(const void *add, int32_t dtype, float *residual, const f
 mb_status mb_quantize_q8(const void *x, int32_t dtype, int64_t x_stride, int32_t block_rows, uint8_t *q, uint8_t *scales,
                          int64_t rows, int64_t width, void *stream);
 
-/* The values back: out [rows, width] (dtype, rounded once; exact in fp32 but below its range). */
+/* The values back: out [rows, width] (dtype; exact in fp32, rounded once in bf16; infinite beyond the type's range). */
 mb_status mb_dequantize_q8(const uint8_t *q, const uint8_t *scales, int32_t block_rows, void *out, int32_t dtype,
                            int64_t rows, int64_t width, void *stream);
 

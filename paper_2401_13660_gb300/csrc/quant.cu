@@ -385,7 +385,7 @@ __global__ void __launch_bounds__(kQuantThreads) dequantize_kernel(const uint8_t
     const int c = (int)(i - row * groups) * 16;
     const uint4 u = ld16(q + row * width + c);
     const unsigned s = scales[(row >> shift) * stride + c / kBlock];
-    // 2^(s - 127) in two factors: byte 0 is 2^-127, and 255 no number
+    // 2^(s - 127): byte 0 is 2^-127, subnormal, and 255 no number
     const float f = s == 255u ? __uint_as_float(0x7fffffffu) : s == 0u ? __uint_as_float(1u << 22) : __uint_as_float(s << 23);
     const unsigned word[4] = {u.x, u.y, u.z, u.w};
     float v[16];
