@@ -59,11 +59,13 @@ MatmulPlan plan_matmul(int64_t p_rows, int64_t n_out, int64_t width, bool out_bf
     // rows by 32, so that the stores of a tile end in it, or 16 rows alone
     const int fewest = (int)((p_rows + kMaxRows - 1) / kMaxRows), most_rows = (int)((p_rows + kChunk - 1) / kChunk);
     const auto height = [&](int rows) { return p_rows <= 16 ? 16 : (int)((((p_rows + rows - 1) / rows) + kChunk - 1) / kChunk * kChunk); };
-    // Rows of a tile and parts of a sum, where there are fewer tiles than SMs. What they cost is the rows of both operands
-    // that a CTA loads (128 bytes each, two cycles a row), what a cluster costs over single CTAs, some 0.5 us, with adding up,
-    // 10 ns to a row, and 1 us more where the clusters do not fit the GPU side by side. Microseconds with the fewest tiles
-    // and no parts, with parts, with what this rule takes: 1 x 2048 x 1024 6.7, 5.0, 4.7; 256 x 1024 x 2304 5.7, 8.7, 4.8;
-    // 200 x 4608 x 2304 21, -, 9.8; 384 x 4608 x 2304 -, 12.1, 11.1; 128 x 2304 x 4608 8.7, -, 6.9.
+    // Rows of a tile and parts of a sum, where there are fewer tiles than SMs, by what they cost. The unit is a row of one of
+    // the operands that a CTA loads for a block of the sum (128 bytes, two cycles, some 1 ns); what a cluster costs over
+    // single CTAs, what adding up costs for a row, and what it costs that the clusters do not fit the GPU side by side are
+    // fitted to the times of whole products. Microseconds (launches one after the other in a graph) with the fewest tiles
+    // and no parts, with the parts that the rule would take of those, with what it takes: 1 x 2048 x 1024 4.6, 3.6, 3.6;
+    // 256 x 1024 x 2304 4.9, 4.9, 4.3; 200 x 4608 x 2304 16.1, 11.5, 9.4; 384 x 4608 x 2304 15.8, 12.3, 10.6;
+    // 128 x 2304 x 4608 7.4, 7.4, 6.2.
     t.rows = fewest;
     t.split = 1;
     const auto cost = [&](int rows, int split) {
@@ -74,9 +76,10 @@ MatmulPlan plan_matmul(int64_t p_rows, int64_t n_out, int64_t width, bool out_bf
     for (int rows = fewest; round && rows <= most_rows && t.features * rows <= lim.sms; ++rows)
         for (int split = 1; split <= kMaxSplit && t.features * rows * split <= lim.sms && 4 * split <= std::max(t.blocks, 4); split *= 2)
             if ((split <= 2 || clusters(split) > 0) && cost(rows, split) < cost(t.rows, t.split)) t.rows = rows, t.split = split;
-    // Pairs of CTAs load half of a tile's rows each, but wait for one another, some 1.4 us. Microseconds of single CTAs and
-    // pairs: 1024 x 2304 x 2304 8.7, 10.7; 2048 x 4608 x 1024 13.0, 15.1; 4096 x 4608 x 768 17.7, 16.4. Tiles in several
-    // rounds: 200 x 2304 x 32000 24.9, 21.7; 64 x 1024 x 32000 9.2, 11.5.
+    // Pairs of CTAs load half of a tile's rows each, but wait for one another: 2800 of those units, fitted in the same way.
+    // Microseconds of single CTAs and pairs: 1024 x 2304 x 2304 8.1, 10.1; 256 x 2304 x 9216 8.5, 10.4; 2048 x 4608 x 1024
+    // 12.7, 14.7; 4096 x 4608 x 768 17.5, 16.6. Tiles in several rounds: 200 x 2304 x 32000 24.2, 20.4; 64 x 1024 x 32000
+    // 8.6, 10.6.
     const int pairs = (t.features + 1) / 2, pair_rows = std::max(fewest, std::min(most_rows, lim.sms / 2 / pairs));
     const bool pair = n_out > kFeatures && p_rows > kPairRows &&
                       (!round || cost(t.rows, t.split) > (int64_t)t.blocks * (kFeatures + height(pair_rows) / 2) + 2800);
@@ -88,14 +91,14 @@ MatmulPlan plan_matmul(int64_t p_rows, int64_t n_out, int64_t width, bool out_bf
     plan.ctas = pair ? 2 : 1;
     t.height = height(t.rows);
     t.rows = (int)((p_rows + t.height - 1) / t.height);
-    t.band = t.rows > 16 ? 4 : 1;   // 65536 x 1024 x 4096: 190 us, with 1 202; 256 x 2304 x 9216: 11.9 and 11.1
+    t.band = t.rows > 16 ? 4 : 1;   // 65536 x 1024 x 4096: 190 us, with 1 204
     const int64_t tiles = (int64_t)t.features * t.rows;
     plan.team = pair ? 2 : t.split;
     const bool one = tiles <= lim.sms / plan.team;   // tile to a CTA (or team)
     const int unit = (kFeatures + t.height / plan.ctas) * kK;
     const bool tight = t.split > 2 && tiles > clusters(t.split);
     // What a stage costs the warp that issues its products, some 250 cycles beside them, is little next to 4 x 128 columns of
-    // few rows (1 x 2304 x 9216: 8.4 -> 6.1 us, 256 x 2304 x 9216: 11.5 -> 9.7); a pair's products hide it.
+    // few rows (1 x 2304 x 9216: 7.8 us, of two 6.0, of four 5.3; 256 x 2304 x 9216: 9.9, of two 8.6); a pair's products hide it.
     t.deep = pair || tight ? 1 : unit <= 20 * 1024 ? 4 : unit <= 32 * 1024 ? 2 : 1;
     const int stage = t.deep * unit, share = ((t.blocks + t.deep - 1) / t.deep + t.split - 1) / t.split;   // stages of a tile
     const int chunk = kChunk * kFeatures * (out_bf16 ? 2 : 4);
@@ -105,8 +108,8 @@ MatmulPlan plan_matmul(int64_t p_rows, int64_t n_out, int64_t width, bool out_bf
     t.held = one || out_bf16 ? halves : (halves + 1) / 2;
     const size_t fixed = 1024 + kSlots * kSlotBytes + (one ? 0 : (size_t)kGroups * t.held * chunk);
     const size_t most = lim.smem_optin - kBarrierBytes, beside = lim.smem_sm / 2 - lim.smem_reserved - kBarrierBytes;
-    // as deep as it may be (256 x 2304 x 9216: 6 stages 10.7 us, 3 stages and room for the next kernel's CTA 12.8), but where
-    // the clusters would not fit the GPU side by side then, two CTAs to an SM
+    // as deep as it may be (256 x 2304 x 9216: three stages of two blocks 8.5 us, two 10.0), but where the clusters would not
+    // fit the GPU side by side then, two CTAs to an SM
     t.stages = std::min((int)(((tight ? beside : most) - fixed) / stage), kMaxStages);
     if (one) t.stages = std::min(t.stages, share);
     const size_t parts = one ? std::max((size_t)kGroups * t.held * chunk, t.split > 1 ? (size_t)t.height * kFeatures * 4 : 0) : 0;
